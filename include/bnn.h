@@ -348,6 +348,107 @@ int bnn_gemm_i8_mfma(const int8_t *A, int64_t lda, const int8_t *B, int64_t ldb,
 int bnn_unpack_i8(const uint32_t *in, int64_t ld_in, int64_t rows, int64_t K,
                   int8_t *out, int64_t ld_out, void *stream);
 
+/* ---- real activations, packed weights: the feed-forward block of a language model with one-bit weights --------------
+ *
+ * Activations are real matrices of one of three types; weights are packed rows as everywhere in this file (bit 1 = +1),
+ * each output channel with an optional real scale.  Sums, statistics and activations are held in float32; a result is
+ * rounded once, when it is written.  Rows may start at any address that is a multiple of the element, and a leading
+ * dimension is any count of elements from the row's length on.  Vectors (scale, bias, gamma, beta and their gradients)
+ * are contiguous float32.
+ */
+typedef enum bnn_type { BNN_BF16 = 0, BNN_F16 = 1, BNN_F32 = 2 } bnn_type;
+
+typedef enum bnn_act {
+    BNN_ACT_NONE = 0,
+    BNN_ACT_RELU = 1,      /* max(z, 0); derivative at 0: 0 */
+    BNN_ACT_SILU = 2,      /* z / (1 + e^-z) */
+    BNN_ACT_GELU = 3,      /* z/2 (1 + erf(z / sqrt 2)) */
+    BNN_ACT_GELU_TANH = 4, /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+    BNN_ACT_SIGMOID = 5    /* 1 / (1 + e^-z) */
+} bnn_act;
+
+typedef enum bnn_norm {
+    BNN_NORM_NONE = 0,     /* v */
+    BNN_NORM_RMS = 1,      /* v / sqrt(mean(v^2) + eps) * gamma */
+    BNN_NORM_LAYER = 2     /* (v - mean(v)) / sqrt(var(v) + eps) * gamma + beta */
+} bnn_norm;
+
+/*
+ * A product with its epilogue, one launch:
+ *   y[m][n] = act(scale[n] * sum_{k<K} x[m][k] w[n][k] + bias[n]) + residual[m][n]
+ *   x [M][ld_x], residual [M][ld_r] (or NULL), y [M][ld_y] of `type`; w [N][ld_w] packed rows of K bits;
+ *   scale, bias [N] or NULL (1 and 0).
+ * y may be residual itself (same address and leading dimension); nothing else may overlap.  K == 0 is a sum of nothing.
+ */
+int bnn_linear_bits(int type, const void *x, int64_t ld_x, const uint32_t *w, int64_t ld_w, const float *scale,
+                    const float *bias, int act, const void *residual, int64_t ld_r, void *y, int64_t ld_y,
+                    int64_t M, int64_t N, int64_t K, void *stream);
+
+/*
+ * The gated feed-forward's first half, one launch: both projections, the activation and their product,
+ *   h[m][f] = act(z[m][f]) * z[m][F + f],   z = scale * (x w^T) + bias
+ *   w [2F][ld_w]: the F rows of the gate, then the F rows of the other projection; scale, bias [2F] or NULL;
+ *   h [M][ld_h].
+ */
+int bnn_gated_bits(int type, const void *x, int64_t ld_x, const uint32_t *w, int64_t ld_w, const float *scale,
+                   const float *bias, int act, void *h, int64_t ld_h, int64_t M, int64_t F, int64_t K, void *stream);
+
+/*
+ * Backward passes.  With s = x w^T, z = scale * s + bias and dz the gradient of z:
+ *   linear:  dz = dy * act'(z)
+ *   gated:   dz[m][f] = dh * z[m][F + f] * act'(z[m][f]),   dz[m][F + f] = dh * act(z[m][f])
+ *   dx = (dz * scale) w          [M][ld_dx] of `type`
+ *   dw = (dz * scale)^T x        [N][ld_dw] of `type`: the gradient of the weights as if they were real, which a
+ *                                straight-through estimator hands to the values that were binarized (Alg. 1, the
+ *                                backward propagation's g_W)
+ *   dscale[n] = sum_m dz s,  dbias[n] = sum_m dz     float32
+ * (dresidual is dy.)  Any of dx, dw, dscale, dbias may be NULL: not wanted.  dz * scale is rounded to `type` before the two
+ * products that read it.  Sums over rows are made in an order that depends on the sizes alone.
+ * workspace: 16-byte aligned device memory of at least the bytes that the _workspace function returns for the same sizes
+ * (-1 for sizes or a type that the call would refuse); what it holds before and after means nothing.
+ */
+int64_t bnn_linear_bits_backward_workspace(int type, int64_t M, int64_t N, int64_t K, int act);
+int bnn_linear_bits_backward(int type, const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const uint32_t *w,
+                             int64_t ld_w, const float *scale, const float *bias, int act, void *dx, int64_t ld_dx,
+                             void *dw, int64_t ld_dw, float *dscale, float *dbias, int64_t M, int64_t N, int64_t K,
+                             void *workspace, int64_t workspace_bytes, void *stream);
+int64_t bnn_gated_bits_backward_workspace(int type, int64_t M, int64_t F, int64_t K, int act);
+int bnn_gated_bits_backward(int type, const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const uint32_t *w,
+                            int64_t ld_w, const float *scale, const float *bias, int act, void *dx, int64_t ld_dx,
+                            void *dw, int64_t ld_dw, float *dscale, float *dbias, int64_t M, int64_t F, int64_t K,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * What stands between two blocks, one launch: the norm after a block, its gate and residual scale, the sum with the
+ * stream, and the norm before the next block,
+ *   t = post(y),   r[m] = x[m] + res_scale * gate[m / rows_per_gate] * t[m],   n = pre(r)
+ *   y, x (or NULL: 0), r, n [M][ld] of `type`, rows of D; gate [ceil(M / rows_per_gate)][ld_gate] of `type` or NULL (1);
+ *   post, pre: bnn_norm, with gamma [D] or NULL (1) and beta [D] or NULL (0; only with BNN_NORM_LAYER).
+ * r may be NULL (not wanted) or x itself (same address and leading dimension); n must be NULL exactly if pre is
+ * BNN_NORM_NONE.  n is taken of the unrounded r.  rows_per_gate >= 1 also where gate is NULL.
+ */
+int bnn_norm_residual(int type, const void *y, int64_t ld_y, const void *x, int64_t ld_x, const void *gate,
+                      int64_t ld_gate, int64_t rows_per_gate, float res_scale, int post, const float *post_gamma,
+                      const float *post_beta, int pre, const float *pre_gamma, const float *pre_beta, float eps, void *r,
+                      int64_t ld_r, void *n, int64_t ld_n, int64_t M, int64_t D, void *stream);
+
+/*
+ * Its backward pass, from dr (the gradient of r by every other way, or NULL: 0) and dn (the gradient of n; NULL exactly if
+ * pre is BNN_NORM_NONE), with y and r as the forward pass had them (r is read only if pre is a norm):
+ *   d = dr + pre'(dn);   dx = d;   dgate[g] = sum over the gate's rows of res_scale * d * t;   dy = post'(res_scale * gate * d)
+ * dx, dy [M][ld] and dgate [ceil(M / rows_per_gate)][ld_dgate] of `type`; the gradients of the gammas and betas [D] float32.
+ * Any output may be NULL.  The gradient of an absent gate cannot be asked for, that of an absent gamma or beta can (it is
+ * the one at 1 or 0); betas only with BNN_NORM_LAYER, gammas only with a norm.  workspace as above.
+ */
+int64_t bnn_norm_residual_backward_workspace(int64_t M, int64_t D, int64_t rows_per_gate);
+int bnn_norm_residual_backward(int type, const void *dr, int64_t ld_dr, const void *dn, int64_t ld_dn, const void *y,
+                               int64_t ld_y, const void *r, int64_t ld_r, const void *gate, int64_t ld_gate,
+                               int64_t rows_per_gate, float res_scale, int post, const float *post_gamma,
+                               const float *post_beta, int pre, const float *pre_gamma, float eps, void *dx, int64_t ld_dx,
+                               void *dy, int64_t ld_dy, void *dgate, int64_t ld_dgate, float *dpost_gamma,
+                               float *dpost_beta, float *dpre_gamma, float *dpre_beta, int64_t M, int64_t D,
+                               void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

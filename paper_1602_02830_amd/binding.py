@@ -25,6 +25,10 @@ POOL_APART, POOL_IN_CONV, POOL_WINDOWS = range(3)
 (KERNEL_AUTO, KERNEL_NAIVE, KERNEL_TILED128, KERNEL_KSPLIT, KERNEL_TILED64, KERNEL_MFMA, KERNEL_MFMA128,
  KERNEL_MFMA_SHORTK, KERNEL_MFMA_PERSIST, KERNEL_MFMA_BIG, KERNEL_MFMA_SPLITK) = range(11)
 
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_SIGMOID = range(6)
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}         # bnn_type
+
 _i64 = ctypes.c_int64
 _int = ctypes.c_int
 _ptr = ctypes.c_void_p
@@ -59,6 +63,20 @@ _SIGNATURES = {
     "bnn_maxpool_bits": (_int, [_ptr, _i64, _i64, _i64, _i64, _int, _int, _int, _ptr, _ptr, _ptr]),
     "bnn_gemm_i8_mfma": (_int, [_ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _i64, _i64, _ptr]),
     "bnn_unpack_i8": (_int, [_ptr, _i64, _i64, _i64, _ptr, _i64, _ptr]),
+    "bnn_linear_bits": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _ptr, _i64, _ptr, _i64, _i64, _i64, _i64, _ptr]),
+    "bnn_gated_bits": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _ptr, _i64, _i64, _i64, _i64, _ptr]),
+    "bnn_linear_bits_backward_workspace": (_i64, [_int, _i64, _i64, _i64, _int]),
+    "bnn_linear_bits_backward": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _ptr, _i64, _ptr, _i64,
+                                        _ptr, _ptr, _i64, _i64, _i64, _ptr, _i64, _ptr]),
+    "bnn_gated_bits_backward_workspace": (_i64, [_int, _i64, _i64, _i64, _int]),
+    "bnn_gated_bits_backward": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _ptr, _i64, _ptr, _i64,
+                                       _ptr, _ptr, _i64, _i64, _i64, _ptr, _i64, _ptr]),
+    "bnn_norm_residual": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _f32, _int, _ptr, _ptr, _int, _ptr, _ptr, _f32,
+                                 _ptr, _i64, _ptr, _i64, _i64, _i64, _ptr]),
+    "bnn_norm_residual_backward_workspace": (_i64, [_i64, _i64, _i64]),
+    "bnn_norm_residual_backward": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _f32, _int,
+                                          _ptr, _ptr, _int, _ptr, _f32, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _ptr,
+                                          _ptr, _i64, _i64, _ptr, _i64, _ptr]),
 }
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -581,3 +599,227 @@ def unpack_i8(bits: torch.Tensor, K: int, ld_out: int | None = None) -> torch.Te
     buf = torch.empty((rows, ld), dtype=torch.int8, device=bits.device)
     _check("bnn_unpack_i8", lib.bnn_unpack_i8(bits.data_ptr(), _ld(bits), rows, K, buf.data_ptr(), ld, _stream(buf)))
     return buf[:, :K] if ld != K else buf
+
+
+# ---- real activations, packed weights --------------------------------------------------------------------------
+
+def _real(t: torch.Tensor, name: str, like: torch.Tensor | None = None):
+    """A matrix of real activations; of the type and on the device of `like`."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be bfloat16, float16 or float32, got {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be 2-D with unit stride along its rows")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    return t
+
+
+def _sized(t: torch.Tensor, rows: int, cols: int, name: str, like: torch.Tensor):
+    _real(t, name, like)
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be [{rows}][{cols}], got {list(t.shape)}")
+    return t
+
+
+def _vector(t: torch.Tensor | None, n: int, name: str, like: torch.Tensor):
+    """Address of a float32 vector of n elements, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 vector of {n} elements on {like.device}")
+    return t.data_ptr()
+
+
+def _weights(x: torch.Tensor, w_bits: torch.Tensor):
+    _dev(w_bits, torch.int32, "w_bits")
+    if w_bits.device != x.device:
+        raise ValueError(f"w_bits must be on {x.device}")
+    if w_bits.shape[1] < words_per_row(x.shape[1]):
+        raise ValueError("packed weights have fewer words per row than x has columns")
+
+
+def _at(t: torch.Tensor | None):
+    """Address and leading dimension of a matrix; (None, 0) where there is none."""
+    return (None, 0) if t is None else (t.data_ptr(), _ld(t))
+
+
+def _workspace(workspace: torch.Tensor | None, size: int, like: torch.Tensor, fn: str) -> torch.Tensor:
+    if size < 0:
+        raise ValueError(f"{fn} takes no such sizes")
+    if workspace is None:
+        return torch.empty(size, dtype=torch.uint8, device=like.device)
+    if workspace.dtype != torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {like.device}")
+    if workspace.numel() < size:
+        raise ValueError(f"workspace holds {workspace.numel()} bytes, {size} are needed")
+    return workspace
+
+
+def linear_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                act: int = ACT_NONE, residual: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """bnn_linear_bits: real x [M][K], packed weights [N][ceil(K/32)] -> act(scale * (x w^T) + bias) + residual [M][N].
+    `out` may be `residual`."""
+    lib = load_library()
+    _real(x, "x")
+    _weights(x, w_bits)
+    (M, K), N = x.shape, w_bits.shape[0]
+    if residual is not None:
+        _sized(residual, M, N, "residual", x)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    _sized(out, M, N, "out", x)
+    _check("bnn_linear_bits",
+           lib.bnn_linear_bits(_TYPES[x.dtype], *_at(x), *_at(w_bits), _vector(scale, N, "scale", x), _vector(bias, N, "bias", x), act,
+                               *_at(residual), *_at(out), M, N, K, _stream(x)))
+    return out
+
+
+def _halves(w_bits: torch.Tensor) -> int:
+    if w_bits.shape[0] % 2:
+        raise ValueError("gated weights are the gate's rows and as many of the other projection")
+    return w_bits.shape[0] // 2
+
+
+def gated_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               act: int = ACT_SILU, out: torch.Tensor | None = None) -> torch.Tensor:
+    """bnn_gated_bits: real x [M][K], packed weights [2F][ceil(K/32)] (the gate's rows first) -> act(z_gate) * z_up [M][F]
+    with z = scale * (x w^T) + bias."""
+    lib = load_library()
+    _real(x, "x")
+    _weights(x, w_bits)
+    (M, K), F = x.shape, _halves(w_bits)
+    if out is None:
+        out = torch.empty((M, F), dtype=x.dtype, device=x.device)
+    _sized(out, M, F, "out", x)
+    _check("bnn_gated_bits",
+           lib.bnn_gated_bits(_TYPES[x.dtype], *_at(x), *_at(w_bits), _vector(scale, 2 * F, "scale", x),
+                              _vector(bias, 2 * F, "bias", x), act, *_at(out), M, F, K, _stream(x)))
+    return out
+
+
+def _real_type(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise ValueError(f"activations are bfloat16, float16 or float32, not {dtype}")
+    return _TYPES[dtype]
+
+
+def linear_bits_backward_workspace(dtype: torch.dtype, M: int, N: int, K: int, act: int = ACT_NONE) -> int:
+    """bnn_linear_bits_backward_workspace: bytes."""
+    return load_library().bnn_linear_bits_backward_workspace(_real_type(dtype), M, N, K, act)
+
+
+def gated_bits_backward_workspace(dtype: torch.dtype, M: int, F: int, K: int, act: int = ACT_SILU) -> int:
+    """bnn_gated_bits_backward_workspace: bytes."""
+    return load_library().bnn_gated_bits_backward_workspace(_real_type(dtype), M, F, K, act)
+
+
+def _bits_backward(name, dy, x, w_bits, cols, scale, bias, act, need_dx, need_dw, workspace):
+    lib = load_library()
+    _real(x, "x")
+    _weights(x, w_bits)
+    (M, K), N = x.shape, w_bits.shape[0]
+    _sized(dy, M, cols, "the gradient of the result", x)
+    size = getattr(lib, name + "_workspace")(_TYPES[x.dtype], M, cols, K, act)
+    at_scale, at_bias = _vector(scale, N, "scale", x), _vector(bias, N, "bias", x)
+    ws = _workspace(workspace, size, x, name)
+    dx = torch.empty((M, K), dtype=x.dtype, device=x.device) if need_dx else None
+    dw = torch.empty((N, K), dtype=x.dtype, device=x.device) if need_dw else None
+    dscale = torch.empty(N, dtype=torch.float32, device=x.device) if scale is not None else None
+    dbias = torch.empty(N, dtype=torch.float32, device=x.device) if bias is not None else None
+    _check(name, getattr(lib, name)(_TYPES[x.dtype], *_at(dy), *_at(x), *_at(w_bits), at_scale, at_bias, act, *_at(dx), *_at(dw),
+                                    None if dscale is None else dscale.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                                    M, cols, K, ws.data_ptr(), ws.numel(), _stream(x)))
+    return {"dx": dx, "dw": dw, "dscale": dscale, "dbias": dbias}
+
+
+def linear_bits_backward(dy: torch.Tensor, x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None,
+                         bias: torch.Tensor | None = None, act: int = ACT_NONE, need_dx: bool = True, need_dw: bool = True,
+                         workspace: torch.Tensor | None = None) -> dict:
+    """bnn_linear_bits_backward: {"dx" [M][K], "dw" [N][K], "dscale" [N], "dbias" [N]}, None for what was not there or not
+    wanted.  dw is the gradient of the weights as real numbers; the residual's gradient is dy."""
+    return _bits_backward("bnn_linear_bits_backward", dy, x, w_bits, w_bits.shape[0], scale, bias, act, need_dx, need_dw, workspace)
+
+
+def gated_bits_backward(dh: torch.Tensor, x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None,
+                        bias: torch.Tensor | None = None, act: int = ACT_SILU, need_dx: bool = True, need_dw: bool = True,
+                        workspace: torch.Tensor | None = None) -> dict:
+    """bnn_gated_bits_backward: as linear_bits_backward, with dw [2F][K], dscale and dbias [2F]."""
+    return _bits_backward("bnn_gated_bits_backward", dh, x, w_bits, _halves(w_bits), scale, bias, act, need_dx, need_dw, workspace)
+
+
+def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Tensor | None = None, res_scale: float = 1.0,
+                  post: int = NORM_NONE, post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None,
+                  pre: int = NORM_NONE, pre_gamma: torch.Tensor | None = None, pre_beta: torch.Tensor | None = None,
+                  eps: float = 1e-5, rows_per_gate: int = 1, out: torch.Tensor | None = None, out_n: torch.Tensor | None = None):
+    """bnn_norm_residual: (r, n) with r = x + res_scale * gate * post(y) and n = pre(r); n is None without a `pre` norm.
+    Row m has the gate's row m // rows_per_gate.  `out` may be `x`."""
+    lib = load_library()
+    _real(y, "y")
+    M, D = y.shape
+    if x is not None:
+        _sized(x, M, D, "x", y)
+    if gate is not None:
+        if rows_per_gate < 1:
+            raise ValueError("rows_per_gate must be positive")
+        _sized(gate, -(-M // rows_per_gate), D, "gate", y)
+    if out is None:
+        out = torch.empty((M, D), dtype=y.dtype, device=y.device)
+    _sized(out, M, D, "out", y)
+    if pre == NORM_NONE:
+        if out_n is not None:
+            raise ValueError("out_n needs a norm before the next block")
+    elif out_n is None:
+        out_n = torch.empty((M, D), dtype=y.dtype, device=y.device)
+    if out_n is not None:
+        _sized(out_n, M, D, "out_n", y)
+    _check("bnn_norm_residual",
+           lib.bnn_norm_residual(_TYPES[y.dtype], *_at(y), *_at(x), *_at(gate), rows_per_gate, res_scale, post,
+                                 _vector(post_gamma, D, "post_gamma", y), _vector(post_beta, D, "post_beta", y), pre,
+                                 _vector(pre_gamma, D, "pre_gamma", y), _vector(pre_beta, D, "pre_beta", y), eps,
+                                 *_at(out), *_at(out_n), M, D, _stream(y)))
+    return out, out_n
+
+
+def norm_residual_backward_workspace(M: int, D: int, rows_per_gate: int = 1) -> int:
+    """bnn_norm_residual_backward_workspace: bytes."""
+    return load_library().bnn_norm_residual_backward_workspace(M, D, rows_per_gate)
+
+
+def norm_residual_backward(dr: torch.Tensor | None, dn: torch.Tensor | None, y: torch.Tensor, r: torch.Tensor | None,
+                           gate: torch.Tensor | None = None, res_scale: float = 1.0, post: int = NORM_NONE,
+                           post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None, pre: int = NORM_NONE,
+                           pre_gamma: torch.Tensor | None = None, pre_beta: torch.Tensor | None = None, eps: float = 1e-5,
+                           rows_per_gate: int = 1, need_dx: bool = True, workspace: torch.Tensor | None = None) -> dict:
+    """bnn_norm_residual_backward: {"dx", "dy", "dgate", "dpost_gamma", "dpost_beta", "dpre_gamma", "dpre_beta"}, None for
+    what was not there or not wanted, from the gradients dr of r (by every way but n) and dn of n."""
+    lib = load_library()
+    _real(y, "y")
+    M, D = y.shape
+    for t, name in ((dr, "dr"), (dn, "dn"), (r, "r")):
+        if t is not None:
+            _sized(t, M, D, name, y)
+    if gate is not None:
+        if rows_per_gate < 1:
+            raise ValueError("rows_per_gate must be positive")
+        _sized(gate, -(-M // rows_per_gate), D, "gate", y)
+    if pre != NORM_NONE and (dn is None or r is None):
+        raise ValueError("a norm before the next block needs dn and r")
+    if pre == NORM_NONE and dn is not None:
+        raise ValueError("dn needs a norm before the next block")
+    vectors = {"post_gamma": post_gamma, "post_beta": post_beta, "pre_gamma": pre_gamma, "pre_beta": pre_beta}
+    at = {k: _vector(v, D, k, y) for k, v in vectors.items()}
+    ws = _workspace(workspace, lib.bnn_norm_residual_backward_workspace(M, D, rows_per_gate), y, "bnn_norm_residual_backward")
+    got = {"dx": torch.empty((M, D), dtype=y.dtype, device=y.device) if need_dx else None,
+           "dy": torch.empty((M, D), dtype=y.dtype, device=y.device),
+           "dgate": torch.empty(tuple(gate.shape), dtype=y.dtype, device=y.device) if gate is not None else None}
+    for k, v in vectors.items():
+        got["d" + k] = torch.empty(D, dtype=torch.float32, device=y.device) if v is not None else None
+    _check("bnn_norm_residual_backward",
+           lib.bnn_norm_residual_backward(_TYPES[y.dtype], *_at(dr), *_at(dn), *_at(y), *_at(r), *_at(gate), rows_per_gate, res_scale,
+                                          post, at["post_gamma"], at["post_beta"], pre, at["pre_gamma"], eps, *_at(got["dx"]),
+                                          *_at(got["dy"]), *_at(got["dgate"]),
+                                          *(None if got["d" + k] is None else got["d" + k].data_ptr() for k in vectors), M, D,
+                                          ws.data_ptr(), ws.numel(), _stream(y)))
+    return got

@@ -22,7 +22,7 @@ ARCH = "gfx950"
 HIP_SOURCES = ["pack_sign.hip", "xnor_gemm.hip", "xnor_gemm_mfma.hip", "xnor_gemm_mfma_shortk.hip",
                "xnor_gemm_mfma_persist.hip", "xnor_gemm_mfma_big.hip", "xnor_gemm_mfma_splitk.hip", "xnor_gemm_mfma_strip.hip", "sign_gemm.hip",
                "bn_sign_pack.hip", "im2col_pack.hip", "conv_implicit.hip", "conv_patch.hip", "conv_strip.hip", "gemm_i8_mfma.hip",
-               "bitplane_gemm.hip", "valu_fallbacks.hip"]
+               "bitplane_gemm.hip", "valu_fallbacks.hip", "linear_bits.hip", "bits_backward.hip", "norm_residual.hip"]
 HOST_SOURCES = ["bn_fold.cpp", "api.cpp"]
 
 HIP_FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}",

@@ -1,0 +1,273 @@
+// Backward passes of the products with packed weights: bnn_linear_bits_backward and bnn_gated_bits_backward.
+//
+//   1. the gradient before the scale, ds = dz * scale, in the activations' type.  With an activation (or a gate) the product
+//      of the forward pass is made again and its epilogue turns the sums into ds and the column sums for dscale and dbias
+//      while they are in registers; without one, dz is dy: a pass over dy makes ds and dbias (nothing at all without a scale).
+//   2. dx = ds w: the same tile product as forwards, on the weights' bits transposed (a 16th or a 32nd of an operand's bytes).
+//   3. dw = ds^T x.  Without an activation it is made of dy itself, the scale put on the sums, and
+//      dscale[n] = sum_k w[n][k] sum_m dy[m][n] x[m][k] comes out of the same sums.
+//   4. column sums of the tiles joined, in a fixed order.
+#include "bit_transpose.h"
+#include "bits_launch.h"
+#include "weight_grad.h"
+
+namespace bnn {
+
+namespace {
+
+// ---- transposed weights ------------------------------------------------------------------------------------------
+// out[k] bit n of a row of `half` columns a half: w[n][k] and, from column `half` on, w[F + n][k]; 0 for rows that are not there.
+// A workgroup turns 512 rows x 128 columns: each half wavefront blocks of 32 x 32 in registers, LDS puts words of a row together.
+constexpr int kTurnWords = 16, kTurnK = 128;
+
+__global__ __launch_bounds__(256) void transpose_weights_kernel(const uint32_t* w, int64_t ld_w, int F, int half, int halves, int K,
+                                                                uint32_t* out, int64_t ld_out, int blocks_k) {
+    __shared__ uint32_t turned[kTurnK][kTurnWords + 1];
+    const int tid = threadIdx.x, half_wave = tid >> 5, l = tid & 31;
+    const int bn = blockIdx.x / uint32_t(blocks_k), bk = int(blockIdx.x) - bn * blocks_k;
+    const int word0 = bn * kTurnWords, k0 = bk * kTurnK, words = half * halves / 32, kw = (K + 31) >> 5;
+#pragma unroll
+    for (int i = 0; i < kTurnWords * 4 / 8; ++i) {
+        const int b = i * 8 + half_wave, wn = b >> 2, q = b & 3;
+        const int c = (word0 + wn) * 32 + l, second = c >= half ? 1 : 0, f = c - second * half;
+        const int kword = (k0 >> 5) + q;
+        uint32_t v = 0;
+        if (word0 + wn < words && f < F && kword < kw) v = w[(int64_t(second) * F + f) * ld_w + kword];
+        turned[q * 32 + l][wn] = transpose_bits_32_lanes(v);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurnK * kTurnWords / 256; ++i) {
+        const int id = i * 256 + tid, row = id / kTurnWords, wn = id % kTurnWords;
+        if (k0 + row < K && word0 + wn < words) out[int64_t(k0 + row) * ld_out + word0 + wn] = turned[row][wn];
+    }
+}
+
+// ---- dy * scale and the column sums of dy ------------------------------------------------------------------------
+// A workgroup takes `strip` rows x 512 columns, a thread eight columns of every fourth row.
+template <typename E>
+__global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t ld_dy, const float* scale, E* ds, int64_t ld_ds,
+                                                            float* part, int M, int N, int strip, int blocks_n) {
+    __shared__ float sums_s[4][512];
+    const int tid = threadIdx.x, c = tid & 63, r = tid >> 6;
+    const int bm = blockIdx.x / uint32_t(blocks_n), bn = int(blockIdx.x) - bm * blocks_n;
+    const int n = bn * 512 + c * 8;
+    const int64_t first = int64_t(bm) * strip, last = min(first + strip, int64_t(M));
+    float sc[8], sum[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sc[i] = scale && n + i < N ? scale[n + i] : 1.0f;
+    for (int64_t m = first + r; m < last; m += 4) {
+        const auto v = load8<E>(dy + m * ld_dy + n, int64_t(N) - n);
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sum[i] += float(v[i]);
+            o[i] = float(v[i]) * sc[i];
+        }
+        if (ds && n < ld_ds) store8<E>(ds + m * ld_ds + n, o, 8);
+    }
+    if (!part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums_s[r][c * 8 + i] = sum[i];
+    __syncthreads();
+    for (int i = tid; i < 512; i += 256)
+        if (bn * 512 + i < N) part[int64_t(bm) * N + bn * 512 + i] = sums_s[0][i] + sums_s[1][i] + sums_s[2][i] + sums_s[3][i];
+}
+
+// out[c] = sum over t of part[t][c].  64 columns a workgroup, four threads each for every fourth t.
+__global__ __launch_bounds__(256) void join_sums_kernel(const float* part, int tiles, int N, float* out) {
+    __shared__ float sums_s[4][64];
+    const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
+    const int64_t n = int64_t(blockIdx.x) * 64 + c;
+    float sum = 0.0f;
+    if (n < N)
+        for (int t = r; t < tiles; t += 4) sum += part[int64_t(t) * N + n];
+    sums_s[r][c] = sum;
+    __syncthreads();
+    if (r == 0 && n < N) out[n] = (sums_s[0][c] + sums_s[1][c]) + (sums_s[2][c] + sums_s[3][c]);
+}
+
+int join_sums(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
+    join_sums_kernel<<<dim3(uint32_t(ceil_div(N, 64))), dim3(256), 0, s>>>(part, int(tiles), int(N), out);
+    return check_launch();
+}
+
+// ---- the plan ----------------------------------------------------------------------------------------------------
+
+constexpr int kBackRows = 128, kStrips = 256;
+
+inline int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
+
+// Everything a call puts into its workspace, by sizes alone.  cols: columns of dy (gated: F).
+struct Plan {
+    int64_t half, halves, ds_cols, wt_ld, strip, part_rows;
+    int64_t ds_at, wt_at, scale_at, bias_at, bytes;
+    bool recompute;
+    Plan(int64_t size, int64_t M, int64_t cols, int64_t K, int act, bool gated) {
+        recompute = gated || act != BNN_ACT_NONE;
+        halves = gated ? 2 : 1;
+        half = round_up(cols, 64);
+        ds_cols = half * halves;
+        wt_ld = round_up(ds_cols / 32, 4);
+        strip = recompute ? kBackRows : round_up(ceil_div(M > 0 ? M : 1, kStrips), 4);
+        part_rows = ceil_div(M, strip);
+        const int64_t channels = halves * cols;
+        const int64_t scale_rows = recompute ? part_rows : ceil_div(K, kGradTile);
+        auto take = [&](int64_t b) {
+            const int64_t at = bytes;
+            bytes += round_up(b, 256);
+            return at;
+        };
+        bytes = 0;
+        ds_at = take(M * ds_cols * size);
+        wt_at = take(K * wt_ld * 4);
+        scale_at = take(scale_rows * channels * 4);
+        bias_at = take(part_rows * channels * 4);
+    }
+};
+
+template <typename E>
+int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w, int64_t ld_w,
+             const float* scale, const float* bias, int act, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, float* dscale,
+             float* dbias, int64_t M, int64_t cols, int64_t K, char* ws, hipStream_t s) {
+    E* const ds = reinterpret_cast<E*>(ws + p.ds_at);
+    uint32_t* const wt = reinterpret_cast<uint32_t*>(ws + p.wt_at);
+    float* const part_scale = reinterpret_cast<float*>(ws + p.scale_at);
+    float* const part_bias = reinterpret_cast<float*>(ws + p.bias_at);
+    const int64_t channels = p.halves * cols;
+    int st = BNN_OK;
+    const void* g = ds;                // what dx is made of
+    int64_t ld_g = p.ds_cols, cols_g = p.ds_cols;
+    if (p.recompute && M > 0 && cols > 0) {
+        ProductArgs a{};
+        a.x = x; a.ld_x = ld_x; a.w = w; a.ld_w = ld_w; a.scale = scale; a.bias = bias; a.act = act;
+        a.dy = dy; a.ld_dy = ld_dy; a.y = ds; a.ld_y = p.ds_cols; a.half = int(p.half); a.channels = int(channels);
+        a.part_scale = dscale ? part_scale : nullptr;
+        a.part_bias = dbias ? part_bias : nullptr;
+        a.M = int(M); a.N = int(cols); a.K = int(K);
+        st = gated ? launch_product<E, kGatedBack, 2, 2, 2, 2>(a, s) : launch_product<E, kLinearBack, 2, 2, 2, 2>(a, s);
+    } else if (!p.recompute) {
+        const bool make_ds = scale && dx;
+        if (!make_ds) {
+            g = dy;
+            ld_g = ld_dy;
+            cols_g = cols;
+        }
+        if (M > 0 && cols > 0 && (make_ds || dbias)) {
+            const int64_t blocks_n = ceil_div(p.half, 512);
+            if (p.part_rows * blocks_n > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
+            scale_and_sum_kernel<E><<<dim3(uint32_t(p.part_rows * blocks_n)), dim3(256), 0, s>>>(
+                static_cast<const E*>(dy), ld_dy, scale, make_ds ? ds : nullptr, p.ds_cols, dbias ? part_bias : nullptr, int(M),
+                int(cols), int(p.strip), int(blocks_n));
+            st = check_launch();
+        }
+    }
+    if (st != BNN_OK) return st;
+    if (dx && M > 0 && K > 0) {
+        if (cols > 0) {
+            const int64_t blocks_n = ceil_div(p.ds_cols / 32, kTurnWords), blocks_k = ceil_div(K, kTurnK);
+            if (blocks_n * blocks_k > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
+            transpose_weights_kernel<<<dim3(uint32_t(blocks_n * blocks_k)), dim3(256), 0, s>>>(
+                w, ld_w, int(cols), int(p.half), int(p.halves), int(K), wt, p.wt_ld, int(blocks_k));
+            if ((st = check_launch()) != BNN_OK) return st;
+        }
+        ProductArgs a{};
+        a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx;
+        a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
+        if ((st = launch_product<E, kLinear, 2, 2, 2, 2>(a, s)) != BNN_OK) return st;
+    }
+    const bool scale_by_k = dscale && !p.recompute;
+    if ((dw || scale_by_k) && cols > 0 && K > 0) {
+        WeightGradArgs a{};
+        a.g = p.recompute ? ds : dy; a.ld_g = p.recompute ? p.ds_cols : ld_dy;
+        a.x = x; a.ld_x = ld_x; a.dw = dw; a.ld_dw = ld_dw;
+        a.row_scale = p.recompute ? nullptr : scale;
+        a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w; a.part = part_scale;
+        a.M = int(M); a.K = int(K); a.cols = int(p.recompute ? p.ds_cols : cols); a.half = int(p.half); a.F = int(cols);
+        const int64_t tiles_n = ceil_div(a.cols, kGradTile), tiles_k = ceil_div(K, kGradTile);
+        if (tiles_n * tiles_k > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
+        a.map = tile_map(tiles_n, tiles_k);
+        weight_grad_kernel<E><<<dim3(uint32_t(tiles_n * tiles_k)), dim3(256), 0, s>>>(a);
+        if ((st = check_launch()) != BNN_OK) return st;
+    }
+    if (dscale && channels > 0) {
+        const int64_t tiles = p.recompute ? p.part_rows : ceil_div(K, kGradTile);
+        if ((st = join_sums(part_scale, tiles, channels, dscale, s)) != BNN_OK) return st;
+    }
+    if (dbias && channels > 0) return join_sums(part_bias, p.part_rows, channels, dbias, s);
+    return BNN_OK;
+}
+
+// Sizes that a call takes; BNN_OK or what it answers.
+int check_sizes(int type, int64_t M, int64_t cols, int64_t K, int act, bool gated) {
+    if (cols < 0 || cols > kMaxDim / 2) return BNN_ERR_INVALID_ARG;
+    const int st = check_product(type, nullptr, K, nullptr, ceil_div(K, 32), nullptr, nullptr, act, 0, gated ? 2 * cols : cols, K);
+    if (st != BNN_OK) return st;
+    if (M < 0 || M > kMaxDim) return BNN_ERR_INVALID_ARG;
+    // Both products have K and the channels as columns and as what is summed over; the tiles' ends stay below 2^31.
+    if (M > kMaxDim - 512 || K > kMaxDim - 512 || cols > kMaxDim / 2 - 512) return BNN_ERR_UNSUPPORTED;
+    return BNN_OK;
+}
+
+int check_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w, int64_t ld_w,
+                   const float* scale, const float* bias, int act, const void* dx, int64_t ld_dx, const void* dw, int64_t ld_dw,
+                   const float* dscale, const float* dbias, int64_t M, int64_t cols, int64_t K, bool gated, const void* ws,
+                   int64_t ws_bytes) {
+    int st = check_sizes(type, M, cols, K, act, gated);
+    if (st != BNN_OK) return st;
+    st = check_product(type, x, ld_x, w, ld_w, scale, bias, act, M, gated ? 2 * cols : cols, K);
+    if (st != BNN_OK) return st;
+    const int64_t size = type_bytes(type);
+    if (ld_dy < cols || ld_dy > kMaxDim || (dx && (ld_dx < K || ld_dx > kMaxDim)) || (dw && (ld_dw < K || ld_dw > kMaxDim)))
+        return BNN_ERR_INVALID_ARG;
+    if (M > 0 && cols > 0 && !dy) return BNN_ERR_INVALID_ARG;
+    if (!aligned_to(dy, size) || !aligned_to(dx, size) || !aligned_to(dw, size) || !aligned_to(dscale, 4) || !aligned_to(dbias, 4) ||
+        !aligned_to(ws, 16))
+        return BNN_ERR_ALIGNMENT;
+    const int64_t need = Plan(size, M, cols, K, act, gated).bytes;
+    if (ws_bytes < need || (need > 0 && !ws)) return BNN_ERR_INVALID_ARG;
+    return BNN_OK;
+}
+
+int run_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w, int64_t ld_w,
+                 const float* scale, const float* bias, int act, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, float* dscale,
+                 float* dbias, int64_t M, int64_t cols, int64_t K, bool gated, void* ws, int64_t ws_bytes, void* stream) {
+    int st = check_backward(type, dy, ld_dy, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M, cols, K,
+                            gated, ws, ws_bytes);
+    if (st != BNN_OK) return st;
+    const Plan p(type_bytes(type), M, cols, K, act, gated);
+    with_type(type, [&](auto e) {
+        st = backward<decltype(e)>(p, gated, dy, ld_dy, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M,
+                                   cols, K, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    });
+    return st;
+}
+
+}  // namespace
+}  // namespace bnn
+
+extern "C" int64_t bnn_linear_bits_backward_workspace(int type, int64_t M, int64_t N, int64_t K, int act) {
+    using namespace bnn;
+    return check_sizes(type, M, N, K, act, false) == BNN_OK ? Plan(type_bytes(type), M, N, K, act, false).bytes : -1;
+}
+
+extern "C" int64_t bnn_gated_bits_backward_workspace(int type, int64_t M, int64_t F, int64_t K, int act) {
+    using namespace bnn;
+    return check_sizes(type, M, F, K, act, true) == BNN_OK ? Plan(type_bytes(type), M, F, K, act, true).bytes : -1;
+}
+
+extern "C" int bnn_linear_bits_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w,
+                                        int64_t ld_w, const float* scale, const float* bias, int act, void* dx, int64_t ld_dx,
+                                        void* dw, int64_t ld_dw, float* dscale, float* dbias, int64_t M, int64_t N, int64_t K,
+                                        void* workspace, int64_t workspace_bytes, void* stream) {
+    return bnn::run_backward(type, dy, ld_dy, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M, N, K, false,
+                             workspace, workspace_bytes, stream);
+}
+
+extern "C" int bnn_gated_bits_backward(int type, const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, const uint32_t* w,
+                                       int64_t ld_w, const float* scale, const float* bias, int act, void* dx, int64_t ld_dx,
+                                       void* dw, int64_t ld_dw, float* dscale, float* dbias, int64_t M, int64_t F, int64_t K,
+                                       void* workspace, int64_t workspace_bytes, void* stream) {
+    return bnn::run_backward(type, dh, ld_dh, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M, F, K, true,
+                             workspace, workspace_bytes, stream);
+}
