@@ -94,7 +94,7 @@ int join_sums(const float* part, int64_t tiles, int64_t N, float* out, hipStream
 
 // ---- the plan ----------------------------------------------------------------------------------------------------
 
-constexpr int kBackRows = 128, kStrips = 256;
+constexpr int kBackRows = 128, kStrips = 256;       // rows of the smallest tile; strips of rows without a product
 
 inline int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 
@@ -137,7 +137,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
     const int64_t channels = p.halves * cols;
     int st = BNN_OK;
     const void* g = ds;                // what dx is made of
-    int64_t ld_g = p.ds_cols, cols_g = p.ds_cols;
+    int64_t ld_g = p.ds_cols, cols_g = p.ds_cols, part_rows = p.part_rows;
     if (p.recompute && M > 0 && cols > 0) {
         ProductArgs a{};
         a.x = x; a.ld_x = ld_x; a.w = w; a.ld_w = ld_w; a.scale = scale; a.bias = bias; a.act = act;
@@ -145,7 +145,9 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.part_scale = dscale ? part_scale : nullptr;
         a.part_bias = dbias ? part_bias : nullptr;
         a.M = int(M); a.N = int(cols); a.K = int(K);
-        st = gated ? launch_product<E, kGatedBack, 2, 2, 2, 2>(a, s) : launch_product<E, kLinearBack, 2, 2, 2, 2>(a, s);
+        const int form = product_rows<E>(M, channels, ld_x);
+        part_rows = ceil_div(M, rows_of_tile(form));
+        st = gated ? launch_tiles<E, kGatedBack>(a, form, s) : launch_tiles<E, kLinearBack>(a, form, s);
     } else if (!p.recompute) {
         const bool make_ds = scale && dx;
         if (!make_ds) {
@@ -174,7 +176,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         ProductArgs a{};
         a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx;
         a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
-        if ((st = launch_product<E, kLinear, 2, 2, 2, 2>(a, s)) != BNN_OK) return st;
+        if ((st = launch_tiles<E, kLinear>(a, product_rows<E>(M, K, ld_g), s)) != BNN_OK) return st;
     }
     const bool scale_by_k = dscale && !p.recompute;
     if ((dw || scale_by_k) && cols > 0 && K > 0) {
@@ -191,10 +193,10 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         if ((st = check_launch()) != BNN_OK) return st;
     }
     if (dscale && channels > 0) {
-        const int64_t tiles = p.recompute ? p.part_rows : ceil_div(K, kGradTile);
+        const int64_t tiles = p.recompute ? part_rows : ceil_div(K, kGradTile);
         if ((st = join_sums(part_scale, tiles, channels, dscale, s)) != BNN_OK) return st;
     }
-    if (dbias && channels > 0) return join_sums(part_bias, p.part_rows, channels, dbias, s);
+    if (dbias && channels > 0) return join_sums(part_bias, part_rows, channels, dbias, s);
     return BNN_OK;
 }
 

@@ -1,7 +1,7 @@
 // The product of real rows with packed +-1 rows, s[m][n] = sum_k x[m][k] w[n][k], as tiles of the matrix engine, and what
 // its epilogues make of the sums while they are in registers.
 //
-// Each word of 32 weights becomes operands of 16-bit floats in registers (minus_weights in real_types.h), so weights move
+// Each word of 32 weights becomes operands of 16-bit floats in registers (Widening in real_types.h), so weights move
 // through memory and caches as bits and are never stored wider; the activations go through LDS, float32 ones as three
 // bfloat16 terms whose sum they are, which makes the product as exact as a float32 one.  K is taken in steps of 64: the
 // two halves of a wavefront take one word each of every weight row, and the activations' eight-element chunks in the same order.
@@ -52,17 +52,20 @@ struct ProductTile {
     static constexpr int CN = 32 * TN * FN;                       // channels: rows of w of a tile
     static constexpr int BN = kGatedForm ? CN / 2 : CN;           // columns of a tile of y
     static constexpr int kTerms = is_f32<E> ? 3 : 1;
+    // Three buffers let a wavefront run on from step to step, with the barrier in the middle; float32 rows have room for two.
+    static constexpr int kBuffers = is_f32<E> ? 2 : 3;
     static constexpr int kChunks = BM * (kStepK / 8) / kThreads;  // chunks of eight elements that a thread stages
 };
 
-template <typename E, int EPI, int TM, int TN, int FM, int FN>
+template <typename E, int EPI, int TM, int TN, int FM, int FN, bool FAR = false>
 __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const ProductArgs a) {
     using S = ProductTile<E, EPI, TM, TN, FM, FN>;
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
     constexpr bool FAST = !is_f32<E>;
     constexpr bool GATED = S::kGatedForm, BACK = EPI == kLinearBack || EPI == kGatedBack;
-    __shared__ __attribute__((aligned(16))) O8 xs[2][S::kTerms][S::BM * 8];      // rows of 8 chunks, slot = chunk ^ row % 8
+    __shared__ __attribute__((aligned(16))) O8 xs[S::kBuffers][S::kTerms][S::BM * 8];      // rows of 8 chunks, slot = chunk ^ row % 8
+    __shared__ uint4 ws[2][4][S::CN];           // 512 elements of each weight row, 16 bytes of a row at a time
     __shared__ float scale_s[S::CN], bias_s[S::CN];
     __shared__ float sums_s[BACK ? 2 * TM * S::CN : 1];
 
@@ -87,37 +90,60 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
         bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
     }
 
-    const uint32_t* wrow[FN];
+    constexpr int WQ = 4 * S::CN / S::kThreads;        // 16-byte pieces of weights that a thread stages
+    const uint32_t* wrow[WQ];
 #pragma unroll
-    for (int f = 0; f < FN; ++f) {
-        const int col = min(block_col(f) + consecutive_rows(fr), a.N - 1);          // a column that is not there: the last one
-        wrow[f] = a.w + (int64_t(block_half(f)) * a.N + col) * a.ld_w;
+    for (int i = 0; i < WQ; ++i) {
+        const int c = (i * S::kThreads + tid) % S::CN, b = c >> 5, w_ = b / FN, f = b % FN;
+        const int col = n0 + (GATED ? w_ * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : b * 32) + (c & 31);
+        wrow[i] = a.w + (int64_t(GATED && f >= FN / 2 ? a.N : 0) + min(col, a.N - 1)) * a.ld_w;
     }
+    uint4 wstage[WQ];
+    auto load_w = [&](int word0) {
+#pragma unroll
+        for (int i = 0; i < WQ; ++i) {
+            const int w0 = word0 + 4 * ((i * S::kThreads + tid) / S::CN);
+            if (w0 + 4 <= kw) wstage[i] = load_quad_any(wrow[i] + w0);
+            else wstage[i] = make_uint4(wrow[i][min(w0, kw - 1)], wrow[i][min(w0 + 1, kw - 1)], wrow[i][min(w0 + 2, kw - 1)], 0u);
+        }
+    };
+    auto store_w = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < WQ; ++i) ws[buf][(i * S::kThreads + tid) / S::CN][(i * S::kThreads + tid) % S::CN] = wstage[i];
+    };
+    auto read_w = [&](uint32_t (&w)[FN], int step) {
+        const int word = 2 * (step & 7) + fh;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(&ws[(step >> 3) & 1][word >> 2][(wn * FN) * 32 + consecutive_rows(fr)]) + (word & 3);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) w[f] = p[f * 32 * 4];
+    };
 
-    const E* xrow[S::kChunks];
-    bool row_there[S::kChunks];
+    // Activations: a uniform base that moves along K, and this thread's rows from there (rows that are not there: the last one).
+    using Offset = typename std::conditional<FAR, int64_t, uint32_t>::type;
+    const char* const xbase = static_cast<const char*>(a.x) + int64_t(m0) * a.ld_x * int64_t(sizeof(E));
+    Offset xoff[S::kChunks];
 #pragma unroll
     for (int i = 0; i < S::kChunks; ++i) {
-        const int id = i * S::kThreads + tid, m = m0 + (id >> 3);
-        row_there[i] = m < a.M;
-        xrow[i] = static_cast<const E*>(a.x) + int64_t(min(m, a.M - 1)) * a.ld_x + (id & 7) * 8;
+        const int id = i * S::kThreads + tid;
+        xoff[i] = (Offset(min(id >> 3, a.M - 1 - m0)) * Offset(a.ld_x) + Offset(id & 7) * 8) * Offset(sizeof(E));
     }
-
     typename Vec8<E>::type stage[S::kChunks];
-    uint32_t wnext[FN];
-    auto load = [&](int k0) {
+    const int whole = a.K / kStepK;                  // steps that need no checks
+    auto load = [&](int t) {
+        const char* const p = xbase + int64_t(t) * (kStepK * int64_t(sizeof(E)));
+        if (t < whole) {
 #pragma unroll
-        for (int i = 0; i < S::kChunks; ++i) {
-            const int c8 = ((i * S::kThreads + tid) & 7) * 8;
-            stage[i] = load8<E>(xrow[i] + k0, row_there[i] ? int64_t(a.K) - k0 - c8 : 0);
+            for (int i = 0; i < S::kChunks; ++i) stage[i] = *reinterpret_cast<const typename Vec8<E>::any*>(p + xoff[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::kChunks; ++i)
+                stage[i] = load8<E>(reinterpret_cast<const E*>(p + xoff[i]), a.K - t * kStepK - ((i * S::kThreads + tid) & 7) * 8);
         }
-#pragma unroll
-        for (int f = 0; f < FN; ++f) wnext[f] = wrow[f][min((k0 >> 5) + fh, kw - 1)];
     };
     auto store = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i) {
-            const int id = i * S::kThreads + tid, row = id >> 3, slot = (id & 7) ^ (row & 7);
+            const int id = i * S::kThreads + tid, row = id >> 3, slot = (id & 7) ^ ((row >> 1) & 7);
             if constexpr (is_f32<E>) {
                 O8 t[3];
 #pragma unroll
@@ -137,33 +163,81 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     };
 
     v16f_t acc[FN][FM] = {};
-    if (a.K > 0) {
+    // Operands of a quarter step: of activations straight from LDS, of weights widened from the step's words.
+    auto read_x = [&](O8 (&xf)[S::kTerms][FM], int buf, int s) {
+#pragma unroll
+        for (int p = 0; p < S::kTerms; ++p)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int row = (wm * FM + j) * 32 + fr;
+                xf[p][j] = xs[buf][p][row * 8 + ((4 * fh + s) ^ ((row >> 1) & 7))];
+            }
+    };
+    const Widening<O> minus_weights;
+    auto widen = [&](O8 (&wf)[FN], const uint32_t (&w)[FN], int s) {
+#pragma unroll
+        for (int f = 0; f < FN; ++f) wf[f] = minus_weights(s < 2 ? spread_low(w[f]) : spread_high(w[f]), s & 1);
+    };
+    const int steps = (a.K + kStepK - 1) / kStepK;
+    if (steps > 0) {
+        uint32_t w[2][FN];                  // of this step and of the next
+        O8 xf[2][S::kTerms][FM], wf[2][FN];
+        load_w(0);
         load(0);
+        store_w(0);
         store(0);
-    }
-    for (int k0 = 0, buf = 0; k0 < a.K; k0 += kStepK, buf ^= 1) {
-        uint32_t w[FN];
-#pragma unroll
-        for (int f = 0; f < FN; ++f) w[f] = wnext[f];
+        if (steps > 1) load(1);
         __syncthreads();
-        const bool more = k0 + kStepK < a.K;
-        if (more) load(k0 + kStepK);
+        read_w(w[0], 0);
+        read_x(xf[0], 0, 0);
+        widen(wf[0], w[0], 0);
+        int buf = 0;
+        for (int t = 0; t < steps; ++t) {
+            const int next = buf == S::kBuffers - 1 ? 0 : buf + 1;
+            const bool more = t + 1 < steps;
+            if constexpr (S::kBuffers == 3) {
+                // Buffer `next` held step t - 2, which every wavefront has left behind since the barrier in step t - 1.
+                if (more) store(next);
+            }
+            if (S::kBuffers == 3 ? t + 2 < steps : t > 0 && more) load(S::kBuffers == 3 ? t + 2 : t + 1);
+            // The weights of the next 512 elements: the buffer that they take was last read in the step before the last.
+            if ((t & 7) == 1 && t + 7 < steps) load_w((t + 7) * 2);
+            if ((t & 7) == 5 && t + 3 < steps) store_w(((t + 3) >> 3) & 1);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            O8 wf[FN];
-#pragma unroll
-            for (int f = 0; f < FN; ++f) wf[f] = minus_weights<O>(s < 2 ? spread_low(w[f]) : spread_high(w[f]), s & 1);
-#pragma unroll
-            for (int p = 0; p < S::kTerms; ++p)
-#pragma unroll
-                for (int j = 0; j < FM; ++j) {
-                    const int row = (wm * FM + j) * 32 + fr;
-                    const O8 xf = xs[buf][p][row * 8 + ((4 * fh + s) ^ (row & 7))];
-#pragma unroll
-                    for (int f = 0; f < FN; ++f) acc[f][j] = mfma16(wf[f], xf, acc[f][j]);
+            for (int s = 0; s < 4; ++s) {
+                if (S::kBuffers == 3 && s == 2) {
+                    __syncthreads();
+                    read_w(w[1], t + 1);
                 }
+                if (s < 3) {
+                    read_x(xf[(s + 1) & 1], buf, s + 1);
+                    widen(wf[(s + 1) & 1], w[0], s + 1);
+                } else if (S::kBuffers == 3) {
+                    read_x(xf[0], next, 0);             // after the last step: read, not used
+                    widen(wf[0], w[1], 0);
+                }
+#pragma unroll
+                for (int p = 0; p < S::kTerms; ++p)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j)
+#pragma unroll
+                        for (int f = 0; f < FN; ++f) acc[f][j] = mfma16(wf[s & 1][f], xf[s & 1][p][j], acc[f][j]);
+                // Keeps the quarters apart: moved over their borders, reads lie in wait longer than they take.
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (S::kBuffers == 3) {
+#pragma unroll
+                for (int f = 0; f < FN; ++f) w[0][f] = w[1][f];
+            } else if (more) {
+                // Two buffers: `next` held step t - 1, which everyone had left before the barrier at this step's start.
+                store(next);
+                __syncthreads();
+                read_w(w[0], t + 1);
+                read_x(xf[0], next, 0);
+                widen(wf[0], w[0], 0);
+            }
+            buf = next;
         }
-        if (more) store(buf ^ 1);
     }
     __syncthreads();
 

@@ -28,6 +28,7 @@ __global__ __launch_bounds__(1024) void bits_rows_kernel(const ProductArgs a) {
     for (int f = 0; f < FN; ++f) wrow[f] = a.w + (int64_t(f) * a.N + col) * a.ld_w;
     const E* const xrow = static_cast<const E*>(a.x) + int64_t(min(fr, a.M - 1)) * a.ld_x;
 
+    const Widening<O> minus_weights;
     v16f_t acc[FN] = {};
     for (int64_t k0 = int64_t(wave) * 128; k0 < a.K; k0 += int64_t(waves) * 128) {
         const int kl = int(k0) + 64 * fh, word = kl >> 5;
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(1024) void bits_rows_kernel(const ProductArgs a) {
 #pragma unroll
             for (int f = 0; f < FN; ++f) {
                 const uint32_t word_s = w[f][s >> 2];
-                const O8 wf = minus_weights<O>((s & 2) ? spread_high(word_s) : spread_low(word_s), s & 1);
+                const O8 wf = minus_weights((s & 2) ? spread_high(word_s) : spread_low(word_s), s & 1);
 #pragma unroll
                 for (int p = 0; p < TERMS; ++p) acc[f] = mfma16(wf, t[p], acc[f]);
             }
@@ -111,7 +112,7 @@ int launch_rows(const ProductArgs& a, hipStream_t s) {
 template <typename E, int EPI>
 int launch_forward(const ProductArgs& a, hipStream_t s) {
     if (a.M <= 32) return launch_rows<E, EPI>(a, s);
-    return launch_product<E, EPI, 2, 2, 2, 2>(a, s);
+    return launch_tiles<E, EPI>(a, product_rows<E>(a.M, int64_t(a.N) * (EPI == kGated ? 2 : 1), a.ld_x), s);
 }
 
 }  // namespace

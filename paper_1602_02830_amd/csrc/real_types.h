@@ -150,13 +150,18 @@ __device__ inline void activate_both(int act, float z, float& f, float& df) {
 template <typename O>
 inline constexpr uint32_t kOnes = std::is_same<O, bf16_t>::value ? 0x3F803F80u : 0x3C003C00u;
 
+// The two constants in registers: with both in sight the compiler makes two operations with literals of the one.
 template <typename O>
-__device__ inline typename Vec8<O>::type minus_weights(uint32_t y, int s) {       // 8 elements from 8 * s on, s = 0 or 1
-    v4u_t d;
+struct Widening {
+    uint32_t signs = 0x80008000u, ones = kOnes<O>;
+    __device__ inline Widening() { asm("" : "+s"(signs), "+v"(ones)); }
+    __device__ inline typename Vec8<O>::type operator()(uint32_t y, int s) const {       // elements from 8 * s on, s = 0 or 1
+        v4u_t d;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) d[j] = ((y << (15 - 8 * s - 2 * j)) & 0x80008000u) | kOnes<O>;
-    return __builtin_bit_cast(typename Vec8<O>::type, d);
-}
+        for (int j = 0; j < 4; ++j) d[j] = ((y << (15 - 8 * s - 2 * j)) & signs) | ones;
+        return __builtin_bit_cast(typename Vec8<O>::type, d);
+    }
+};
 
 __device__ inline uint32_t spread_low(uint32_t w) {
     const uint32_t b = w & 0xFFFFu;
