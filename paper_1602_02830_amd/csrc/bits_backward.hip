@@ -87,32 +87,51 @@ __global__ __launch_bounds__(256) void join_sums_kernel(const float* part, int t
     if (r == 0 && n < N) out[n] = (sums_s[0][c] + sums_s[1][c]) + (sums_s[2][c] + sums_s[3][c]);
 }
 
-int join_sums(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
-    join_sums_kernel<<<dim3(uint32_t(ceil_div(N, 64))), dim3(256), 0, s>>>(part, int(tiles), int(N), out);
-    return check_launch();
-}
-
 // ---- the plan ----------------------------------------------------------------------------------------------------
 
-constexpr int kBackRows = 128, kStrips = 256;       // rows of the smallest tile; strips of rows without a product
+constexpr int kStrips = 256;       // strips of rows for the column sums without a product
 
 inline int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
+
+// How dw is made: tiles of 256, 128 or 64 rows and columns, and over how many parts of the rows.  Tiles of 256 are the
+// fastest where they fill the chip (4096 x 4096 x 4096: 126 us, tiles of 128 169; with half as many of them 126 and 85), those of 64 where
+// those of 128 do not (1000 x 1024 x 1024: 11.0 us against 14.2).  Where even they are few, rows are split and the parts joined:
+// a product of 16384 rows and 512 x 512 would be 64 tiles of 512 steps, 190 us.
+struct GradPlan {
+    int tile, splits, split_rows;
+    bool general;
+    GradPlan(bool f32, int64_t M, int64_t cols, int64_t K) {
+        auto tiles = [&](int64_t t) { return ceil_div(cols, t) * ceil_div(K, t); };
+        general = cols < 8 || K < 8;
+        tile = general ? 64 : !f32 && tiles(256) >= 192 ? 256 : tiles(128) >= 256 ? 128 : 64;
+        const int64_t most = M / (8 * kGradStep), wanted = tiles(tile) > 0 ? 512 / tiles(tile) : 1;
+        const int64_t parts = wanted < most ? wanted : most;
+        split_rows = int(round_up(ceil_div(M, parts > 1 ? parts : 1), kGradStep));
+        splits = int(parts > 1 ? ceil_div(M, split_rows) : 1);
+        if (splits == 1) split_rows = int(M);
+    }
+};
 
 // Everything a call puts into its workspace, by sizes alone.  cols: columns of dy (gated: F).
 struct Plan {
     int64_t half, halves, ds_cols, wt_ld, strip, part_rows;
-    int64_t ds_at, wt_at, scale_at, bias_at, bytes;
+    int64_t ds_at, wt_at, scale_at, bias_at, pieces_at, bytes;
+    Form form;
     bool recompute;
-    Plan(int64_t size, int64_t M, int64_t cols, int64_t K, int act, bool gated) {
-        recompute = gated || act != BNN_ACT_NONE;
+    GradPlan grad;
+    Plan(int64_t size, int64_t M, int64_t cols, int64_t K, int act, bool gated)
+        : recompute(gated || act != BNN_ACT_NONE), grad(size == 4, M, recompute ? round_up(cols, 64) * (gated ? 2 : 1) : cols, K) {
         halves = gated ? 2 : 1;
         half = round_up(cols, 64);
         ds_cols = half * halves;
         wt_ld = round_up(ds_cols / 32, 4);
-        strip = recompute ? kBackRows : round_up(ceil_div(M > 0 ? M : 1, kStrips), 4);
-        part_rows = ceil_div(M, strip);
         const int64_t channels = halves * cols;
-        const int64_t scale_rows = recompute ? part_rows : ceil_div(K, kGradTile);
+        form = product_form(size == 4, false, M, channels);
+        strip = round_up(ceil_div(M > 0 ? M : 1, kStrips), 4);
+        // Tiles of a form with 64-bit offsets have 128 rows: never more of them than of the smaller of the two.
+        const int64_t rows = rows_of_form(form);
+        part_rows = ceil_div(M, recompute ? (rows < 128 ? rows : 128) : strip);
+        const int64_t scale_rows = recompute ? part_rows : ceil_div(K, 64);
         auto take = [&](int64_t b) {
             const int64_t at = bytes;
             bytes += round_up(b, 256);
@@ -123,8 +142,44 @@ struct Plan {
         wt_at = take(K * wt_ld * 4);
         scale_at = take(scale_rows * channels * 4);
         bias_at = take(part_rows * channels * 4);
+        pieces_at = take(grad.splits > 1 ? grad.splits * channels * K * 4 : 0);
     }
 };
+
+template <typename E, int TK, int TN, int FK, int FN, bool GENERAL = false>
+int launch_grad(WeightGradArgs a, hipStream_t s) {
+    using S = GradTile<E, TK, TN, FK, FN>;
+    const int64_t tiles_n = ceil_div(a.cols, S::BN), tiles_k = ceil_div(a.K, S::BK);
+    if (tiles_n * tiles_k * a.splits > max_blocks(S::kThreads)) return BNN_ERR_UNSUPPORTED;
+    a.map = tile_map(tiles_n, tiles_k);
+    weight_grad_kernel<E, TK, TN, FK, FN, GENERAL><<<dim3(uint32_t(tiles_n * tiles_k * a.splits)), dim3(S::kThreads), 0, s>>>(a);
+    return check_launch();
+}
+
+int join_sums(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
+    join_sums_kernel<<<dim3(uint32_t(ceil_div(N, 64))), dim3(256), 0, s>>>(part, int(tiles), int(N), out);
+    return check_launch();
+}
+
+// dw and, where a.w is given, dscale; part: room for the column sums of the tiles.
+template <typename E>
+int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* part, float* dscale, hipStream_t s) {
+    a.splits = g.splits;
+    a.split_rows = g.split_rows;
+    a.pieces = g.splits > 1 ? pieces : nullptr;
+    a.part = part;
+    int st;
+    if (g.general) st = launch_grad<E, 2, 2, 1, 1, true>(a, s);
+    else if (g.tile == 64) st = launch_grad<E, 2, 2, 1, 1>(a, s);
+    else if (is_f32<E> || g.tile == 128) st = launch_grad<E, 2, 4, 2, 1>(a, s);
+    else if constexpr (!is_f32<E>) st = launch_grad<E, 4, 2, 2, 4>(a, s);
+    if (st != BNN_OK) return st;
+    if (g.splits > 1) {
+        join_pieces_kernel<E><<<dim3(uint32_t(a.channels)), dim3(256), 0, s>>>(a, dscale);
+        return check_launch();
+    }
+    return a.w ? join_sums(part, ceil_div(a.K, g.tile), a.channels, dscale, s) : BNN_OK;
+}
 
 template <typename E>
 int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w, int64_t ld_w,
@@ -145,9 +200,8 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.part_scale = dscale ? part_scale : nullptr;
         a.part_bias = dbias ? part_bias : nullptr;
         a.M = int(M); a.N = int(cols); a.K = int(K);
-        const int form = product_rows<E>(M, channels, ld_x);
-        part_rows = ceil_div(M, rows_of_tile(form));
-        st = gated ? launch_tiles<E, kGatedBack>(a, form, s) : launch_tiles<E, kLinearBack>(a, form, s);
+        part_rows = ceil_div(M, rows_of_tile<E>(p.form, ld_x));
+        st = gated ? launch_form<E, kGatedBack>(a, p.form, s) : launch_form<E, kLinearBack>(a, p.form, s);
     } else if (!p.recompute) {
         const bool make_ds = scale && dx;
         if (!make_ds) {
@@ -176,7 +230,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         ProductArgs a{};
         a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx;
         a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
-        if ((st = launch_tiles<E, kLinear>(a, product_rows<E>(M, K, ld_g), s)) != BNN_OK) return st;
+        if ((st = launch_form<E, kLinear>(a, product_form(is_f32<E>, true, M, K), s)) != BNN_OK) return st;
     }
     const bool scale_by_k = dscale && !p.recompute;
     if ((dw || scale_by_k) && cols > 0 && K > 0) {
@@ -184,17 +238,13 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.g = p.recompute ? ds : dy; a.ld_g = p.recompute ? p.ds_cols : ld_dy;
         a.x = x; a.ld_x = ld_x; a.dw = dw; a.ld_dw = ld_dw;
         a.row_scale = p.recompute ? nullptr : scale;
-        a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w; a.part = part_scale;
+        a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w;
         a.M = int(M); a.K = int(K); a.cols = int(p.recompute ? p.ds_cols : cols); a.half = int(p.half); a.F = int(cols);
-        const int64_t tiles_n = ceil_div(a.cols, kGradTile), tiles_k = ceil_div(K, kGradTile);
-        if (tiles_n * tiles_k > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
-        a.map = tile_map(tiles_n, tiles_k);
-        weight_grad_kernel<E><<<dim3(uint32_t(tiles_n * tiles_k)), dim3(256), 0, s>>>(a);
-        if ((st = check_launch()) != BNN_OK) return st;
+        a.channels = int(channels);
+        if ((st = weight_gradient<E>(p.grad, a, reinterpret_cast<float*>(ws + p.pieces_at), part_scale, dscale, s)) != BNN_OK) return st;
     }
-    if (dscale && channels > 0) {
-        const int64_t tiles = p.recompute ? part_rows : ceil_div(K, kGradTile);
-        if ((st = join_sums(part_scale, tiles, channels, dscale, s)) != BNN_OK) return st;
+    if (dscale && channels > 0 && (p.recompute || K == 0)) {
+        if ((st = join_sums(part_scale, p.recompute ? part_rows : 0, channels, dscale, s)) != BNN_OK) return st;
     }
     if (dbias && channels > 0) return join_sums(part_bias, part_rows, channels, dbias, s);
     return BNN_OK;

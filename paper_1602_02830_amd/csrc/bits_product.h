@@ -43,6 +43,70 @@ enum Epilogue {
 
 constexpr int kStepK = 64;          // elements of K a step
 
+template <int EPI>
+inline constexpr int kHalves = EPI == kGated || EPI == kGatedBack ? 2 : 1;
+template <int EPI>
+inline constexpr bool kBackward = EPI == kLinearBack || EPI == kGatedBack;
+
+// The epilogue of W = 8 (or 4) consecutive columns from n on of row m, from their sums (gated: of both halves).  scale, bias: of
+// the columns of each half.  Backwards, sum_s and sum_z grow by dz * s and dz.
+template <typename E, int EPI, int W>
+__device__ inline void finish(const ProductArgs& a, int m, int n, const float (&s)[kHalves<EPI>][W], const float* const (&scale)[kHalves<EPI>],
+                              const float* const (&bias)[kHalves<EPI>], float (&sum_s)[kHalves<EPI>][W], float (&sum_z)[kHalves<EPI>][W]) {
+    constexpr bool FAST = !is_f32<E>;
+    constexpr int HALVES = kHalves<EPI>;
+    E* const y = static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n;
+    const int64_t valid = int64_t(a.N) - n;
+    if (m >= a.M) return;
+    if constexpr (EPI == kLinear) {
+        if (valid <= 0) return;
+        float r[W] = {}, v[W];
+        if (a.residual) load_some<E, W>(static_cast<const E*>(a.residual) + int64_t(m) * a.ld_r + n, valid, r);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = activate<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i])) + r[i];
+        store_some<E, W>(y, v, valid);
+    } else if constexpr (EPI == kGated) {
+        if (valid <= 0) return;
+        float v[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            v[i] = activate<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i])) * fmaf(s[1][i], scale[1][i], bias[1][i]);
+        store_some<E, W>(y, v, valid);
+    } else {
+        if (n >= a.half) return;
+        float d[W], out[HALVES][W];
+        load_some<E, W>(static_cast<const E*>(a.dy) + int64_t(m) * a.ld_dy + n, valid, d);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            float f, slope, dz[HALVES];
+            activate_both<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i]), f, slope);
+            if constexpr (HALVES == 2) {
+                dz[0] = d[i] * fmaf(s[1][i], scale[1][i], bias[1][i]) * slope;
+                dz[1] = d[i] * f;
+            } else {
+                dz[0] = d[i] * slope;
+            }
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+                // A column that is not there counts nothing, whatever its sums are.
+                out[h][i] = i < valid ? dz[h] * scale[h][i] : 0.0f;
+                sum_s[h][i] += i < valid ? dz[h] * s[h][i] : 0.0f;
+                sum_z[h][i] += i < valid ? dz[h] : 0.0f;
+            }
+        }
+        // Columns from N up to `half` are written as zeros.
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) store_some<E, W>(y + int64_t(h) * a.half, out[h], W);
+    }
+}
+
+// Over the 32 rows of a block's lanes: what lane 0 of each half has afterwards is their sum.
+__device__ inline float sum_rows(float v) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
 // TN wavefronts along the channels, TM along the rows, 32-row blocks FN x FM for each.
 template <typename E, int EPI, int TM, int TN, int FM, int FN>
 struct ProductTile {
@@ -53,7 +117,7 @@ struct ProductTile {
     static constexpr int BN = kGatedForm ? CN / 2 : CN;           // columns of a tile of y
     static constexpr int kTerms = is_f32<E> ? 3 : 1;
     // Three buffers let a wavefront run on from step to step, with the barrier in the middle; float32 rows have room for two.
-    static constexpr int kBuffers = is_f32<E> ? 2 : 3;
+    static constexpr int kBuffers = is_f32<E> && BM > 64 ? 2 : 3;
     static constexpr int kChunks = BM * (kStepK / 8) / kThreads;  // chunks of eight elements that a thread stages
 };
 
@@ -62,8 +126,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     using S = ProductTile<E, EPI, TM, TN, FM, FN>;
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
-    constexpr bool FAST = !is_f32<E>;
-    constexpr bool GATED = S::kGatedForm, BACK = EPI == kLinearBack || EPI == kGatedBack;
+    constexpr bool GATED = S::kGatedForm, BACK = kBackward<EPI>;
     __shared__ __attribute__((aligned(16))) O8 xs[S::kBuffers][S::kTerms][S::BM * 8];      // rows of 8 chunks, slot = chunk ^ row % 8
     __shared__ uint4 ws[2][4][S::CN];           // 512 elements of each weight row, 16 bytes of a row at a time
     __shared__ float scale_s[S::CN], bias_s[S::CN];
@@ -144,21 +207,10 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
 #pragma unroll
         for (int i = 0; i < S::kChunks; ++i) {
             const int id = i * S::kThreads + tid, row = id >> 3, slot = (id & 7) ^ ((row >> 1) & 7);
-            if constexpr (is_f32<E>) {
-                O8 t[3];
+            O8 t[S::kTerms];
+            terms_of<E>(stage[i], t);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    bf16_t part[3];
-                    split3(stage[i][e], part);
-                    t[0][e] = part[0];
-                    t[1][e] = part[1];
-                    t[2][e] = part[2];
-                }
-#pragma unroll
-                for (int p = 0; p < 3; ++p) xs[buf][p][row * 8 + slot] = t[p];
-            } else {
-                xs[buf][0][row * 8 + slot] = stage[i];
-            }
+            for (int p = 0; p < S::kTerms; ++p) xs[buf][p][row * 8 + slot] = t[p];
         }
     };
 
@@ -198,8 +250,8 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
             if constexpr (S::kBuffers == 3) {
                 // Buffer `next` held step t - 2, which every wavefront has left behind since the barrier in step t - 1.
                 if (more) store(next);
+                if (t + 2 < steps) load(t + 2);
             }
-            if (S::kBuffers == 3 ? t + 2 < steps : t > 0 && more) load(S::kBuffers == 3 ? t + 2 : t + 1);
             // The weights of the next 512 elements: the buffer that they take was last read in the step before the last.
             if ((t & 7) == 1 && t + 7 < steps) load_w((t + 7) * 2);
             if ((t & 7) == 5 && t + 3 < steps) store_w(((t + 3) >> 3) & 1);
@@ -231,6 +283,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
             } else if (more) {
                 // Two buffers: `next` held step t - 1, which everyone had left before the barrier at this step's start.
                 store(next);
+                if (t + 2 < steps) load(t + 2);
                 __syncthreads();
                 read_w(w[0], t + 1);
                 read_x(xf[0], next, 0);
@@ -242,114 +295,42 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     __syncthreads();
 
     // ---- epilogue: lane l has columns 16 fh .. 16 fh + 15 of row fr of each block ----
-    E* const y = static_cast<E*>(a.y);
-    if constexpr (EPI == kLinear) {
-        const E* const residual = static_cast<const E*>(a.residual);
+    constexpr int HALVES = kHalves<EPI>, FY = FN / HALVES;
 #pragma unroll
-        for (int f = 0; f < FN; ++f) {
-            const int c0 = (wn * FN + f) * 32 + 16 * fh, n = block_col(f) + 16 * fh;
+    for (int f = 0; f < FY; ++f)
 #pragma unroll
-            for (int j = 0; j < FM; ++j) {
-                const int m = m0 + (wm * FM + j) * 32 + fr;
-                if (m >= a.M || n >= a.N) continue;
+        for (int g = 0; g < 2; ++g) {
+            const int c0 = (wn * FN + f) * 32 + 16 * fh + 8 * g;          // its channel; the other half's is 16 FN further
+            const float *scale[HALVES], *bias[HALVES];
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int64_t valid = int64_t(a.N) - n - 8 * g;
-                    typename Vec8<E>::type r = {};
-                    if (residual) r = load8<E>(residual + int64_t(m) * a.ld_r + n + 8 * g, valid);
-                    float v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        v[i] = activate<FAST>(a.act, fmaf(-acc[f][j][8 * g + i], scale_s[c0 + 8 * g + i], bias_s[c0 + 8 * g + i])) + float(r[i]);
-                    store8<E>(y + int64_t(m) * a.ld_y + n + 8 * g, v, valid);
-                }
+            for (int h = 0; h < HALVES; ++h) {
+                scale[h] = scale_s + c0 + 16 * FN * h;
+                bias[h] = bias_s + c0 + 16 * FN * h;
             }
-        }
-    } else if constexpr (EPI == kGated) {
-#pragma unroll
-        for (int f = 0; f < FN / 2; ++f) {
-            const int cg = (wn * FN + f) * 32 + 16 * fh, cu = cg + 16 * FN, n = block_col(f) + 16 * fh;
+            float sum_s[HALVES][8] = {}, sum_z[HALVES][8] = {};
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                const int m = m0 + (wm * FM + j) * 32 + fr;
-                if (m >= a.M || n >= a.N) continue;
+                float sums[HALVES][8];
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    float v[8];
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sums[h][i] = -acc[f + FY * h][j][8 * g + i];
+                finish<E, EPI, 8>(a, m0 + (wm * FM + j) * 32 + fr, block_col(f) + 16 * fh + 8 * g, sums, scale, bias, sum_s, sum_z);
+            }
+            if constexpr (BACK) {
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int e = 8 * g + i;
-                        const float zg = fmaf(-acc[f][j][e], scale_s[cg + e], bias_s[cg + e]);
-                        const float zu = fmaf(-acc[f + FN / 2][j][e], scale_s[cu + e], bias_s[cu + e]);
-                        v[i] = activate<FAST>(a.act, zg) * zu;
-                    }
-                    store8<E>(y + int64_t(m) * a.ld_y + n + 8 * g, v, int64_t(a.N) - n - 8 * g);
-                }
-            }
-        }
-    } else {
-        const E* const dy = static_cast<const E*>(a.dy);
-        constexpr int HALVES = GATED ? 2 : 1, FY = FN / HALVES;
-#pragma unroll
-        for (int f = 0; f < FY; ++f) {
-            const int c0 = (wn * FN + f) * 32 + 16 * fh, n = block_col(f) + 16 * fh;
-            float sum_s[HALVES][16] = {}, sum_z[HALVES][16] = {};
-#pragma unroll
-            for (int j = 0; j < FM; ++j) {
-                const int m = m0 + (wm * FM + j) * 32 + fr;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int64_t valid = m < a.M ? int64_t(a.N) - n - 8 * g : 0;
-                    const auto d = load8<E>(dy + int64_t(min(m, a.M - 1)) * a.ld_dy + n + 8 * g, valid);
-                    float out[HALVES][8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int e = 8 * g + i;
-                        const float s0 = -acc[f][j][e], z0 = fmaf(s0, scale_s[c0 + e], bias_s[c0 + e]);
-                        float act, slope, dz[HALVES], s[HALVES];
-                        activate_both<FAST>(a.act, z0, act, slope);
-                        s[0] = s0;
-                        if constexpr (GATED) {
-                            const int cu = c0 + 16 * FN + e;
-                            s[1] = -acc[f + FN / 2][j][e];
-                            dz[0] = float(d[i]) * fmaf(s[1], scale_s[cu], bias_s[cu]) * slope;
-                            dz[1] = float(d[i]) * act;
-                        } else {
-                            dz[0] = float(d[i]) * slope;
-                        }
-#pragma unroll
-                        for (int h = 0; h < HALVES; ++h) {
-                            // What is not there counts nothing, whatever its sums are.
-                            dz[h] = i < valid ? dz[h] : 0.0f;
-                            out[h][i] = i < valid ? dz[h] * scale_s[c0 + 16 * FN * h + e] : 0.0f;
-                            sum_s[h][e] += i < valid ? dz[h] * s[h] : 0.0f;
-                            sum_z[h][e] += dz[h];
+                        const float p = sum_rows(sum_s[h][i]), q = sum_rows(sum_z[h][i]);
+                        if (fr == 0) {
+                            sums_s[(wm * 2) * S::CN + c0 + 16 * FN * h + i] = p;
+                            sums_s[(wm * 2 + 1) * S::CN + c0 + 16 * FN * h + i] = q;
                         }
                     }
-                    if (m < a.M && n < a.half)         // columns from N up to `half` are written as zeros
-#pragma unroll
-                        for (int h = 0; h < HALVES; ++h)
-                            store8<E>(y + int64_t(m) * a.ld_y + int64_t(h) * a.half + n + 8 * g, out[h], 8);
-                }
             }
-            // Over the 32 rows of the lanes of each half, then over the wavefronts of the same columns.
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float p = sum_s[h][e], q = sum_z[h][e];
-#pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) {
-                        p += __shfl_xor(p, off);
-                        q += __shfl_xor(q, off);
-                    }
-                    if (fr == 0) {
-                        const int c = c0 + 16 * FN * h + e;
-                        sums_s[(wm * 2) * S::CN + c] = p;
-                        sums_s[(wm * 2 + 1) * S::CN + c] = q;
-                    }
-                }
         }
+    if constexpr (BACK) {
         __syncthreads();
         for (int c = tid; c < S::CN; c += S::kThreads) {
             const int b = c >> 5, w_ = b / FN, f = b % FN;

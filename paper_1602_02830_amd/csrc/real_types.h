@@ -40,18 +40,37 @@ inline bool with_type(int type, F&& f) {
 inline int64_t type_bytes(int type) { return type == BNN_F32 ? 4 : type == BNN_BF16 || type == BNN_F16 ? 2 : 0; }
 
 // Eight elements from p on, of which the first `valid` exist; zero for the others, which are not read.  p is aligned to
-// its element: a whole group is one or two 16-byte loads, which need no more than that.
+// its element: a whole group is one or two 16-byte loads, which need no more than that.  The elements of a part of a group are
+// loaded all at once (the last one again for those that are not there): one by one, each would wait for the one before.
 template <typename E>
 __device__ inline typename Vec8<E>::type load8(const E* p, int64_t valid) {
     typename Vec8<E>::type v = {};
     if (valid >= 8) {
         v = *reinterpret_cast<const typename Vec8<E>::any*>(p);
-    } else {
+    } else if (valid > 0) {
+        const int last = int(valid) - 1;
+        E e[7];
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < valid) v[i] = p[i];
+        for (int i = 0; i < 7; ++i) e[i] = p[min(i, last)];
+#pragma unroll
+        for (int i = 0; i < 7; ++i) v[i] = i <= last ? e[i] : E(0.0f);
     }
     return v;
+}
+
+// What is left of a row from a group's first element on, `left` elements: the group as it is for 8 or more, and for fewer the
+// last ones of v - the row's last eight elements, loaded in the group's place - moved down, with zeros after them.
+template <typename E>
+__device__ inline typename Vec8<E>::type row_end(typename Vec8<E>::type v, int left) {
+    const int by = 8 - left;
+#pragma unroll
+    for (int step = 4; step > 0; step >>= 1) {
+        typename Vec8<E>::type moved = v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) moved[i] = i + step < 8 ? v[i + step] : E(0.0f);
+        if (by > 0 && (by & step)) v = moved;
+    }
+    return left > 0 ? v : typename Vec8<E>::type{};
 }
 
 template <typename E>
@@ -65,6 +84,32 @@ __device__ inline void store8(E* p, const float (&v)[8], int64_t valid) {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
             if (i < valid) p[i] = o[i];
+    }
+}
+
+// The same with W of the eight, as plain floats.
+template <typename E, int W>
+__device__ inline void load_some(const E* p, int64_t valid, float (&v)[W]) {
+    typename Vec8<E>::type q = {};
+    if constexpr (W == 8) {
+        q = load8<E>(p, valid);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < valid) q[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = float(q[i]);
+}
+
+template <typename E, int W>
+__device__ inline void store_some(E* p, const float (&v)[W], int64_t valid) {
+    if constexpr (W == 8) {
+        store8<E>(p, v, valid);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < valid) p[i] = E(v[i]);
     }
 }
 
@@ -173,6 +218,12 @@ __device__ inline uint32_t spread_high(uint32_t w) {
     return b | (b << 15);
 }
 
+// One byte of a word: 8 elements.
+__device__ inline uint32_t spread_byte(uint32_t w, int byte) {
+    const uint32_t b = __builtin_amdgcn_ubfe(w, 8 * byte, 8);
+    return b | (b << 15);
+}
+
 __device__ inline v16f_t mfma16(Vec8<bf16_t>::type a, Vec8<bf16_t>::type b, v16f_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -181,17 +232,54 @@ __device__ inline v16f_t mfma16(Vec8<f16_t>::type a, Vec8<f16_t>::type b, v16f_t
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// v = t[0] + t[1] + t[2] exactly, each a bfloat16 (8 significant bits; a float32 has 24).  Each term is what is left cut off
-// after 8 bits: all have the sign of v, so no sum of some of them is larger than v and overflows where v does not.  An
-// infinity or a NaN stays in the first term alone.
+typedef float v4f_t __attribute__((ext_vector_type(4)));
+
+__device__ inline v4f_t mfma32(Vec8<bf16_t>::type a, Vec8<bf16_t>::type b, v4f_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ inline v4f_t mfma32(Vec8<f16_t>::type a, Vec8<f16_t>::type b, v4f_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 __device__ inline float cut_off(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
 
-__device__ inline void split3(float v, bf16_t (&t)[3]) {
-    const bool finite = __builtin_fabsf(v) < __builtin_inff();
-    const float top = cut_off(v), r1 = finite ? v - top : 0.0f, middle = cut_off(r1);
-    t[0] = bf16_t(finite ? top : v);
-    t[1] = bf16_t(middle);
-    t[2] = bf16_t(r1 - middle);
+// The upper halves of two words, the first one's below.
+__device__ inline uint32_t upper_halves(float lo, float hi) {
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+
+// Eight activations as operands: one term of a 16-bit type, three of float32.
+template <typename E>
+inline constexpr int kTermsOf = is_f32<E> ? 3 : 1;
+
+// A float32 is the sum of three bfloat16 exactly (24 significant bits, 8 each).  Each term is what is left cut off after 8
+// bits: all have the sign of the value, so no sum of some of them is larger than it and overflows where it does not.  An infinity
+// stays in the first term alone, and so does a NaN (whose upper half is kept from being an infinity's).
+template <typename E>
+__device__ inline void terms_of(const typename Vec8<E>::type& v, typename Vec8<Operand<E>>::type (&t)[kTermsOf<E>]) {
+    if constexpr (is_f32<E>) {
+        v4u_t d[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float top[2], rest[2], middle[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x = v[2 * i + e];
+                top[e] = cut_off(x);
+                rest[e] = __builtin_fabsf(x) < __builtin_inff() ? x - top[e] : 0.0f;
+                top[e] = x != x ? x + x : top[e];
+                middle[e] = cut_off(rest[e]);
+            }
+            d[0][i] = upper_halves(top[0], top[1]);
+            d[1][i] = upper_halves(middle[0], middle[1]);
+            d[2][i] = upper_halves(rest[0] - middle[0], rest[1] - middle[1]);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) t[p] = __builtin_bit_cast(typename Vec8<Operand<E>>::type, d[p]);
+    } else {
+        t[0] = v;
+    }
 }
 
 // Row of a 32-row operand block that lane a of the first operand loads, so that accumulator register i of lane half h is

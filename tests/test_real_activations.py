@@ -145,6 +145,39 @@ def test_linear(M, N, K, T):
     close(got, *linear_want(p, "silu"), "linear silu")
 
 
+# Sizes whose tiles fill the chip in each of the tiled forms (64, 128 and 256 rows), with partial tiles, steps and words.
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1000, 4090, 100), (2040, 4090, 70), (4090, 4090, 65), (4000, 4096, 640), (300, 20000, 7)])
+def test_linear_large_tiles(M, N, K, T):
+    T = TYPES[T]
+    p = Product(M, N, K, T, seed=2, gap=1 if K == 65 else 0)
+    r = torch.randn(M, N, generator=torch.Generator().manual_seed(1)).to(T)
+    close(bnn.linear_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_NONE, r.to(DEV)), *linear_want(p, "none", r), "large")
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M,F,K", [(1000, 2045, 100), (2040, 2045, 70), (4090, 2045, 65)])
+def test_gated_large_tiles(M, F, K, T):
+    p = Product(M, 2 * F, K, TYPES[T], seed=2)
+    close(bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU), *gated_want(p, "silu"), "large")
+
+
+@gpu
+@pytest.mark.parametrize("M", [5, 40, 130])
+def test_rows_far_apart(M):
+    """Rows more than 2^23 elements apart: a tile's offsets need 64 bits."""
+    K, N, ld = 70, 20480, 2 ** 23 + 9
+    p = Product(M, N, K, torch.bfloat16)
+    far = torch.empty((M - 1) * ld + K, dtype=torch.bfloat16, device=DEV).as_strided((M, K), (ld, 1))
+    far.copy_(p.x)
+    close(bnn.linear_bits(far, p.wd, p.scaled, p.biased), *linear_want(p, "none"), "far")
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).bfloat16()
+    got = bnn.linear_bits_backward(dy.to(DEV), far, p.wd, p.scaled, p.biased, bnn.ACT_SILU)
+    check_backward(p, "silu", False, dy, got)
+
+
 @gpu
 @pytest.mark.parametrize("T", TYPES)
 @pytest.mark.parametrize("act", ACTS)
@@ -266,6 +299,30 @@ def test_gated_backward(M, F, K, act, T):
     p = Product(M, 2 * F, K, T, seed=9)
     dh = torch.randn(M, F, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
     check_backward(p, act, True, dh, bnn.gated_bits_backward(dh.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act]))
+
+
+# Tiles of 64, 128 and 256 rows with their column sums, and the weights' gradient in tiles of 64 (whole and in parts of the rows),
+# 128 and 256.
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("M,N,K", [(1000, 4090, 100), (2040, 4090, 70), (4090, 4090, 65), (70, 4090, 3100), (40, 2100, 2000), (4000, 100, 90),
+                                   (1500, 3, 5), (70, 5, 300), (70, 300, 5)])
+def test_linear_backward_large_tiles(M, N, K, act, T):
+    T = TYPES[T]
+    p = Product(M, N, K, T, seed=7)
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+    check_backward(p, act, False, dy, bnn.linear_bits_backward(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act]))
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M,F,K", [(1000, 2045, 100), (2040, 2045, 70), (4090, 2045, 65), (70, 2045, 3100), (3000, 50, 90)])
+def test_gated_backward_large_tiles(M, F, K, T):
+    T = TYPES[T]
+    p = Product(M, 2 * F, K, T, seed=9)
+    dh = torch.randn(M, F, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+    check_backward(p, "silu", True, dh, bnn.gated_bits_backward(dh.to(DEV), p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU))
 
 
 @gpu
