@@ -9,6 +9,7 @@
 //   4. column sums of the tiles joined, in a fixed order.
 #include "bit_transpose.h"
 #include "bits_launch.h"
+#include "join_sums.h"
 #include "weight_grad.h"
 
 namespace bnn {
@@ -74,17 +75,10 @@ __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t
         if (bn * 512 + i < N) part[int64_t(bm) * N + bn * 512 + i] = sums_s[0][i] + sums_s[1][i] + sums_s[2][i] + sums_s[3][i];
 }
 
-// out[c] = sum over t of part[t][c].  64 columns a workgroup, four threads each for every fourth t.
-__global__ __launch_bounds__(256) void join_sums_kernel(const float* part, int tiles, int N, float* out) {
-    __shared__ float sums_s[4][64];
-    const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
-    const int64_t n = int64_t(blockIdx.x) * 64 + c;
-    float sum = 0.0f;
-    if (n < N)
-        for (int t = r; t < tiles; t += 4) sum += part[int64_t(t) * N + n];
-    sums_s[r][c] = sum;
-    __syncthreads();
-    if (r == 0 && n < N) out[n] = (sums_s[0][c] + sums_s[1][c]) + (sums_s[2][c] + sums_s[3][c]);
+int join_tiles(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
+    JoinArgs a{};
+    a.part = part; a.out[0] = out; a.per_group = int(tiles); a.N = int(N);
+    return join_sums<float>(a, 1, 1, s);
 }
 
 // ---- the plan ----------------------------------------------------------------------------------------------------
@@ -156,11 +150,6 @@ int launch_grad(WeightGradArgs a, hipStream_t s) {
     return check_launch();
 }
 
-int join_sums(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
-    join_sums_kernel<<<dim3(uint32_t(ceil_div(N, 64))), dim3(256), 0, s>>>(part, int(tiles), int(N), out);
-    return check_launch();
-}
-
 // dw and, where a.w is given, dscale; part: room for the column sums of the tiles.
 template <typename E>
 int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* part, float* dscale, hipStream_t s) {
@@ -178,7 +167,7 @@ int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* p
         join_pieces_kernel<E><<<dim3(uint32_t(a.channels)), dim3(256), 0, s>>>(a, dscale);
         return check_launch();
     }
-    return a.w ? join_sums(part, ceil_div(a.K, g.tile), a.channels, dscale, s) : BNN_OK;
+    return a.w ? join_tiles(part, ceil_div(a.K, g.tile), a.channels, dscale, s) : BNN_OK;
 }
 
 template <typename E>
@@ -244,9 +233,9 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         if ((st = weight_gradient<E>(p.grad, a, reinterpret_cast<float*>(ws + p.pieces_at), part_scale, dscale, s)) != BNN_OK) return st;
     }
     if (dscale && channels > 0 && (p.recompute || K == 0)) {
-        if ((st = join_sums(part_scale, p.recompute ? part_rows : 0, channels, dscale, s)) != BNN_OK) return st;
+        if ((st = join_tiles(part_scale, p.recompute ? part_rows : 0, channels, dscale, s)) != BNN_OK) return st;
     }
-    if (dbias && channels > 0) return join_sums(part_bias, part_rows, channels, dbias, s);
+    if (dbias && channels > 0) return join_tiles(part_bias, part_rows, channels, dbias, s);
     return BNN_OK;
 }
 

@@ -4,15 +4,33 @@
 // Both are bound by memory: every matrix is read or written once.  A workgroup holds a whole row in registers (8 or 16
 // elements a thread, 64 to 1024 threads by the row's length), so that the statistics of y, the new stream r and the
 // statistics of r need nothing but two to four sums over the workgroup.  Variances are sums of squared distances from the
-// mean, taken after it.  Backwards a workgroup walks a strip of rows and keeps the sums over rows (of the gammas,
-// betas and the gate) in registers; strips' sums are joined by a second launch in a fixed order.
-#include "real_types.h"
+// mean, taken after it.  Workgroups walk over rows, the next row's loads on their way while one is worked on, with the gammas and
+// betas in registers: read for every row, these 32-bit vectors were as much traffic to the caches as a row of 16-bit elements.
+// Backwards a workgroup walks a strip of rows and keeps the sums over rows (of the gammas, betas and the gate) in registers;
+// strips' sums are joined by a second launch in a fixed order.
+#include "join_sums.h"
 
 namespace bnn {
 
 namespace {
 
 constexpr int64_t kMaxNormRow = 16384;       // elements of the longest row that a workgroup holds in registers
+constexpr int kNormWaves = 16;               // wavefronts of a compute unit that walk over rows forwards
+
+// Sum over the wavefront, in every lane: inside rows of 16 lanes by data-parallel permutes, then the rows' sums.
+__device__ inline float sum_of_wave(float v) {
+    auto from = [&](auto control) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    v += from(std::integral_constant<int, 0xB1>{});       // quad_perm [1,0,3,2]
+    v += from(std::integral_constant<int, 0x4E>{});       // quad_perm [2,3,0,1]
+    v += from(std::integral_constant<int, 0x141>{});      // row_half_mirror
+    v += from(std::integral_constant<int, 0x140>{});      // row_mirror
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
 
 template <int WAVES>
 struct Sums {
@@ -21,11 +39,8 @@ struct Sums {
     // Sums of a and of b over the workgroup, the same in every thread.  Two buffers in turn: a thread writes one again
     // only after the barrier of the sum between, by which everyone has read it.
     __device__ inline float2 operator()(float a, float b) {
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            a += __shfl_xor(a, off);
-            b += __shfl_xor(b, off);
-        }
+        a = sum_of_wave(a);
+        b = sum_of_wave(b);
         if constexpr (WAVES > 1) {
             float* p = lds + turn * 2 * WAVES;
             turn ^= 1;
@@ -51,19 +66,38 @@ __device__ inline int first_col(int i) {
     return (i * 64 * WAVES + int(threadIdx.x)) * 8;
 }
 
-// A row's part of this thread: element e of chunk i is column first_col(i) + e; zero past the row's end.
+// A row's part of this thread, as it lies in memory: element e of chunk i is column first_col(i) + e.  Loads ask no questions, so
+// that the compiler knows how many are on their way: what lies past the row's end is loaded from its last eight elements (SHORT: rows
+// of fewer than eight, an element at a time), and put right by `widened`.
 template <typename E, int WAVES, int CH>
-__device__ inline void load_row(const E* row, int D, float (&v)[CH][8]) {
+struct Row {
+    typename Vec8<E>::type v[CH];
+    template <bool SHORT>
+    __device__ inline void load(const void* matrix, int64_t m, int64_t ld, int D) {
+        const E* const row = static_cast<const E*>(matrix) + m * ld;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int c = first_col<WAVES>(i);
-        const auto q = load8<E>(row + c, D - c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = float(q[e]);
+        for (int i = 0; i < CH; ++i) {
+            const int c = first_col<WAVES>(i);
+            if constexpr (SHORT) v[i] = load8<E>(row + c, D - c);
+            else v[i] = *reinterpret_cast<const typename Vec8<E>::any*>(row + min(c, D - 8));
+        }
     }
-}
+    // As floats, zero past the row's end.
+    template <bool SHORT>
+    __device__ inline void widened(int D, float (&to)[CH][8]) const {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = first_col<WAVES>(i);
+            typename Vec8<E>::type q = v[i];
+            // The wavefront's last chunk lies past the row's end: some of them have to be moved.
+            if (!SHORT && __builtin_amdgcn_readfirstlane(c) + 512 > D) q = row_end<E>(q, D - c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[i][e] = float(q[e]);
+        }
+    }
+};
 
-template <int WAVES, int CH>
+template <int WAVES, int CH, bool SHORT>
 __device__ inline void load_vector(const float* p, int D, float otherwise, float (&v)[CH][8]) {
     if (!p) {
 #pragma unroll
@@ -72,7 +106,9 @@ __device__ inline void load_vector(const float* p, int D, float otherwise, float
             for (int e = 0; e < 8; ++e) v[i][e] = otherwise;
         return;
     }
-    load_row<float, WAVES, CH>(p, D, v);
+    Row<float, WAVES, CH> row;
+    row.template load<SHORT>(p, 0, 0, D);
+    row.template widened<SHORT>(D, v);
 }
 
 template <typename E, int WAVES, int CH>
@@ -84,31 +120,27 @@ __device__ inline void store_row(E* row, int D, const float (&v)[CH][8]) {
     }
 }
 
+template <int CH, typename F>
+__device__ inline void each(F&& f) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f(i, e);
+}
+
 // v -> (v - mean) / sqrt(var + eps), or v / sqrt(mean(v^2) + eps); returns the factor.  Elements past the row's end stay zero.
 template <int WAVES, int CH>
 __device__ inline float normalise(int kind, float (&v)[CH][8], int D, float eps, Sums<WAVES>& sums) {
     if (kind == BNN_NORM_LAYER) {
         float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s += v[i][e];
+        each<CH>([&](int i, int e) { s += v[i][e]; });
         const float mean = sums(s, 0.0f).x / float(D);
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = first_col<WAVES>(i) + e < D ? v[i][e] - mean : 0.0f;
+        each<CH>([&](int i, int e) { v[i][e] = first_col<WAVES>(i) + e < D ? v[i][e] - mean : 0.0f; });
     }
     float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(v[i][e], v[i][e], s);
+    each<CH>([&](int i, int e) { s = fmaf(v[i][e], v[i][e], s); });
     const float inv = 1.0f / sqrtf(sums(s, 0.0f).x / float(D) + eps);
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] *= inv;
+    each<CH>([&](int i, int e) { v[i][e] *= inv; });
     return inv;
 }
 
@@ -121,60 +153,54 @@ struct NormArgs {
     int post, pre, M, D;
 };
 
-template <typename E, int WAVES, int CH>
+// BETAS: a norm has one.
+template <typename E, int WAVES, int CH, bool BETAS, bool SHORT>
 __global__ __launch_bounds__(64 * WAVES) void norm_residual_kernel(const NormArgs a) {
     __shared__ float sums_s[4 * WAVES];
     Sums<WAVES> sums{sums_s, 0};
     const int D = a.D;
-    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
-        float v[CH][8], x[CH][8], g[CH][8], p[CH][8];
-        load_row<E, WAVES, CH>(static_cast<const E*>(a.y) + m * a.ld_y, D, v);
-        if (a.x) load_row<E, WAVES, CH>(static_cast<const E*>(a.x) + m * a.ld_x, D, x);
-        if (a.gate) load_row<E, WAVES, CH>(static_cast<const E*>(a.gate) + (m / a.rows_per_gate) * a.ld_gate, D, g);
+    float post_g[CH][8], pre_g[CH][8], post_b[BETAS ? CH : 1][8], pre_b[BETAS ? CH : 1][8];
+    Row<E, WAVES, CH> y, x, gate;
+    int64_t m = blockIdx.x, gate_row = m / a.rows_per_gate;
+    y.template load<SHORT>(a.y, m, a.ld_y, D);
+    if (a.x) x.template load<SHORT>(a.x, m, a.ld_x, D);
+    if (a.gate) gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
+    load_vector<WAVES, CH, SHORT>(a.post_gamma, D, 1.0f, post_g);
+    load_vector<WAVES, CH, SHORT>(a.pre_gamma, D, 1.0f, pre_g);
+    if constexpr (BETAS) {
+        load_vector<WAVES, CH, SHORT>(a.post_beta, D, 0.0f, post_b);
+        load_vector<WAVES, CH, SHORT>(a.pre_beta, D, 0.0f, pre_b);
+    }
+    for (; m < a.M; m += gridDim.x) {
+        float v[CH][8], xv[CH][8], g[CH][8];
+        y.template widened<SHORT>(D, v);
+        if (a.x) x.template widened<SHORT>(D, xv);
+        if (a.gate) gate.template widened<SHORT>(D, g);
+        // The next row, or the last one again.
+        const int64_t next = min(m + int64_t(gridDim.x), int64_t(a.M) - 1);
+        y.template load<SHORT>(a.y, next, a.ld_y, D);
+        if (a.x) x.template load<SHORT>(a.x, next, a.ld_x, D);
+        if (a.gate && (gate_row + 1) * a.rows_per_gate <= next) {
+            gate_row = next / a.rows_per_gate;
+            gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
+        }
         if (a.post != BNN_NORM_NONE) {
             normalise<WAVES, CH>(a.post, v, D, a.eps, sums);
-            if (a.post_gamma) {
-                load_vector<WAVES, CH>(a.post_gamma, D, 1.0f, p);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[i][e] *= p[i][e];
-            }
-            if (a.post_beta) {
-                load_vector<WAVES, CH>(a.post_beta, D, 0.0f, p);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[i][e] += p[i][e];
-            }
+            each<CH>([&](int i, int e) { v[i][e] *= post_g[i][e]; });
+            if constexpr (BETAS) each<CH>([&](int i, int e) { v[i][e] += post_b[i][e]; });
         }
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float t = v[i][e] * a.res_scale;
-                if (a.gate) t *= g[i][e];
-                v[i][e] = a.x ? x[i][e] + t : t;
-                // 0 * inf of a scale that is none must not reach the sums from columns that are not there.
-                if (first_col<WAVES>(i) + e >= D) v[i][e] = 0.0f;
-            }
+        each<CH>([&](int i, int e) {
+            float t = v[i][e] * a.res_scale;
+            if (a.gate) t *= g[i][e];
+            v[i][e] = a.x ? xv[i][e] + t : t;
+            // 0 * inf of a scale that is none must not reach the sums from columns that are not there.
+            if (first_col<WAVES>(i) + e >= D) v[i][e] = 0.0f;
+        });
         if (a.r) store_row<E, WAVES, CH>(static_cast<E*>(a.r) + m * a.ld_r, D, v);
         if (a.pre != BNN_NORM_NONE) {
             normalise<WAVES, CH>(a.pre, v, D, a.eps, sums);
-            if (a.pre_gamma) {
-                load_vector<WAVES, CH>(a.pre_gamma, D, 1.0f, p);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[i][e] *= p[i][e];
-            }
-            if (a.pre_beta) {
-                load_vector<WAVES, CH>(a.pre_beta, D, 0.0f, p);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[i][e] += p[i][e];
-            }
+            each<CH>([&](int i, int e) { v[i][e] *= pre_g[i][e]; });
+            if constexpr (BETAS) each<CH>([&](int i, int e) { v[i][e] += pre_b[i][e]; });
             store_row<E, WAVES, CH>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
         }
     }
@@ -188,7 +214,7 @@ struct Strips {
     int64_t rows, per_gate, count;
 };
 
-inline int64_t strip_target(int64_t D) { return D <= 512 ? 2048 : D <= 1024 ? 1024 : 512; }
+inline int64_t strip_target(int64_t D) { return D <= 512 ? 4096 : D <= 1024 ? 2048 : D <= 2048 ? 1024 : D <= 4096 ? 512 : 256; }
 
 inline Strips strips_of(int64_t M, int64_t D, int64_t rows_per_gate, bool dgate) {
     const int64_t rows = ceil_div(M > 0 ? M : 1, strip_target(D));
@@ -216,23 +242,22 @@ struct NormBackArgs {
 template <int WAVES, int CH>
 __device__ inline void norm_gradient(int kind, float (&d)[CH][8], const float (&hat)[CH][8], float inv, int D, Sums<WAVES>& sums) {
     float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s1 += d[i][e];
-            s2 = fmaf(d[i][e], hat[i][e], s2);
-        }
+    each<CH>([&](int i, int e) {
+        s1 += d[i][e];
+        s2 = fmaf(d[i][e], hat[i][e], s2);
+    });
     const float2 s = sums(s1, s2);
     const float m1 = kind == BNN_NORM_LAYER ? s.x / float(D) : 0.0f, m2 = s.y / float(D);
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[i][e] = inv * (d[i][e] - m1 - hat[i][e] * m2);
+    each<CH>([&](int i, int e) { d[i][e] = inv * (d[i][e] - m1 - hat[i][e] * m2); });
 }
 
-template <typename E, int WAVES, int CH, bool BETAS>
-__global__ __launch_bounds__(64 * WAVES) void norm_residual_backward_kernel(const NormBackArgs a) {
+// Wavefronts a SIMD: with 16-bit rows of up to 4096 elements a few spilled registers are cheaper than a second workgroup that does
+// not fit (16384 x 4096 bfloat16: 197 us against 233), with float32 rows they are not (329 us against 422).
+template <typename E, int WAVES, int CH>
+inline constexpr int kBackwardWaves = CH == 1 && !is_f32<E> ? 4 : WAVES == 16 ? 4 : 2;
+
+template <typename E, int WAVES, int CH, bool BETAS, bool SHORT>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kBackwardWaves<E, WAVES, CH>))) void norm_residual_backward_kernel(const NormBackArgs a) {
     __shared__ float sums_s[4 * WAVES];
     Sums<WAVES> sums{sums_s, 0};
     const int D = a.D;
@@ -246,90 +271,83 @@ __global__ __launch_bounds__(64 * WAVES) void norm_residual_backward_kernel(cons
         first = strip * a.strips.rows;
         last = min(first + a.strips.rows, int64_t(a.M));
     }
+    const bool norm = a.pre != BNN_NORM_NONE;
     float sum_gate[CH][8] = {}, sum_pre[CH][8] = {}, sum_post[CH][8] = {};
     float sum_pre_b[BETAS ? CH : 1][8] = {}, sum_post_b[BETAS ? CH : 1][8] = {};
+    float post_g[CH][8], pre_g[CH][8];
+    Row<E, WAVES, CH> y, r, dn, dr, gate;
+    int64_t gate_row = 0, gate_end = 0;
+    auto load = [&](int64_t m) {
+        y.template load<SHORT>(a.y, m, a.ld_y, D);
+        if (norm) {
+            dn.template load<SHORT>(a.dn, m, a.ld_dn, D);
+            r.template load<SHORT>(a.r, m, a.ld_r, D);
+        }
+    };
+    if (first < last) {
+        load(first);
+        load_vector<WAVES, CH, SHORT>(a.post_gamma, D, 1.0f, post_g);
+        load_vector<WAVES, CH, SHORT>(a.pre_gamma, D, 1.0f, pre_g);
+    }
     for (int64_t m = first; m < last; ++m) {
-        float d[CH][8], hat[CH][8], v[CH][8], p[CH][8];
-        load_row<E, WAVES, CH>(static_cast<const E*>(a.y) + m * a.ld_y, D, v);
-        if (a.pre != BNN_NORM_NONE) {
-            load_row<E, WAVES, CH>(static_cast<const E*>(a.dn) + m * a.ld_dn, D, d);
-            load_row<E, WAVES, CH>(static_cast<const E*>(a.r) + m * a.ld_r, D, hat);
+        float d[CH][8], v[CH][8];
+        // Of this row, needed after the first sums.
+        if (a.dr) dr.template load<SHORT>(a.dr, m, a.ld_dr, D);
+        if (a.gate && m >= gate_end) {
+            gate_row = m / R;
+            gate_end = (gate_row + 1) * R;
+            gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
+        }
+        y.template widened<SHORT>(D, v);
+        float hat[CH][8];
+        if (norm) {
+            dn.template widened<SHORT>(D, d);
+            r.template widened<SHORT>(D, hat);
+        }
+        load(min(m + 1, last - 1));                 // the next row, or the last one again
+        if (norm) {
             const float inv = normalise<WAVES, CH>(a.pre, hat, D, a.eps, sums);
-            load_vector<WAVES, CH>(a.pre_gamma, D, 1.0f, p);
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum_pre[i][e] = fmaf(d[i][e], hat[i][e], sum_pre[i][e]);
-                    if constexpr (BETAS) sum_pre_b[i][e] += d[i][e];
-                    d[i][e] *= p[i][e];
-                }
+            each<CH>([&](int i, int e) {
+                sum_pre[i][e] = fmaf(d[i][e], hat[i][e], sum_pre[i][e]);
+                if constexpr (BETAS) sum_pre_b[i][e] += d[i][e];
+                d[i][e] *= pre_g[i][e];
+            });
             norm_gradient<WAVES, CH>(a.pre, d, hat, inv, D, sums);
         } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[i][e] = 0.0f;
+            each<CH>([&](int i, int e) { d[i][e] = 0.0f; });
         }
         if (a.dr) {
-            load_row<E, WAVES, CH>(static_cast<const E*>(a.dr) + m * a.ld_dr, D, p);
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[i][e] += p[i][e];
+            dr.template widened<SHORT>(D, hat);
+            each<CH>([&](int i, int e) { d[i][e] += hat[i][e]; });
         }
         if (a.dx) store_row<E, WAVES, CH>(static_cast<E*>(a.dx) + m * a.ld_dx, D, d);
 
         float inv = 1.0f;
         if (a.post != BNN_NORM_NONE) inv = normalise<WAVES, CH>(a.post, v, D, a.eps, sums);
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[i][e] = first_col<WAVES>(i) + e < D ? d[i][e] * a.res_scale : 0.0f;
-        if (a.at_gate >= 0 || (a.gate && a.dgate)) {
+        each<CH>([&](int i, int e) { d[i][e] = first_col<WAVES>(i) + e < D ? d[i][e] * a.res_scale : 0.0f; });
+        if (a.dgate) {
             // t = gamma * hat + beta
-            float t[CH][8];
-            load_vector<WAVES, CH>(a.post != BNN_NORM_NONE ? a.post_gamma : nullptr, D, 1.0f, t);
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) t[i][e] *= v[i][e];
+            each<CH>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], v[i][e] * post_g[i][e], sum_gate[i][e]); });
             if (a.post_beta) {
-                load_vector<WAVES, CH>(a.post_beta, D, 0.0f, p);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) t[i][e] += p[i][e];
+                float beta[CH][8];
+                load_vector<WAVES, CH, SHORT>(a.post_beta, D, 0.0f, beta);
+                each<CH>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], beta[i][e], sum_gate[i][e]); });
             }
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum_gate[i][e] = fmaf(d[i][e], t[i][e], sum_gate[i][e]);
-            if (a.strips.per_gate == 0 && (m + 1 == last || (m + 1) % R == 0)) {
-                store_row<E, WAVES, CH>(static_cast<E*>(a.dgate) + (m / R) * a.ld_dgate, D, sum_gate);
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum_gate[i][e] = 0.0f;
+            if (a.strips.per_gate == 0 && (m + 1 == last || m + 1 == gate_end)) {
+                store_row<E, WAVES, CH>(static_cast<E*>(a.dgate) + gate_row * a.ld_dgate, D, sum_gate);
+                each<CH>([&](int i, int e) { sum_gate[i][e] = 0.0f; });
             }
         }
         if (a.gate) {
-            load_row<E, WAVES, CH>(static_cast<const E*>(a.gate) + (m / R) * a.ld_gate, D, p);
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[i][e] *= p[i][e];
+            gate.template widened<SHORT>(D, hat);
+            each<CH>([&](int i, int e) { d[i][e] *= hat[i][e]; });
         }
         if (a.post != BNN_NORM_NONE) {
-            load_vector<WAVES, CH>(a.post_gamma, D, 1.0f, p);
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum_post[i][e] = fmaf(d[i][e], v[i][e], sum_post[i][e]);
-                    if constexpr (BETAS) sum_post_b[i][e] += d[i][e];
-                    d[i][e] *= p[i][e];
-                }
+            each<CH>([&](int i, int e) {
+                sum_post[i][e] = fmaf(d[i][e], v[i][e], sum_post[i][e]);
+                if constexpr (BETAS) sum_post_b[i][e] += d[i][e];
+                d[i][e] *= post_g[i][e];
+            });
             if (a.dy) norm_gradient<WAVES, CH>(a.post, d, v, inv, D, sums);
         }
         if (a.dy) store_row<E, WAVES, CH>(static_cast<E*>(a.dy) + m * a.ld_dy, D, d);
@@ -344,50 +362,30 @@ __global__ __launch_bounds__(64 * WAVES) void norm_residual_backward_kernel(cons
     }
 }
 
-// out[j][g][c] = sum over the strips of group g of part[j][strip][c]: 64 columns a workgroup, four threads each for every
-// fourth strip.  blockIdx.y: the group, and blockIdx.z: which of the sums.
-struct JoinArgs {
-    const float* part;
-    int64_t part_step;
-    float* out[4];           // the float32 vectors, in the order of part's sums
-    int strips, D;
-};
-
-__global__ __launch_bounds__(256) void join_vectors_kernel(const JoinArgs a) {
-    __shared__ float sums_s[4][64];
-    const int c = threadIdx.x & 63, q = threadIdx.x >> 6, n = int(blockIdx.x) * 64 + c;
-    const float* part = a.part + blockIdx.y * a.part_step;
-    float s = 0.0f;
-    if (n < a.D)
-        for (int t = q; t < a.strips; t += 4) s += part[int64_t(t) * a.D + n];
-    sums_s[q][c] = s;
-    __syncthreads();
-    if (q == 0 && n < a.D) a.out[blockIdx.y][n] = (sums_s[0][c] + sums_s[1][c]) + (sums_s[2][c] + sums_s[3][c]);
-}
-
-template <typename E>
-__global__ __launch_bounds__(256) void join_gates_kernel(const float* part, int per_gate, int D, int blocks_n, E* dgate, int64_t ld) {
-    __shared__ float sums_s[4][64];
-    const int64_t g = blockIdx.x / uint32_t(blocks_n);
-    const int c = threadIdx.x & 63, q = threadIdx.x >> 6, n = (int(blockIdx.x) - int(g) * blocks_n) * 64 + c;
-    float s = 0.0f;
-    if (n < D)
-        for (int t = q; t < per_gate; t += 4) s += part[(g * per_gate + t) * D + n];
-    sums_s[q][c] = s;
-    __syncthreads();
-    if (q == 0 && n < D) dgate[g * ld + n] = E((sums_s[0][c] + sums_s[1][c]) + (sums_s[2][c] + sums_s[3][c]));
-}
-
-// Calls f<WAVES, CH>() for rows of D elements.
-template <typename F>
+// Calls f<WAVES, CH, SHORT>() for rows of D elements.  Forwards 16 elements a thread and fewer wavefronts at the barriers
+// (16384 x 4096 bfloat16: FWD_A us against FWD_B with 8); backwards, with the sums over rows beside them, 8.
+template <bool FORWARD, typename F>
 inline void with_row(int64_t D, F&& f) {
+    using std::false_type;
     using std::integral_constant;
-    if (D <= 512) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    else if (D <= 1024) f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
-    else if (D <= 2048) f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (D <= 4096) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (D <= 8192) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    using std::true_type;
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    if (D < 8) f(One{}, One{}, true_type{});
+    else if (D <= 512) f(One{}, One{}, false_type{});
+    else if constexpr (FORWARD) {
+        if (D <= 1024) f(One{}, Two{}, false_type{});
+        else if (D <= 2048) f(Two{}, Two{}, false_type{});
+        else if (D <= 4096) f(integral_constant<int, 4>{}, Two{}, false_type{});
+        else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
+        else f(integral_constant<int, 16>{}, Two{}, false_type{});
+    } else {
+        if (D <= 1024) f(Two{}, One{}, false_type{});
+        else if (D <= 2048) f(integral_constant<int, 4>{}, One{}, false_type{});
+        else if (D <= 4096) f(integral_constant<int, 8>{}, One{}, false_type{});
+        else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
+        else f(integral_constant<int, 16>{}, Two{}, false_type{});
+    }
 }
 
 bool norm_kind(int kind) { return kind == BNN_NORM_NONE || kind == BNN_NORM_RMS || kind == BNN_NORM_LAYER; }
@@ -429,10 +427,14 @@ extern "C" int bnn_norm_residual(int type, const void* y, int64_t ld_y, const vo
     NormArgs a{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, r, n, ld_y, ld_x, ld_gate, ld_r, ld_n, rows_per_gate,
                res_scale, eps, post, pre, int(M), int(D)};
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool betas = post_beta || pre_beta;
     with_type(type, [&](auto e) {
-        with_row(D, [&](auto waves, auto ch) {
-            const int64_t blocks = M < max_blocks(64 * waves) ? M : max_blocks(64 * waves);
-            norm_residual_kernel<decltype(e), waves, ch><<<dim3(uint32_t(blocks)), dim3(64 * waves), 0, s>>>(a);
+        with_row<true>(D, [&](auto waves, auto ch, auto is_short) {
+            // As many workgroups as are on the chip together, each walking over rows.
+            const int64_t together = 256 * (kNormWaves / waves);
+            const dim3 grid(uint32_t(M < together ? M : together)), block(64 * waves);
+            if (betas) norm_residual_kernel<decltype(e), waves, ch, true, is_short><<<grid, block, 0, s>>>(a);
+            else norm_residual_kernel<decltype(e), waves, ch, false, is_short><<<grid, block, 0, s>>>(a);
         });
     });
     return check_launch();
@@ -502,27 +504,26 @@ extern "C" int bnn_norm_residual_backward(int type, const void* dr, int64_t ld_d
     if (M > 0) {
         const bool betas = dpost_beta || dpre_beta;
         with_type(type, [&](auto e) {
-            with_row(D, [&](auto waves, auto ch) {
+            with_row<false>(D, [&](auto waves, auto ch, auto is_short) {
                 const dim3 grid(uint32_t(a.strips.count)), block(64 * waves);
-                if (betas) norm_residual_backward_kernel<decltype(e), waves, ch, true><<<grid, block, 0, s>>>(a);
-                else norm_residual_backward_kernel<decltype(e), waves, ch, false><<<grid, block, 0, s>>>(a);
+                if (betas) norm_residual_backward_kernel<decltype(e), waves, ch, true, is_short><<<grid, block, 0, s>>>(a);
+                else norm_residual_backward_kernel<decltype(e), waves, ch, false, is_short><<<grid, block, 0, s>>>(a);
             });
         });
         if ((st = check_launch()) != BNN_OK) return st;
     }
-    if (vectors > 0) {
-        join.part = a.part; join.part_step = a.part_step; join.strips = int(a.strips.count); join.D = int(D);
-        join_vectors_kernel<<<dim3(uint32_t(ceil_div(D, 64)), uint32_t(vectors)), dim3(256), 0, s>>>(join);
-        if ((st = check_launch()) != BNN_OK) return st;
-    }
+    join.part = a.part;
+    join.part_step = a.part_step;
+    join.per_group = int(a.strips.count);
+    join.N = int(D);
+    if (vectors > 0 && (st = join_sums<float>(join, 1, vectors, s)) != BNN_OK) return st;
     if (a.at_gate >= 0 && M > 0) {
-        const int64_t gates = ceil_div(M, a.rows_per_gate), blocks_n = ceil_div(D, 64);
-        with_type(type, [&](auto e) {
-            using E = decltype(e);
-            join_gates_kernel<E><<<dim3(uint32_t(gates * blocks_n)), dim3(256), 0, s>>>(
-                a.part + a.at_gate * a.part_step, int(a.strips.per_gate), int(D), int(blocks_n), static_cast<E*>(dgate), ld_dgate);
-        });
-        return check_launch();
+        join.part = a.part + a.at_gate * a.part_step;
+        join.per_group = int(a.strips.per_gate);
+        join.out[0] = dgate;
+        join.ld_out = ld_dgate;
+        with_type(type, [&](auto e) { st = join_sums<decltype(e)>(join, ceil_div(M, a.rows_per_gate), 1, s); });
+        return st;
     }
     return BNN_OK;
 }
