@@ -661,6 +661,10 @@ def linear_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | Non
                 act: int = ACT_NONE, residual: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """bnn_linear_bits: real x [M][K], packed weights [N][ceil(K/32)] -> act(scale * (x w^T) + bias) + residual [M][N].
     `out` may be `residual`."""
+    if out is not None and _calls is not None:
+        st = _calls.linear_bits(x, w_bits, scale, bias, act, residual, out)
+        if st == 0 or _took("bnn_linear_bits", st):
+            return out
     lib = load_library()
     _real(x, "x")
     _weights(x, w_bits)
@@ -686,6 +690,10 @@ def gated_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None
                act: int = ACT_SILU, out: torch.Tensor | None = None) -> torch.Tensor:
     """bnn_gated_bits: real x [M][K], packed weights [2F][ceil(K/32)] (the gate's rows first) -> act(z_gate) * z_up [M][F]
     with z = scale * (x w^T) + bias."""
+    if out is not None and _calls is not None:
+        st = _calls.gated_bits(x, w_bits, scale, bias, act, out)
+        if st == 0 or _took("bnn_gated_bits", st):
+            return out
     lib = load_library()
     _real(x, "x")
     _weights(x, w_bits)
@@ -755,6 +763,11 @@ def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Te
                   eps: float = 1e-5, rows_per_gate: int = 1, out: torch.Tensor | None = None, out_n: torch.Tensor | None = None):
     """bnn_norm_residual: (r, n) with r = x + res_scale * gate * post(y) and n = pre(r); n is None without a `pre` norm.
     Row m has the gate's row m // rows_per_gate.  `out` may be `x`."""
+    if out is not None and _calls is not None:
+        st = _calls.norm_residual(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
+                                  out, out_n)
+        if st == 0 or _took("bnn_norm_residual", st):
+            return out, out_n
     lib = load_library()
     _real(y, "y")
     M, D = y.shape

@@ -18,8 +18,8 @@ namespace {
 
 // ---- transposed weights ------------------------------------------------------------------------------------------
 // out[k] bit n of a row of `half` columns a half: w[n][k] and, from column `half` on, w[F + n][k]; 0 for rows that are not there.
-// A workgroup turns 512 rows x 128 columns: each half wavefront blocks of 32 x 32 in registers, LDS puts words of a row together.
-constexpr int kTurnWords = 16, kTurnK = 128;
+// A workgroup turns 256 rows x 128 columns: each half wavefront blocks of 32 x 32 in registers, LDS puts words of a row together.
+constexpr int kTurnWords = 8, kTurnK = 128;
 
 __global__ __launch_bounds__(256) void transpose_weights_kernel(const uint32_t* w, int64_t ld_w, int F, int half, int halves, int K,
                                                                 uint32_t* out, int64_t ld_out, int blocks_k) {
@@ -232,11 +232,17 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.channels = int(channels);
         if ((st = weight_gradient<E>(p.grad, a, reinterpret_cast<float*>(ws + p.pieces_at), part_scale, dscale, s)) != BNN_OK) return st;
     }
-    if (dscale && channels > 0 && (p.recompute || K == 0)) {
+    if (channels == 0) return BNN_OK;
+    if (p.recompute && dscale && dbias) {
+        JoinArgs a{};
+        a.part = part_scale; a.part_step = part_bias - part_scale; a.out[0] = dscale; a.out[1] = dbias;
+        a.per_group = int(part_rows); a.N = int(channels);
+        return join_sums<float>(a, 1, 2, s);
+    }
+    if (dscale && (p.recompute || K == 0)) {
         if ((st = join_tiles(part_scale, p.recompute ? part_rows : 0, channels, dscale, s)) != BNN_OK) return st;
     }
-    if (dbias && channels > 0) return join_tiles(part_bias, part_rows, channels, dbias, s);
-    return BNN_OK;
+    return dbias ? join_tiles(part_bias, part_rows, channels, dbias, s) : BNN_OK;
 }
 
 // Sizes that a call takes; BNN_OK or what it answers.

@@ -60,31 +60,38 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
     if (m >= a.M) return;
     if constexpr (EPI == kLinear) {
         if (valid <= 0) return;
-        float r[W] = {}, v[W];
+        float r[W] = {}, z[W], v[W];
         if (a.residual) load_some<E, W>(static_cast<const E*>(a.residual) + int64_t(m) * a.ld_r + n, valid, r);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = activate<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i])) + r[i];
+        for (int i = 0; i < W; ++i) z[i] = fmaf(s[0][i], scale[0][i], bias[0][i]);
+        activate<FAST, W>(a.act, z, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += r[i];
         store_some<E, W>(y, v, valid);
     } else if constexpr (EPI == kGated) {
         if (valid <= 0) return;
-        float v[W];
+        float z[W], v[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i)
-            v[i] = activate<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i])) * fmaf(s[1][i], scale[1][i], bias[1][i]);
+        for (int i = 0; i < W; ++i) z[i] = fmaf(s[0][i], scale[0][i], bias[0][i]);
+        activate<FAST, W>(a.act, z, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] *= fmaf(s[1][i], scale[1][i], bias[1][i]);
         store_some<E, W>(y, v, valid);
     } else {
         if (n >= a.half) return;
-        float d[W], out[HALVES][W];
+        float d[W], z[W], f[W], slope[W], out[HALVES][W];
         load_some<E, W>(static_cast<const E*>(a.dy) + int64_t(m) * a.ld_dy + n, valid, d);
 #pragma unroll
+        for (int i = 0; i < W; ++i) z[i] = fmaf(s[0][i], scale[0][i], bias[0][i]);
+        activate_both<FAST, W>(a.act, z, f, slope);
+#pragma unroll
         for (int i = 0; i < W; ++i) {
-            float f, slope, dz[HALVES];
-            activate_both<FAST>(a.act, fmaf(s[0][i], scale[0][i], bias[0][i]), f, slope);
+            float dz[HALVES];
             if constexpr (HALVES == 2) {
-                dz[0] = d[i] * fmaf(s[1][i], scale[1][i], bias[1][i]) * slope;
-                dz[1] = d[i] * f;
+                dz[0] = d[i] * fmaf(s[1][i], scale[1][i], bias[1][i]) * slope[i];
+                dz[1] = d[i] * f[i];
             } else {
-                dz[0] = d[i] * slope;
+                dz[0] = d[i] * slope[i];
             }
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
@@ -98,13 +105,6 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) store_some<E, W>(y + int64_t(h) * a.half, out[h], W);
     }
-}
-
-// Over the 32 rows of a block's lanes: what lane 0 of each half has afterwards is their sum.
-__device__ inline float sum_rows(float v) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
 }
 
 // TN wavefronts along the channels, TM along the rows, 32-row blocks FN x FM for each.
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
                 for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float p = sum_rows(sum_s[h][i]), q = sum_rows(sum_z[h][i]);
+                        const float p = sum_of_32(sum_s[h][i]), q = sum_of_32(sum_z[h][i]);
                         if (fr == 0) {
                             sums_s[(wm * 2) * S::CN + c0 + 16 * FN * h + i] = p;
                             sums_s[(wm * 2 + 1) * S::CN + c0 + 16 * FN * h + i] = q;

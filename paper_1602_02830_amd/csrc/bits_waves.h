@@ -160,7 +160,7 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
             for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = sum_rows(sum_s[h][i]), q = sum_rows(sum_z[h][i]);
+                    const float p = sum_of_32(sum_s[h][i]), q = sum_of_32(sum_z[h][i]);
                     if (fr == 0) {
                         sums_s[(j * 2) * S::CN + c0 + 32 * FY * h + i] = p;
                         sums_s[(j * 2 + 1) * S::CN + c0 + 32 * FY * h + i] = q;

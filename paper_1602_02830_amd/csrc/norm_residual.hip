@@ -17,19 +17,10 @@ namespace {
 constexpr int64_t kMaxNormRow = 16384;       // elements of the longest row that a workgroup holds in registers
 constexpr int kNormWaves = 16;               // wavefronts of a compute unit that walk over rows forwards
 
-// Sum over the wavefront, in every lane: inside rows of 16 lanes by data-parallel permutes, then the rows' sums.
 __device__ inline float sum_of_wave(float v) {
-    auto from = [&](auto control) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xF, 0xF, true));
-    };
-    v += from(std::integral_constant<int, 0xB1>{});       // quad_perm [1,0,3,2]
-    v += from(std::integral_constant<int, 0x4E>{});       // quad_perm [2,3,0,1]
-    v += from(std::integral_constant<int, 0x141>{});      // row_half_mirror
-    v += from(std::integral_constant<int, 0x140>{});      // row_mirror
-    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+    v = sum_of_32(v);
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
 template <int WAVES>
@@ -362,8 +353,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kBac
     }
 }
 
-// Calls f<WAVES, CH, SHORT>() for rows of D elements.  Forwards 16 elements a thread and fewer wavefronts at the barriers
-// (16384 x 4096 bfloat16: FWD_A us against FWD_B with 8); backwards, with the sums over rows beside them, 8.
+// Calls f<WAVES, CH, SHORT>() for rows of D elements.  Forwards 16 elements a thread, for fewer wavefronts at the barriers;
+// backwards, with the sums over rows beside them, 8 where the row is short enough.
 template <bool FORWARD, typename F>
 inline void with_row(int64_t D, F&& f) {
     using std::false_type;
@@ -376,13 +367,17 @@ inline void with_row(int64_t D, F&& f) {
     else if constexpr (FORWARD) {
         if (D <= 1024) f(One{}, Two{}, false_type{});
         else if (D <= 2048) f(Two{}, Two{}, false_type{});
+        else if (D <= 3072) f(integral_constant<int, 3>{}, Two{}, false_type{});
         else if (D <= 4096) f(integral_constant<int, 4>{}, Two{}, false_type{});
+        else if (D <= 6144) f(integral_constant<int, 6>{}, Two{}, false_type{});
         else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
         else f(integral_constant<int, 16>{}, Two{}, false_type{});
     } else {
         if (D <= 1024) f(Two{}, One{}, false_type{});
         else if (D <= 2048) f(integral_constant<int, 4>{}, One{}, false_type{});
+        else if (D <= 3072) f(integral_constant<int, 6>{}, One{}, false_type{});
         else if (D <= 4096) f(integral_constant<int, 8>{}, One{}, false_type{});
+        else if (D <= 6144) f(integral_constant<int, 6>{}, Two{}, false_type{});
         else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
         else f(integral_constant<int, 16>{}, Two{}, false_type{});
     }

@@ -47,6 +47,13 @@ struct EntryPoints {
                                           const int32_t*, Words, uint32_t*, int64_t, void*);
     int (*conv_im2col_pack)(Words, int64_t, int64_t, int64_t, int64_t, int, int, int, int, uint32_t*, int64_t, void*);
     int (*maxpool_bits)(Words, int64_t, int64_t, int64_t, int64_t, int, int, int, Words, uint32_t*, void*);
+    int (*linear_bits)(int, const void*, int64_t, Words, int64_t, const float*, const float*, int, const void*, int64_t, void*,
+                       int64_t, int64_t, int64_t, int64_t, void*);
+    int (*gated_bits)(int, const void*, int64_t, Words, int64_t, const float*, const float*, int, void*, int64_t, int64_t, int64_t,
+                      int64_t, void*);
+    int (*norm_residual)(int, const void*, int64_t, const void*, int64_t, const void*, int64_t, int64_t, float, int, const float*,
+                         const float*, int, const float*, const float*, float, void*, int64_t, void*, int64_t, int64_t, int64_t,
+                         void*);
 };
 
 EntryPoints entry{};
@@ -391,6 +398,100 @@ PyObject* maxpool_bits(PyObject* const* a) {
     });
 }
 
+// ---- real activations, packed weights ----
+
+// The bnn_type of a matrix of activations; -1 for another type.
+int real_type(at::ScalarType t) { return t == at::kBFloat16 ? 0 : t == at::kHalf ? 1 : t == at::kFloat ? 2 : -1; }
+
+// A matrix of activations; of the type and on the device of `like`, with its rows and cols given.
+bool read_real(PyObject* o, Matrix& m, const at::Tensor* like, int64_t rows, int64_t cols) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::ScalarType type = like ? like->scalar_type() : THPVariable_Unpack(o).scalar_type();
+    if (real_type(type) < 0 || !m.read(o, type)) return false;
+    return !like || (m.t->get_device() == like->get_device() && m.rows == rows && m.cols == cols);
+}
+
+// A contiguous float32 vector of n elements on the device of `like`, or None; false for anything else.
+bool read_vector(PyObject* o, int64_t n, const at::Tensor& like, const float*& data) {
+    data = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o, at::kFloat);
+    if (!t || t->dim() != 1 || t->size(0) != n || !t->is_contiguous() || t->get_device() != like.get_device()) return false;
+    data = static_cast<const float*>(t->data_ptr());
+    return true;
+}
+
+// x, its packed weights, their scale and bias: the arguments that both products begin with.
+struct Weighted {
+    Matrix x, w;
+    const float *scale = nullptr, *bias = nullptr;
+    int type = -1;
+    bool read(PyObject* const* a) {
+        if (!read_real(a[0], x, nullptr, 0, 0) || !w.read(a[1], at::kInt) || w.t->get_device() != x.t->get_device() ||
+            w.cols < words(x.cols) || !read_vector(a[2], w.rows, *x.t, scale) || !read_vector(a[3], w.rows, *x.t, bias))
+            return false;
+        type = real_type(x.t->scalar_type());
+        return true;
+    }
+};
+
+// (x, w_bits, scale, bias, act, residual, out)
+PyObject* linear_bits(PyObject* const* a) {
+    Weighted p;
+    Matrix residual, out;
+    int act;
+    if (!p.read(a) || !small_integer(a[4], act) || !read_real(a[6], out, p.x.t, p.x.rows, p.w.rows) ||
+        (a[5] != Py_None && !read_real(a[5], residual, p.x.t, p.x.rows, p.w.rows)))
+        return long_way();
+    return launch(*out.t, [&](void* s) {
+        return entry.linear_bits(p.type, p.x.data, p.x.ld, p.w.as<uint32_t>(), p.w.ld, p.scale, p.bias, act, residual.data,
+                                 residual.ld, out.data, out.ld, p.x.rows, p.w.rows, p.x.cols, s);
+    });
+}
+
+// (x, w_bits, scale, bias, act, out)
+PyObject* gated_bits(PyObject* const* a) {
+    Weighted p;
+    Matrix out;
+    int act;
+    if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[4], act) || !read_real(a[5], out, p.x.t, p.x.rows, p.w.rows / 2))
+        return long_way();
+    return launch(*out.t, [&](void* s) {
+        return entry.gated_bits(p.type, p.x.data, p.x.ld, p.w.as<uint32_t>(), p.w.ld, p.scale, p.bias, act, out.data, out.ld,
+                                p.x.rows, p.w.rows / 2, p.x.cols, s);
+    });
+}
+
+bool real_number(PyObject* o, float& v) {
+    if (!PyFloat_CheckExact(o)) return false;
+    v = static_cast<float>(PyFloat_AS_DOUBLE(o));
+    return true;
+}
+
+// (y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, out, out_n)
+PyObject* norm_residual(PyObject* const* a) {
+    Matrix y, x, gate, out, out_n;
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+    float res_scale, eps;
+    int post, pre;
+    int64_t rows_per_gate;
+    if (!read_real(a[0], y, nullptr, 0, 0) || !real_number(a[3], res_scale) || !small_integer(a[4], post) ||
+        !small_integer(a[7], pre) || !real_number(a[10], eps) || !integer(a[11], rows_per_gate) || rows_per_gate < 1)
+        return long_way();
+    const int64_t M = y.rows, D = y.cols;
+    if ((a[1] != Py_None && !read_real(a[1], x, y.t, M, D)) ||
+        (a[2] != Py_None && !read_real(a[2], gate, y.t, M / rows_per_gate + (M % rows_per_gate != 0), D)) ||
+        !read_vector(a[5], D, *y.t, post_gamma) || !read_vector(a[6], D, *y.t, post_beta) || !read_vector(a[8], D, *y.t, pre_gamma) ||
+        !read_vector(a[9], D, *y.t, pre_beta) || !read_real(a[12], out, y.t, M, D) || (pre == 0) != (a[13] == Py_None) ||
+        (a[13] != Py_None && !read_real(a[13], out_n, y.t, M, D)))
+        return long_way();
+    return launch(*out.t, [&](void* s) {
+        return entry.norm_residual(real_type(y.t->scalar_type()), y.data, y.ld, x.data, x.ld, gate.data, gate.ld, rows_per_gate,
+                                   res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, out.data, out.ld,
+                                   out_n.data, out_n.ld, M, D, s);
+    });
+}
+
 // bind({"bnn_pack_sign": address, ...}, raw_stream)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *table, *stream;
@@ -419,6 +520,9 @@ PyObject* bind(PyObject*, PyObject* args) {
     set(e.conv_pool_windows_bn_sign_pack, "bnn_conv_pool_windows_bn_sign_pack");
     set(e.conv_im2col_pack, "bnn_conv_im2col_pack");
     set(e.maxpool_bits, "bnn_maxpool_bits");
+    set(e.linear_bits, "bnn_linear_bits");
+    set(e.gated_bits, "bnn_gated_bits");
+    set(e.norm_residual, "bnn_norm_residual");
     if (!ok || !PyCallable_Check(stream)) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point or the stream function is missing");
         return nullptr;
@@ -451,6 +555,9 @@ PyMethodDef methods[] = {
     fast<conv_pool_windows_bn_sign_pack, 11>("conv_pool_windows_bn_sign_pack"),
     fast<conv_im2col_pack, 7>("conv_im2col_pack"),
     fast<maxpool_bits, 7>("maxpool_bits"),
+    fast<linear_bits, 7>("linear_bits"),
+    fast<gated_bits, 6>("gated_bits"),
+    fast<norm_residual, 14>("norm_residual"),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -132,58 +132,82 @@ constexpr float kSqrtHalf = 0.70710678118654752f;        // sqrt(1 / 2)
 constexpr float kTwoSqrt2OverPi = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;       // 1 / sqrt(2 pi)
 
-template <bool FAST>
-__device__ inline float activate(int act, float z) {
+// W values at a time, so that one is chosen once for them.
+template <bool FAST, int W>
+__device__ inline void activate(int act, const float (&z)[W], float (&f)[W]) {
+    auto all = [&](auto&& one) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[i] = one(z[i]);
+    };
     switch (act) {
-        case BNN_ACT_RELU: return z > 0.0f ? z : z != z ? z : 0.0f;
-        case BNN_ACT_SILU: return over<FAST>(z, 1.0f + exp_of<FAST>(-z));
-        case BNN_ACT_SIGMOID: return over<FAST>(1.0f, 1.0f + exp_of<FAST>(-z));
-        case BNN_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
+        case BNN_ACT_RELU: return all([](float v) { return v > 0.0f ? v : v != v ? v : 0.0f; });
+        case BNN_ACT_SILU: return all([](float v) { return over<FAST>(v, 1.0f + exp_of<FAST>(-v)); });
+        case BNN_ACT_SIGMOID: return all([](float v) { return over<FAST>(1.0f, 1.0f + exp_of<FAST>(-v)); });
+        case BNN_ACT_GELU: return all([](float v) { return 0.5f * v * (1.0f + erff(v * kSqrtHalf)); });
         // 0.5 z (1 + tanh u) = z / (1 + e^(-2u))
-        case BNN_ACT_GELU_TANH: return over<FAST>(z, 1.0f + exp_of<FAST>(-kTwoSqrt2OverPi * (z + 0.044715f * z * z * z)));
-        default: return z;
+        case BNN_ACT_GELU_TANH:
+            return all([](float v) { return over<FAST>(v, 1.0f + exp_of<FAST>(-kTwoSqrt2OverPi * (v + 0.044715f * v * v * v))); });
+        default: return all([](float v) { return v; });
     }
 }
 
 // The activation and its derivative (of relu at 0: 0).
-template <bool FAST>
-__device__ inline void activate_both(int act, float z, float& f, float& df) {
+template <bool FAST, int W>
+__device__ inline void activate_both(int act, const float (&z)[W], float (&f)[W], float (&df)[W]) {
+    auto all = [&](auto&& one) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) one(z[i], f[i], df[i]);
+    };
     switch (act) {
         case BNN_ACT_RELU:
-            f = z > 0.0f ? z : z != z ? z : 0.0f;
-            df = z > 0.0f ? 1.0f : 0.0f;
-            break;
-        case BNN_ACT_SILU: {
-            const float s = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-z));
-            f = z * s;
-            df = s * (1.0f + z * (1.0f - s));
-            break;
-        }
-        case BNN_ACT_SIGMOID: {
-            const float s = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-z));
-            f = s;
-            df = s * (1.0f - s);
-            break;
-        }
-        case BNN_ACT_GELU: {
-            const float c = 0.5f * (1.0f + erff(z * kSqrtHalf));
-            f = z * c;
-            df = c + z * kInvSqrt2Pi * exp_of<FAST>(-0.5f * z * z);
-            break;
-        }
-        case BNN_ACT_GELU_TANH: {
-            const float u2 = kTwoSqrt2OverPi * (z + 0.044715f * z * z * z);
-            const float s = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-u2));
-            f = z * s;
-            // s (1 - s) is 0 long before the polynomial overflows, but 0 * inf is not.
-            const float slope = s * (1.0f - s);
-            df = slope == 0.0f ? s : s + z * slope * kTwoSqrt2OverPi * (1.0f + 0.134145f * z * z);
-            break;
-        }
+            return all([](float v, float& y, float& dy) {
+                y = v > 0.0f ? v : v != v ? v : 0.0f;
+                dy = v > 0.0f ? 1.0f : 0.0f;
+            });
+        case BNN_ACT_SILU:
+            return all([](float v, float& y, float& dy) {
+                const float s = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-v));
+                y = v * s;
+                dy = s * (1.0f + v * (1.0f - s));
+            });
+        case BNN_ACT_SIGMOID:
+            return all([](float v, float& y, float& dy) {
+                y = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-v));
+                dy = y * (1.0f - y);
+            });
+        case BNN_ACT_GELU:
+            return all([](float v, float& y, float& dy) {
+                const float c = 0.5f * (1.0f + erff(v * kSqrtHalf));
+                y = v * c;
+                dy = c + v * kInvSqrt2Pi * exp_of<FAST>(-0.5f * v * v);
+            });
+        case BNN_ACT_GELU_TANH:
+            return all([](float v, float& y, float& dy) {
+                const float s = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-kTwoSqrt2OverPi * (v + 0.044715f * v * v * v)));
+                y = v * s;
+                // s (1 - s) is 0 long before the polynomial overflows, but 0 * inf is not.
+                const float slope = s * (1.0f - s);
+                dy = slope == 0.0f ? s : s + v * slope * kTwoSqrt2OverPi * (1.0f + 0.134145f * v * v);
+            });
         default:
-            f = z;
-            df = 1.0f;
+            return all([](float v, float& y, float& dy) {
+                y = v;
+                dy = 1.0f;
+            });
     }
+}
+
+// Sum over each half wavefront of 32 lanes, in every lane of it: inside rows of 16 lanes by data-parallel permutes, then the rows'.
+__device__ inline float sum_of_32(float v) {
+    auto from = [&](auto control) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    v += from(std::integral_constant<int, 0xB1>{});       // quad_perm [1,0,3,2]
+    v += from(std::integral_constant<int, 0x4E>{});       // quad_perm [2,3,0,1]
+    v += from(std::integral_constant<int, 0x141>{});      // row_half_mirror
+    v += from(std::integral_constant<int, 0x140>{});      // row_mirror
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
 // ---- packed weights as operands of the matrix engine --------------------------------------------------------------
