@@ -760,9 +760,10 @@ def gated_bits_backward(dh: torch.Tensor, x: torch.Tensor, w_bits: torch.Tensor,
 def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Tensor | None = None, res_scale: float = 1.0,
                   post: int = NORM_NONE, post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None,
                   pre: int = NORM_NONE, pre_gamma: torch.Tensor | None = None, pre_beta: torch.Tensor | None = None,
-                  eps: float = 1e-5, rows_per_gate: int = 1, out: torch.Tensor | None = None, out_n: torch.Tensor | None = None):
-    """bnn_norm_residual: (r, n) with r = x + res_scale * gate * post(y) and n = pre(r); n is None without a `pre` norm.
-    Row m has the gate's row m // rows_per_gate.  `out` may be `x`."""
+                  eps: float = 1e-5, rows_per_gate: int = 1, out: torch.Tensor | None = None, out_n: torch.Tensor | None = None,
+                  need_r: bool = True):
+    """bnn_norm_residual: (r, n) with r = x + res_scale * gate * post(y) and n = pre(r); n is None without a `pre` norm, r where
+    it is not needed.  Row m has the gate's row m // rows_per_gate.  `out` may be `x`."""
     if out is not None and _calls is not None:
         st = _calls.norm_residual(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
                                   out, out_n)
@@ -777,9 +778,10 @@ def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Te
         if rows_per_gate < 1:
             raise ValueError("rows_per_gate must be positive")
         _sized(gate, -(-M // rows_per_gate), D, "gate", y)
-    if out is None:
+    if out is None and need_r:
         out = torch.empty((M, D), dtype=y.dtype, device=y.device)
-    _sized(out, M, D, "out", y)
+    if out is not None:
+        _sized(out, M, D, "out", y)
     if pre == NORM_NONE:
         if out_n is not None:
             raise ValueError("out_n needs a norm before the next block")

@@ -259,3 +259,62 @@ class BinaryConvNet:
         B.xnor_gemm(a, self.w_bits[-1], self.K[-1], out=self.scores)
         return self.scores
 
+
+
+class BinaryFeedForward:
+    """One feed-forward block of a language model with one-bit weights on a real stream, with the norms, gate and
+    residual scale around it:
+
+        n = pre(x);  h = act(n Wg) * (n Wu);  y = h Wo;  r = x + res_scale * gate * post(y);  n' = next_pre(r)
+
+    Weights are binarized with Eq. (1) and packed once; a channel's scale is the mean magnitude of its real weights.  forward()
+    takes the stream and the normalised input that the block before made of it (first_norm() for the first block) and gives
+    those for the next one; with one row it is the block's form for single tokens.  backward() follows a forward() of the same
+    rows: the gradients of the real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights,
+    here with the channel's scale, handed to the real ones), of scales, gammas and gate.
+
+    w_in: float32 device weights [2F][D], the gate's rows first; w_out: [D][F]; gammas: float32 [D] or None (1);
+    gate: [1][D] in the stream's type, shared by all rows, or None.
+    """
+
+    def __init__(self, w_in, w_out, act: int = B.ACT_SILU, pre_gamma=None, post_gamma=None, next_gamma=None, gate=None,
+                 res_scale: float = 1.0, eps: float = 1e-5):
+        self.D, self.F, self.act = int(w_out.shape[0]), int(w_out.shape[1]), act
+        if tuple(w_in.shape) != (2 * self.F, self.D):
+            raise ValueError("w_in must be [2F][D] where w_out is [D][F]")
+        self.pre_gamma, self.post_gamma, self.next_gamma = pre_gamma, post_gamma, next_gamma
+        self.gate, self.res_scale, self.eps = gate, float(res_scale), float(eps)
+        self.grads = {}
+        self.set_weights(w_in, w_out)
+        self._kept = None
+
+    def set_weights(self, w_in, w_out):
+        """Packs the weights (again, after a training step)."""
+        self.w_in, self.w_out = B.pack_sign(w_in), B.pack_sign(w_out)
+        self.scale_in, self.scale_out = w_in.abs().mean(1), w_out.abs().mean(1)
+
+    def first_norm(self, x: torch.Tensor) -> torch.Tensor:
+        """pre(x): what the first block of a stack reads beside the stream."""
+        return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, need_r=False)[1]
+
+    def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
+        """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""
+        h = B.gated_bits(n, self.w_in, self.scale_in, None, self.act)
+        y = B.linear_bits(h, self.w_out, self.scale_out)
+        r, after = B.norm_residual(y, x, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma,
+                                   None, self.eps, max(x.shape[0], 1))
+        self._kept = (n, h, y, r) if keep else None
+        return r, after
+
+    def backward(self, dr: torch.Tensor | None, dn_after: torch.Tensor):
+        """Gradients of r (by every way but n') and of n' -> (dx, dn); the parameters' gradients are left in self.grads."""
+        if self._kept is None:
+            raise RuntimeError("backward() needs a forward(keep=True) before it")
+        n, h, y, r = self._kept
+        got = B.norm_residual_backward(dr, dn_after, y, r, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
+                                       self.next_gamma, None, self.eps, max(y.shape[0], 1))
+        out = B.linear_bits_backward(got["dy"], h, self.w_out, self.scale_out)
+        gated = B.gated_bits_backward(out["dx"], n, self.w_in, self.scale_in, None, self.act)
+        self.grads = {"w_in": gated["dw"], "w_out": out["dw"], "scale_in": gated["dscale"], "scale_out": out["dscale"],
+                      "gate": got["dgate"], "post_gamma": got["dpost_gamma"], "next_gamma": got["dpre_gamma"]}
+        return got["dx"], gated["dx"]

@@ -664,6 +664,121 @@ def test_product_rows_past_2_31_elements():
     assert torch.equal(y[:-3], p.biased.bfloat16().expand(M - 3, N))
 
 
+# ---- the block -------------------------------------------------------------------------------------------------------
+
+def block64(x, n, w_in, w_out, s_in, s_out, gate, post_g, next_g, act):
+    """BinaryFeedForward in float64 on the CPU, weights +-1 as given (leaves for differentiation)."""
+    z = (n @ w_in.t()) * s_in
+    F = z.shape[1] // 2
+    y = ((phi(z[:, :F], act)[0] * z[:, F:]) @ w_out.t()) * s_out
+    r = x + 0.7 * gate * norm64(y, "rms", post_g, None)
+    return r, norm64(r, "rms", next_g, None)
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M", [1, 9, 200])
+def test_block_forwards_and_backwards(M, T):
+    T = TYPES[T]
+    D, F = 96, 160
+    g = torch.Generator().manual_seed(M)
+    w_in, w_out = torch.randn(2 * F, D, generator=g) * 0.1, torch.randn(D, F, generator=g) * 0.1
+    gammas = [1 + 0.1 * torch.randn(D, generator=g) for _ in range(3)]
+    gate = (1 + 0.1 * torch.randn(1, D, generator=g)).to(T)
+    x, dr, dn = (torch.randn(M, D, generator=g).to(T) for _ in range(3))
+    block = bnn.BinaryFeedForward(w_in.to(DEV), w_out.to(DEV), bnn.ACT_SILU, *(v.to(DEV) for v in gammas), gate.to(DEV), 0.7)
+    n = block.first_norm(x.to(DEV))
+    r, after = block.forward(x.to(DEV), n, keep=True)
+    dx, dn_in = block.backward(dr.to(DEV), dn.to(DEV))
+    d = lambda t: t.double().requires_grad_(True)
+    sign = lambda w: torch.where(w >= 0, 1.0, -1.0).double().requires_grad_(True)
+    leaves = {"x": d(x), "n": d(n.cpu()), "w_in": sign(w_in), "w_out": sign(w_out), "scale_in": d(block.scale_in.cpu()),
+              "scale_out": d(block.scale_out.cpu()), "gate": d(gate), "post_gamma": d(gammas[1]), "next_gamma": d(gammas[2])}
+    want_n = norm64(leaves["x"].detach(), "rms", gammas[0].double(), None)
+    close(n, want_n, norm_tol(want_n, T, D, 16.0), "first norm")
+    wr, wa = block64(*leaves.values(), "silu")
+    ((wr * dr.double()).sum() + (wa * dn.double()).sum()).backward()
+    # h, y and r, and backwards dr's sum, dy, dh and ds, are rounded to the type on the way: eight roundings of values of the size of
+    # their tensor, each of which reaches a result through factors of order one (norms divide by their size).
+    def near(got, want, what):
+        err = (got.detach().cpu().double() - want).norm() / want.norm()
+        assert err <= 8 * ROUND[T] + 1e-5, (what, err)
+    near(r, wr.detach(), "r")
+    near(after, wa.detach(), "n'")
+    near(dx, leaves["x"].grad, "dx")
+    near(dn_in, leaves["n"].grad, "dn")
+    for k in ("w_in", "w_out", "scale_in", "scale_out", "gate", "post_gamma", "next_gamma"):
+        near(block.grads[k], leaves[k].grad, k)
+    with pytest.raises(RuntimeError):
+        block.forward(x.to(DEV), n)
+        block.backward(dr.to(DEV), dn.to(DEV))
+
+
+@gpu
+def test_block_learns():
+    """Straight-through training of the real weights lowers the loss: everything runs together as a program would use it."""
+    g = torch.Generator().manual_seed(0)
+    D, F, M = 64, 128, 256
+    w_in, w_out = (0.1 * torch.randn(2 * F, D, generator=g)).to(DEV), (0.1 * torch.randn(D, F, generator=g)).to(DEV)
+    block = bnn.BinaryFeedForward(w_in, w_out)
+    x = torch.randn(M, D, generator=g).to(DEV)
+    target = torch.tanh(x @ torch.randn(D, D, generator=g).to(DEV) / 8)
+    n = block.first_norm(x)
+    losses = []
+    for _ in range(60):
+        r, after = block.forward(x, n, keep=True)
+        diff = r - x - target
+        losses.append(diff.square().mean().item())
+        block.backward(2 * diff / diff.numel(), torch.zeros_like(after))
+        for w, k in ((w_in, "w_in"), (w_out, "w_out")):
+            w -= 0.02 * block.grads[k] / (block.grads[k].abs().mean() + 1e-12) * w.abs().mean()
+        block.set_weights(w_in, w_out)
+    assert min(losses[-10:]) < 0.8 * losses[0], losses[::10]
+
+
+@gpu
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_a_captured_graph_replays_what_the_calls_compute(M):
+    """Forwards and backwards in one graph, replayed with other inputs in the same buffers, with eager work between."""
+    D, F = 160, 200
+    w_in = torch.randint(-2 ** 31, 2 ** 31 - 1, (2 * F, 5), dtype=torch.int32, device=DEV)
+    w_out = torch.randint(-2 ** 31, 2 ** 31 - 1, (D, 7), dtype=torch.int32, device=DEV)
+    scale = torch.full((2 * F,), 0.08, device=DEV)
+    x = torch.empty(M, D, dtype=torch.bfloat16, device=DEV)
+    h, y, r, n = (torch.empty(M, c, dtype=torch.bfloat16, device=DEV) for c in (F, D, D, D))
+    ws = torch.empty(bnn.gated_bits_backward_workspace(torch.bfloat16, M, F, D), dtype=torch.uint8, device=DEV)
+
+    def work():
+        bnn.gated_bits(x, w_in, scale, out=h)
+        bnn.linear_bits(h, w_out, scale[:D].clone(), residual=x, out=y)
+        bnn.norm_residual(y, x, None, 0.5, bnn.NORM_RMS, None, None, bnn.NORM_LAYER, None, None, 1e-5, M, out=r, out_n=n)
+        got = bnn.gated_bits_backward(h, x, w_in, scale, workspace=ws)
+        return got["dx"], got["dw"], got["dscale"]
+
+    x.normal_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = work()
+    for seed in range(4):
+        torch.manual_seed(seed)
+        x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        have = [t.clone() for t in (h, y, r, n, *captured)]
+        for t in (h, y, r, n):
+            t.zero_()
+        eager = work()
+        torch.cuda.synchronize()
+        for a, b in zip(have, (h, y, r, n, *eager)):
+            assert torch.equal(a, b)
+
+
 # ---- refusals ------------------------------------------------------------------------------------------------------
 
 def test_entry_points_refuse_before_any_launch():
