@@ -118,6 +118,19 @@ struct ProductTile {
     static constexpr int kTerms = is_f32<E> ? 3 : 1;
     // Three buffers let a wavefront run on from step to step, with the barrier in the middle; float32 rows have room for two.
     static constexpr int kBuffers = is_f32<E> && BM > 64 ? 2 : 3;
+    static constexpr int HALVES = kHalves<EPI>, FY = FN / HALVES;
+    struct Loop {
+        typename Vec8<Operand<E>>::type x[kBuffers][kTerms][BM * 8];      // rows of 8 chunks, chunk c of a row at c ^ (row / 2) % 8
+        uint4 w[2][4][CN];           // 512 elements of each weight row, 16 bytes of a row at a time
+    };
+    struct Sums {
+        float4 block[TM * TN][HALVES][32 * 8];      // a wavefront's own: 32 rows of 32 columns, placed like x
+    };
+    union Shared {
+        __device__ Shared() {}
+        Loop loop;
+        Sums sums;
+    };
     static constexpr int kChunks = BM * (kStepK / 8) / kThreads;  // chunks of eight elements that a thread stages
 };
 
@@ -127,8 +140,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
     constexpr bool GATED = S::kGatedForm, BACK = kBackward<EPI>;
-    __shared__ __attribute__((aligned(16))) O8 xs[S::kBuffers][S::kTerms][S::BM * 8];      // rows of 8 chunks, slot = chunk ^ row % 8
-    __shared__ uint4 ws[2][4][S::CN];           // 512 elements of each weight row, 16 bytes of a row at a time
+    __shared__ typename S::Shared shared;
     __shared__ float scale_s[S::CN], bias_s[S::CN];
     __shared__ float sums_s[BACK ? 2 * TM * S::CN : 1];
 
@@ -143,15 +155,6 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     // FN / 2 of the gate's rows, then the same columns of the other half.
     auto block_col = [&](int f) { return n0 + (GATED ? wn * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : (wn * FN + f) * 32); };
     auto block_half = [&](int f) { return GATED && f >= FN / 2 ? 1 : 0; };
-
-    for (int c = tid; c < S::CN; c += S::kThreads) {
-        const int b = c >> 5, w_ = b / FN, f = b % FN;
-        const int col = n0 + (GATED ? w_ * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : b * 32) + (c & 31);
-        const int64_t row = int64_t(GATED && f >= FN / 2 ? a.N : 0) + col;
-        const bool there = col < a.N;
-        scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
-        bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
-    }
 
     constexpr int WQ = 4 * S::CN / S::kThreads;        // 16-byte pieces of weights that a thread stages
     const uint32_t* wrow[WQ];
@@ -172,11 +175,11 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
     };
     auto store_w = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < WQ; ++i) ws[buf][(i * S::kThreads + tid) / S::CN][(i * S::kThreads + tid) % S::CN] = wstage[i];
+        for (int i = 0; i < WQ; ++i) shared.loop.w[buf][(i * S::kThreads + tid) / S::CN][(i * S::kThreads + tid) % S::CN] = wstage[i];
     };
     auto read_w = [&](uint32_t (&w)[FN], int step) {
         const int word = 2 * (step & 7) + fh;
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(&ws[(step >> 3) & 1][word >> 2][(wn * FN) * 32 + consecutive_rows(fr)]) + (word & 3);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(&shared.loop.w[(step >> 3) & 1][word >> 2][(wn * FN) * 32 + consecutive_rows(fr)]) + (word & 3);
 #pragma unroll
         for (int f = 0; f < FN; ++f) w[f] = p[f * 32 * 4];
     };
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
             O8 t[S::kTerms];
             terms_of<E>(stage[i], t);
 #pragma unroll
-            for (int p = 0; p < S::kTerms; ++p) xs[buf][p][row * 8 + slot] = t[p];
+            for (int p = 0; p < S::kTerms; ++p) shared.loop.x[buf][p][row * 8 + slot] = t[p];
         }
     };
 
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 const int row = (wm * FM + j) * 32 + fr;
-                xf[p][j] = xs[buf][p][row * 8 + ((4 * fh + s) ^ ((row >> 1) & 7))];
+                xf[p][j] = shared.loop.x[buf][p][row * 8 + ((4 * fh + s) ^ ((row >> 1) & 7))];
             }
     };
     const Widening<O> minus_weights;
@@ -230,12 +233,23 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
 #pragma unroll
         for (int f = 0; f < FN; ++f) wf[f] = minus_weights(s < 2 ? spread_low(w[f]) : spread_high(w[f]), s & 1);
     };
+    auto load_scales = [&]() {
+        for (int c = tid; c < S::CN; c += S::kThreads) {
+            const int b = c >> 5, w_ = b / FN, f = b % FN;
+            const int col = n0 + (GATED ? w_ * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : b * 32) + (c & 31);
+            const int64_t row = int64_t(GATED && f >= FN / 2 ? a.N : 0) + col;
+            const bool there = col < a.N;
+            scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
+            bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
+        }
+    };
     const int steps = (a.K + kStepK - 1) / kStepK;
     if (steps > 0) {
         uint32_t w[2][FN];                  // of this step and of the next
         O8 xf[2][S::kTerms][FM], wf[2][FN];
         load_w(0);
         load(0);
+        load_scales();                      // while those are on their way
         store_w(0);
         store(0);
         if (steps > 1) load(1);
@@ -291,45 +305,67 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
             }
             buf = next;
         }
+    } else {
+        load_scales();
     }
     __syncthreads();
 
-    // ---- epilogue: lane l has columns 16 fh .. 16 fh + 15 of row fr of each block ----
-    constexpr int HALVES = kHalves<EPI>, FY = FN / HALVES;
+    // ---- epilogue: a block at a time through a piece of LDS of the wavefront's own, so that four lanes have 32 consecutive columns of
+    // a row between them: as the matrix engine leaves them, a store or a load of 1 KB would be 64 pieces of 64 cache lines.
+    constexpr int HALVES = S::HALVES, FY = S::FY;
+    auto& block = shared.sums.block[wave];
+    const int rq = lane >> 2, cq = lane & 3;
 #pragma unroll
-    for (int f = 0; f < FY; ++f)
+    for (int f = 0; f < FY; ++f) {
+        const int c0 = (wn * FN + f) * 32 + 8 * cq;          // its channel; the other half's is 16 FN further
+        const float *scale[HALVES], *bias[HALVES];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int c0 = (wn * FN + f) * 32 + 16 * fh + 8 * g;          // its channel; the other half's is 16 FN further
-            const float *scale[HALVES], *bias[HALVES];
+        for (int h = 0; h < HALVES; ++h) {
+            scale[h] = scale_s + c0 + 16 * FN * h;
+            bias[h] = bias_s + c0 + 16 * FN * h;
+        }
+        float sum_s[HALVES][8] = {}, sum_z[HALVES][8] = {};
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                scale[h] = scale_s + c0 + 16 * FN * h;
-                bias[h] = bias_s + c0 + 16 * FN * h;
-            }
-            float sum_s[HALVES][8] = {}, sum_z[HALVES][8] = {};
+        for (int j = 0; j < FM; ++j) {
 #pragma unroll
-            for (int j = 0; j < FM; ++j) {
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v16f_t& v = acc[f + FY * h][j];
+                    block[h][fr * 8 + ((4 * fh + q) ^ ((fr >> 1) & 7))] = make_float4(-v[4 * q], -v[4 * q + 1], -v[4 * q + 2], -v[4 * q + 3]);
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int row = 16 * half + rq;
                 float sums[HALVES][8];
 #pragma unroll
                 for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sums[h][i] = -acc[f + FY * h][j][8 * g + i];
-                finish<E, EPI, 8>(a, m0 + (wm * FM + j) * 32 + fr, block_col(f) + 16 * fh + 8 * g, sums, scale, bias, sum_s, sum_z);
-            }
-            if constexpr (BACK) {
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float p = sum_of_32(sum_s[h][i]), q = sum_of_32(sum_z[h][i]);
-                        if (fr == 0) {
-                            sums_s[(wm * 2) * S::CN + c0 + 16 * FN * h + i] = p;
-                            sums_s[(wm * 2 + 1) * S::CN + c0 + 16 * FN * h + i] = q;
-                        }
+                    for (int q = 0; q < 2; ++q) {
+                        const float4 v = block[h][row * 8 + ((2 * cq + q) ^ ((row >> 1) & 7))];
+                        sums[h][4 * q] = v.x;
+                        sums[h][4 * q + 1] = v.y;
+                        sums[h][4 * q + 2] = v.z;
+                        sums[h][4 * q + 3] = v.w;
                     }
+                finish<E, EPI, 8>(a, m0 + (wm * FM + j) * 32 + row, block_col(f) + 8 * cq, sums, scale, bias, sum_s, sum_z);
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
+        if constexpr (BACK) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float p = sum_of_every_fourth(sum_s[h][i]), q = sum_of_every_fourth(sum_z[h][i]);
+                    if (rq == 0) {
+                        sums_s[(wm * 2) * S::CN + c0 + 16 * FN * h + i] = p;
+                        sums_s[(wm * 2 + 1) * S::CN + c0 + 16 * FN * h + i] = q;
+                    }
+                }
+        }
+    }
     if constexpr (BACK) {
         __syncthreads();
         for (int c = tid; c < S::CN; c += S::kThreads) {

@@ -210,6 +210,16 @@ __device__ inline float sum_of_32(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// Sum over the lanes that are 4, 8, ... apart, in every one of them.
+__device__ inline float sum_of_every_fourth(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, true));       // row_ror:4
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true));       // row_ror:8
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
 // ---- packed weights as operands of the matrix engine --------------------------------------------------------------
 // A lane takes 32 elements of a row from one word: element e is bit e.  Of 16 bits b, the word y = b | b << 15 has bit 2j
 // at 2j and bit 2j + 1 at 2j + 16, so that one shift brings a pair of elements to the signs of two 16-bit floats, and one
