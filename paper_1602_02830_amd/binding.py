@@ -723,8 +723,14 @@ def gated_bits_backward_workspace(dtype: torch.dtype, M: int, F: int, K: int, ac
     return load_library().bnn_gated_bits_backward_workspace(_real_type(dtype), M, F, K, act)
 
 
-def _bits_backward(name, dy, x, w_bits, cols, scale, bias, act, need_dx, need_dw, workspace):
+def _bits_backward(name, dy, x, w_bits, scale, bias, act, need_dx, need_dw, workspace):
     lib = load_library()
+    if _calls is not None:
+        got = getattr(_calls, name[4:])(dy, x, w_bits, scale, bias, act, need_dx, need_dw, workspace)
+        if got != -1:
+            _check(name, got[0])
+            return {"dx": got[1], "dw": got[2], "dscale": got[3], "dbias": got[4]}
+    cols = _halves(w_bits) if name == "bnn_gated_bits_backward" else w_bits.shape[0]
     _real(x, "x")
     _weights(x, w_bits)
     (M, K), N = x.shape, w_bits.shape[0]
@@ -747,14 +753,14 @@ def linear_bits_backward(dy: torch.Tensor, x: torch.Tensor, w_bits: torch.Tensor
                          workspace: torch.Tensor | None = None) -> dict:
     """bnn_linear_bits_backward: {"dx" [M][K], "dw" [N][K], "dscale" [N], "dbias" [N]}, None for what was not there or not
     wanted.  dw is the gradient of the weights as real numbers; the residual's gradient is dy."""
-    return _bits_backward("bnn_linear_bits_backward", dy, x, w_bits, w_bits.shape[0], scale, bias, act, need_dx, need_dw, workspace)
+    return _bits_backward("bnn_linear_bits_backward", dy, x, w_bits, scale, bias, act, need_dx, need_dw, workspace)
 
 
 def gated_bits_backward(dh: torch.Tensor, x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None,
                         bias: torch.Tensor | None = None, act: int = ACT_SILU, need_dx: bool = True, need_dw: bool = True,
                         workspace: torch.Tensor | None = None) -> dict:
     """bnn_gated_bits_backward: as linear_bits_backward, with dw [2F][K], dscale and dbias [2F]."""
-    return _bits_backward("bnn_gated_bits_backward", dh, x, w_bits, _halves(w_bits), scale, bias, act, need_dx, need_dw, workspace)
+    return _bits_backward("bnn_gated_bits_backward", dh, x, w_bits, scale, bias, act, need_dx, need_dw, workspace)
 
 
 def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Tensor | None = None, res_scale: float = 1.0,
@@ -810,6 +816,13 @@ def norm_residual_backward(dr: torch.Tensor | None, dn: torch.Tensor | None, y: 
     """bnn_norm_residual_backward: {"dx", "dy", "dgate", "dpost_gamma", "dpost_beta", "dpre_gamma", "dpre_beta"}, None for
     what was not there or not wanted, from the gradients dr of r (by every way but n) and dn of n."""
     lib = load_library()
+    if _calls is not None:
+        got = _calls.norm_residual_backward(dr, dn, y, r, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps,
+                                            rows_per_gate, need_dx, workspace)
+        if got != -1:
+            _check("bnn_norm_residual_backward", got[0])
+            return {"dx": got[1], "dy": got[2], "dgate": got[3], "dpost_gamma": got[4], "dpost_beta": got[5], "dpre_gamma": got[6],
+                    "dpre_beta": got[7]}
     _real(y, "y")
     M, D = y.shape
     for t, name in ((dr, "dr"), (dn, "dn"), (r, "r")):

@@ -4,6 +4,7 @@
 //
 //   returns 0    launched
 //   returns > 0  the library's status (nothing launched)
+//   (the backward passes, which allocate what they return: a tuple of the status and the tensors)
 //   returns -1   not a case for this path (another type, a tensor subclass or wrapper, a shape or stride that the
 //                wrapper refuses): nothing was done, and the wrapper's own checks say what is wrong or go the long way
 //
@@ -14,6 +15,7 @@
 // after a call.
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -54,6 +56,17 @@ struct EntryPoints {
     int (*norm_residual)(int, const void*, int64_t, const void*, int64_t, const void*, int64_t, int64_t, float, int, const float*,
                          const float*, int, const float*, const float*, float, void*, int64_t, void*, int64_t, int64_t, int64_t,
                          void*);
+    int64_t (*linear_bits_backward_workspace)(int, int64_t, int64_t, int64_t, int);
+    int64_t (*gated_bits_backward_workspace)(int, int64_t, int64_t, int64_t, int);
+    int (*linear_bits_backward)(int, const void*, int64_t, const void*, int64_t, Words, int64_t, const float*, const float*, int, void*,
+                                int64_t, void*, int64_t, float*, float*, int64_t, int64_t, int64_t, void*, int64_t, void*);
+    int (*gated_bits_backward)(int, const void*, int64_t, const void*, int64_t, Words, int64_t, const float*, const float*, int, void*,
+                               int64_t, void*, int64_t, float*, float*, int64_t, int64_t, int64_t, void*, int64_t, void*);
+    int64_t (*norm_residual_backward_workspace)(int64_t, int64_t, int64_t);
+    int (*norm_residual_backward)(int, const void*, int64_t, const void*, int64_t, const void*, int64_t, const void*, int64_t,
+                                  const void*, int64_t, int64_t, float, int, const float*, const float*, int, const float*, float,
+                                  void*, int64_t, void*, int64_t, void*, int64_t, float*, float*, float*, float*, int64_t, int64_t,
+                                  void*, int64_t, void*);
 };
 
 EntryPoints entry{};
@@ -492,6 +505,142 @@ PyObject* norm_residual(PyObject* const* a) {
     });
 }
 
+// Backward passes: what they return is allocated here, and comes as (status, tensors or None ...).
+
+bool truth(PyObject* o, bool& v) {
+    if (!PyBool_Check(o)) return false;
+    v = o == Py_True;
+    return true;
+}
+
+at::Tensor empty_like(const at::Tensor& t, at::IntArrayRef size, at::ScalarType type) {
+    return at::empty(size, t.options().dtype(type).requires_grad(false));
+}
+
+// The caller's workspace, or one that is made; false where the caller's is none or too small.
+bool workspace_of(PyObject* o, int64_t size, const at::Tensor& like, at::Tensor& ws) {
+    if (size < 0) return false;
+    if (o == Py_None) {
+        ws = empty_like(like, {size}, at::kByte);
+        return true;
+    }
+    const at::Tensor* t = plain(o, at::kByte);
+    if (!t || !t->is_contiguous() || t->get_device() != like.get_device() || t->numel() < size) return false;
+    ws = *t;
+    return true;
+}
+
+template <size_t N>
+PyObject* results(int status, const at::Tensor (&t)[N]) {
+    PyObject* r = PyTuple_New(N + 1);
+    if (!r) return nullptr;
+    PyObject* s = PyLong_FromLong(status);
+    if (!s) {
+        Py_DECREF(r);
+        return nullptr;
+    }
+    PyTuple_SET_ITEM(r, 0, s);
+    for (size_t i = 0; i < N; ++i) {
+        PyObject* v = nullptr;
+        if (t[i].defined()) {
+            v = THPVariable_Wrap(t[i]);
+        } else {
+            v = Py_None;
+            Py_INCREF(v);
+        }
+        if (!v) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(r, i + 1, v);
+    }
+    return r;
+}
+
+// Calls the library without the interpreter lock.
+template <typename F>
+bool run(const at::Tensor& t, int& status, F&& call) {
+    void* stream;
+    if (!stream_of(t, stream)) return false;
+    Py_BEGIN_ALLOW_THREADS
+    status = call(stream);
+    Py_END_ALLOW_THREADS
+    return true;
+}
+
+void* data_of(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// (dy, x, w_bits, scale, bias, act, need_dx, need_dw, workspace) -> (status, dx, dw, dscale, dbias)
+template <bool GATED>
+PyObject* product_backward(PyObject* const* a) {
+    Weighted p;
+    Matrix dy;
+    int act;
+    bool need_dx, need_dw;
+    if (!p.read(a + 1) || (GATED && p.w.rows % 2 != 0) || !small_integer(a[5], act) || !truth(a[6], need_dx) || !truth(a[7], need_dw))
+        return long_way();
+    const int64_t M = p.x.rows, K = p.x.cols, N = p.w.rows, cols = GATED ? N / 2 : N;
+    if (!read_real(a[0], dy, p.x.t, M, cols)) return long_way();
+    at::Tensor ws, out[4];
+    const int64_t size = (GATED ? entry.gated_bits_backward_workspace : entry.linear_bits_backward_workspace)(p.type, M, cols, K, act);
+    if (!workspace_of(a[8], size, *p.x.t, ws)) return long_way();
+    const at::ScalarType type = p.x.t->scalar_type();
+    if (need_dx) out[0] = empty_like(*p.x.t, {M, K}, type);
+    if (need_dw) out[1] = empty_like(*p.x.t, {N, K}, type);
+    if (p.scale) out[2] = empty_like(*p.x.t, {N}, at::kFloat);
+    if (p.bias) out[3] = empty_like(*p.x.t, {N}, at::kFloat);
+    int status;
+    if (!run(*p.x.t, status, [&](void* s) {
+            return (GATED ? entry.gated_bits_backward : entry.linear_bits_backward)(
+                p.type, dy.data, dy.ld, p.x.data, p.x.ld, p.w.as<uint32_t>(), p.w.ld, p.scale, p.bias, act, data_of(out[0]), K,
+                data_of(out[1]), K, static_cast<float*>(data_of(out[2])), static_cast<float*>(data_of(out[3])), M, cols, K,
+                ws.data_ptr(), ws.numel(), s);
+        }))
+        return nullptr;
+    return results(status, out);
+}
+PyObject* linear_bits_backward(PyObject* const* a) { return product_backward<false>(a); }
+PyObject* gated_bits_backward(PyObject* const* a) { return product_backward<true>(a); }
+
+// (dr, dn, y, r, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, need_dx, workspace)
+//   -> (status, dx, dy, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)
+PyObject* norm_residual_backward(PyObject* const* a) {
+    Matrix dr, dn, y, r, gate;
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+    float res_scale, eps;
+    int post, pre;
+    int64_t R;
+    bool need_dx;
+    if (!read_real(a[2], y, nullptr, 0, 0) || !real_number(a[5], res_scale) || !small_integer(a[6], post) || !small_integer(a[9], pre) ||
+        !real_number(a[12], eps) || !integer(a[13], R) || R < 1 || !truth(a[14], need_dx))
+        return long_way();
+    const int64_t M = y.rows, D = y.cols;
+    auto optional = [&](PyObject* o, Matrix& m, int64_t rows) { return o == Py_None || read_real(o, m, y.t, rows, D); };
+    if (!optional(a[0], dr, M) || !optional(a[1], dn, M) || !optional(a[3], r, M) || !optional(a[4], gate, M / R + (M % R != 0)) ||
+        (pre == 0 ? a[1] != Py_None : a[1] == Py_None || a[3] == Py_None) || !read_vector(a[7], D, *y.t, post_gamma) ||
+        !read_vector(a[8], D, *y.t, post_beta) || !read_vector(a[10], D, *y.t, pre_gamma) || !read_vector(a[11], D, *y.t, pre_beta))
+        return long_way();
+    at::Tensor ws, out[7];
+    if (!workspace_of(a[15], entry.norm_residual_backward_workspace(M, D, R), *y.t, ws)) return long_way();
+    const at::ScalarType type = y.t->scalar_type();
+    if (need_dx) out[0] = empty_like(*y.t, {M, D}, type);
+    out[1] = empty_like(*y.t, {M, D}, type);
+    if (gate.t) out[2] = empty_like(*y.t, {gate.rows, D}, type);
+    const float* const vectors[4] = {post_gamma, post_beta, pre_gamma, pre_beta};
+    for (int i = 0; i < 4; ++i)
+        if (vectors[i]) out[3 + i] = empty_like(*y.t, {D}, at::kFloat);
+    int status;
+    if (!run(*y.t, status, [&](void* s) {
+            return entry.norm_residual_backward(
+                real_type(type), dr.data, dr.ld, dn.data, dn.ld, y.data, y.ld, r.data, r.ld, gate.data, gate.ld, R, res_scale, post,
+                post_gamma, post_beta, pre, pre_gamma, eps, data_of(out[0]), D, data_of(out[1]), D, data_of(out[2]), D,
+                static_cast<float*>(data_of(out[3])), static_cast<float*>(data_of(out[4])), static_cast<float*>(data_of(out[5])),
+                static_cast<float*>(data_of(out[6])), M, D, ws.data_ptr(), ws.numel(), s);
+        }))
+        return nullptr;
+    return results(status, out);
+}
+
 // bind({"bnn_pack_sign": address, ...}, raw_stream)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *table, *stream;
@@ -523,6 +672,12 @@ PyObject* bind(PyObject*, PyObject* args) {
     set(e.linear_bits, "bnn_linear_bits");
     set(e.gated_bits, "bnn_gated_bits");
     set(e.norm_residual, "bnn_norm_residual");
+    set(e.linear_bits_backward_workspace, "bnn_linear_bits_backward_workspace");
+    set(e.gated_bits_backward_workspace, "bnn_gated_bits_backward_workspace");
+    set(e.linear_bits_backward, "bnn_linear_bits_backward");
+    set(e.gated_bits_backward, "bnn_gated_bits_backward");
+    set(e.norm_residual_backward_workspace, "bnn_norm_residual_backward_workspace");
+    set(e.norm_residual_backward, "bnn_norm_residual_backward");
     if (!ok || !PyCallable_Check(stream)) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point or the stream function is missing");
         return nullptr;
@@ -558,6 +713,9 @@ PyMethodDef methods[] = {
     fast<linear_bits, 7>("linear_bits"),
     fast<gated_bits, 6>("gated_bits"),
     fast<norm_residual, 14>("norm_residual"),
+    fast<linear_bits_backward, 9>("linear_bits_backward"),
+    fast<gated_bits_backward, 9>("gated_bits_backward"),
+    fast<norm_residual_backward, 16>("norm_residual_backward"),
     {nullptr, nullptr, 0, nullptr},
 };
 
