@@ -75,12 +75,6 @@ __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t
         if (bn * 512 + i < N) part[int64_t(bm) * N + bn * 512 + i] = sums_s[0][i] + sums_s[1][i] + sums_s[2][i] + sums_s[3][i];
 }
 
-int join_tiles(const float* part, int64_t tiles, int64_t N, float* out, hipStream_t s) {
-    JoinArgs a{};
-    a.part = part; a.out[0] = out; a.per_group = int(tiles); a.N = int(N);
-    return join_sums<float>(a, 1, 1, s);
-}
-
 // ---- the plan ----------------------------------------------------------------------------------------------------
 
 constexpr int kStrips = 256;       // strips of rows for the column sums without a product
@@ -150,9 +144,9 @@ int launch_grad(WeightGradArgs a, hipStream_t s) {
     return check_launch();
 }
 
-// dw and, where a.w is given, dscale; part: room for the column sums of the tiles.
+// dw and, where a.w is given, dscale, or its parts (in `part`), which are then among what is to be joined.
 template <typename E>
-int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* part, float* dscale, hipStream_t s) {
+int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* part, float* dscale, JoinArgs& join, hipStream_t s) {
     a.splits = g.splits;
     a.split_rows = g.split_rows;
     a.pieces = g.splits > 1 ? pieces : nullptr;
@@ -167,7 +161,8 @@ int weight_gradient(const GradPlan& g, WeightGradArgs a, float* pieces, float* p
         join_pieces_kernel<E><<<dim3(uint32_t(a.channels)), dim3(256), 0, s>>>(a, dscale);
         return check_launch();
     }
-    return a.w ? join_tiles(part, ceil_div(a.K, g.tile), a.channels, dscale, s) : BNN_OK;
+    if (a.w) join.add(part, ceil_div(a.K, g.tile), dscale);
+    return BNN_OK;
 }
 
 template <typename E>
@@ -180,6 +175,8 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
     float* const part_bias = reinterpret_cast<float*>(ws + p.bias_at);
     const int64_t channels = p.halves * cols;
     int st = BNN_OK;
+    JoinArgs join{};
+    join.N = int(channels);
     const void* g = ds;                // what dx is made of
     int64_t ld_g = p.ds_cols, cols_g = p.ds_cols, part_rows = p.part_rows;
     if (p.recompute && M > 0 && cols > 0) {
@@ -230,19 +227,12 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w;
         a.M = int(M); a.K = int(K); a.cols = int(p.recompute ? p.ds_cols : cols); a.half = int(p.half); a.F = int(cols);
         a.channels = int(channels);
-        if ((st = weight_gradient<E>(p.grad, a, reinterpret_cast<float*>(ws + p.pieces_at), part_scale, dscale, s)) != BNN_OK) return st;
+        if ((st = weight_gradient<E>(p.grad, a, reinterpret_cast<float*>(ws + p.pieces_at), part_scale, dscale, join, s)) != BNN_OK)
+            return st;
     }
-    if (channels == 0) return BNN_OK;
-    if (p.recompute && dscale && dbias) {
-        JoinArgs a{};
-        a.part = part_scale; a.part_step = part_bias - part_scale; a.out[0] = dscale; a.out[1] = dbias;
-        a.per_group = int(part_rows); a.N = int(channels);
-        return join_sums<float>(a, 1, 2, s);
-    }
-    if (dscale && (p.recompute || K == 0)) {
-        if ((st = join_tiles(part_scale, p.recompute ? part_rows : 0, channels, dscale, s)) != BNN_OK) return st;
-    }
-    return dbias ? join_tiles(part_bias, part_rows, channels, dbias, s) : BNN_OK;
+    if (dscale && (p.recompute || K == 0)) join.add(part_scale, p.recompute ? part_rows : 0, dscale);
+    if (dbias) join.add(part_bias, part_rows, dbias);
+    return join_sums<E>(join, s);
 }
 
 // Sizes that a call takes; BNN_OK or what it answers.

@@ -1,8 +1,9 @@
 // The second half of a sum over rows: what workgroups have summed over their rows each, joined in a fixed order.
 //
-// parts of N sums each; out[g][n] = sum over the parts g * per_group .. of part[n].  A workgroup takes 32 columns, with 32 threads
-// for each, every one of them 1/32 of the parts, eight loads at a time: with four threads a column, one load at a time, joining
-// 512 parts of 4096 columns took longer than what they came from.
+// A vector is the sum of its `parts` sums of N columns; beside vectors there may be one matrix, whose row g is the sum of its
+// parts g * per_group to (g + 1) * per_group.  One launch for all of them.  A workgroup of 1024 threads takes `cols` columns of a
+// vector or of a row, and each thread of a column its share of the parts, eight loads at a time: with four threads a column and one
+// load at a time, joining 512 parts of 4096 columns took longer than what they came from.
 #pragma once
 
 #include "real_types.h"
@@ -10,48 +11,67 @@
 namespace bnn {
 
 constexpr int kMostJoined = 4;          // vectors of one launch
+constexpr int kJoinThreads = 1024;
 
 struct JoinArgs {
-    const float* part;
-    int64_t part_step;                  // from the first vector's parts to the next one's
-    int64_t ld_out;                     // from group to group
-    void* out[kMostJoined];
-    int per_group, N, blocks_n;
+    const float* part[kMostJoined];     // [parts][N]
+    float* out[kMostJoined];
+    int parts[kMostJoined];
+    const float* group_part;            // [groups][per_group][N]
+    void* out_groups;                   // [groups][ld_out]
+    int64_t ld_out;
+    int vectors, groups, per_group, N, cols, group_cols;      // cols: powers of two
+    inline void add(const float* sums, int64_t count, float* to) {
+        part[vectors] = sums;
+        parts[vectors] = int(count);
+        out[vectors++] = to;
+    }
 };
 
 template <typename E>
-__global__ __launch_bounds__(1024) void join_sums_kernel(const JoinArgs a) {
-    __shared__ float sums_s[32][33];
-    const int c = threadIdx.x & 31, q = threadIdx.x >> 5;
-    const int64_t group = blockIdx.x / uint32_t(a.blocks_n);
-    const int n = (int(blockIdx.x) - int(group) * a.blocks_n) * 32 + c;
-    const float* const part = a.part + blockIdx.y * a.part_step + group * a.per_group * a.N + min(n, a.N - 1);
+__global__ __launch_bounds__(kJoinThreads) void join_sums_kernel(const JoinArgs a) {
+    __shared__ float sums_s[kJoinThreads];
+    const int of_vectors = a.vectors * ((a.N + a.cols - 1) / a.cols);
+    const bool matrix = int(blockIdx.x) >= of_vectors;
+    const int cols = matrix ? a.group_cols : a.cols, blocks_n = (a.N + cols - 1) / cols, step = kJoinThreads / cols;
+    const int block = int(blockIdx.x) - (matrix ? of_vectors : 0), row = block / blocks_n;
+    const int c = threadIdx.x & (cols - 1), n = (block - row * blocks_n) * cols + c;
+    const int parts = matrix ? a.per_group : a.parts[row];
+    const float* const part = (matrix ? a.group_part + int64_t(row) * parts * a.N : a.part[row]) + min(n, a.N - 1);
     float s = 0.0f;
-    int t = q;
-    for (; t + 7 * 32 < a.per_group; t += 8 * 32) {
+    int t = threadIdx.x / uint32_t(cols);
+    for (; t + 7 * step < parts; t += 8 * step) {
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = part[int64_t(t + 32 * i) * a.N];
+        for (int i = 0; i < 8; ++i) v[i] = part[int64_t(t + step * i) * a.N];
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += v[i];
     }
-    for (; t < a.per_group; t += 32) s += part[int64_t(t) * a.N];
-    sums_s[q][c] = s;
+    for (; t < parts; t += step) s += part[int64_t(t) * a.N];
+    // The threads of a column in a wavefront, then its wavefronts.
+    for (int off = 32; off >= cols; off >>= 1) s += __shfl_xor(s, off);
+    const int lanes = min(cols, 64);
+    if ((threadIdx.x & 63) < lanes) sums_s[(threadIdx.x >> 6) * lanes + (threadIdx.x & 63)] = s;
     __syncthreads();
-    // Each half wavefront joins one column.
-    s = sums_s[c][q];
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor(s, off);
-    const int m = (int(blockIdx.x) - int(group) * a.blocks_n) * 32 + q;
-    if (c == 0 && m < a.N) static_cast<E*>(a.out[blockIdx.y])[group * a.ld_out + m] = E(s);
+    if (threadIdx.x >= cols || n >= a.N) return;
+    s = 0.0f;
+    for (int w = c; w < kJoinThreads / 64 * lanes; w += cols) s += sums_s[w];
+    if (matrix) static_cast<E*>(a.out_groups)[row * a.ld_out + n] = E(s);
+    else a.out[row][n] = s;
 }
 
-// groups * per_group parts; `vectors` of them, each with parts of its own.
+// E: the type of out_groups.
 template <typename E>
-inline int join_sums(JoinArgs a, int64_t groups, int vectors, hipStream_t s) {
-    a.blocks_n = int(ceil_div(a.N, 32));
-    if (groups * a.blocks_n > max_blocks(1024)) return BNN_ERR_UNSUPPORTED;
-    join_sums_kernel<E><<<dim3(uint32_t(groups * a.blocks_n), uint32_t(vectors)), dim3(1024), 0, s>>>(a);
+inline int join_sums(JoinArgs a, hipStream_t s) {
+    if (a.N == 0) return BNN_OK;
+    // 32 columns a workgroup, fewer where that leaves most of the chip idle (three vectors of 300 columns, 3750 parts each: 30
+    // workgroups 11.7 us, 114 of them 5.5), more where a column has only a few parts.
+    a.cols = (a.vectors + a.groups) * ceil_div(a.N, 32) >= 128 ? 32 : 8;
+    a.group_cols = a.per_group <= 32 ? 256 : a.cols;
+    const int64_t blocks = a.vectors * ceil_div(a.N, a.cols) + a.groups * ceil_div(a.N, a.group_cols);
+    if (blocks > max_blocks(kJoinThreads)) return BNN_ERR_UNSUPPORTED;
+    if (blocks == 0) return BNN_OK;
+    join_sums_kernel<E><<<dim3(uint32_t(blocks)), dim3(kJoinThreads), 0, s>>>(a);
     return check_launch();
 }
 

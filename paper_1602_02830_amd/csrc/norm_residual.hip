@@ -1,13 +1,21 @@
 // What stands between two blocks, forwards and backwards: the norm after a block, its gate and residual scale, the sum with
 // the stream and the norm before the next block (bnn_norm_residual, bnn_norm_residual_backward).
 //
-// Both are bound by memory: every matrix is read or written once.  A workgroup holds a whole row in registers (8 or 16
-// elements a thread, 64 to 1024 threads by the row's length), so that the statistics of y, the new stream r and the
-// statistics of r need nothing but two to four sums over the workgroup.  Variances are sums of squared distances from the
-// mean, taken after it.  Workgroups walk over rows, the next row's loads on their way while one is worked on, with the gammas and
-// betas in registers: read for every row, these 32-bit vectors were as much traffic to the caches as a row of 16-bit elements.
-// Backwards a workgroup walks a strip of rows and keeps the sums over rows (of the gammas, betas and the gate) in registers;
-// strips' sums are joined by a second launch in a fixed order.
+// Both are bound by memory: every matrix is read or written once.  A workgroup holds a whole row in registers (16 elements a
+// thread), so that the statistics of y, the new stream r and the statistics of r need nothing but two to four sums over the
+// workgroup.  Variances are sums of squared distances from the mean, taken after it.  Workgroups walk over rows, the next row's loads
+// on their way while one is worked on.  With 8 elements a thread and twice the wavefronts at each barrier the same rows took longer
+// (10000 x 2049 float32 backwards: 155 us against 125), with 4 longer still.
+//
+// Forwards the gammas and betas stay in registers: read for every row, these 32-bit vectors were as much traffic to the caches as
+// a row of 16-bit elements.  16384 x 4096 bfloat16, root-mean-square norms and a gate: 114 us, 4.7 TB/s, as fast as a large copy.
+//
+// Backwards y and r are both at hand from the start, and their norms share their sums; then follow one pair of sums for the
+// gradient of each norm.  A workgroup walks a strip of rows and keeps the sums over rows (of the gammas, betas and the gate) in
+// registers, the gammas and the beta in LDS; strips' sums are joined by a second launch in a fixed order.  16384 x 4096 bfloat16:
+// 178 us, 4.5 TB/s; 10000 x 2049 float32 with layer norms and all their gradients 178 us, 2.8 TB/s, where the sums over rows and
+// three elements in four of 3 wavefronts' lanes are what costs.  Rows past 8192 elements do not fit the registers (4000 x 16000
+// bfloat16: 552 us, 1.4 TB/s; forwards 118 us).
 #include "join_sums.h"
 
 namespace bnn {
@@ -23,115 +31,166 @@ __device__ inline float sum_of_wave(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// Sums of a and of b over the workgroup of up to WAVES wavefronts, the same in every thread.  Two buffers in turn: a thread writes
+// one again only after the barrier of the sum between, by which everyone has read it.
 template <int WAVES>
 struct Sums {
-    float* lds;              // [2][WAVES][2]
-    int turn;
-    // Sums of a and of b over the workgroup, the same in every thread.  Two buffers in turn: a thread writes one again
-    // only after the barrier of the sum between, by which everyone has read it.
+    float2* lds;             // [2][WAVES]; zero where there is no such wavefront
+    int turn = 0;
+    __device__ inline explicit Sums(float2* p) : lds(p) {
+        if constexpr (WAVES > 1) {
+            if (threadIdx.x < 2 * WAVES) lds[threadIdx.x] = make_float2(0.0f, 0.0f);
+            __syncthreads();
+        }
+    }
     __device__ inline float2 operator()(float a, float b) {
         a = sum_of_wave(a);
         b = sum_of_wave(b);
         if constexpr (WAVES > 1) {
-            float* p = lds + turn * 2 * WAVES;
+            float2* const p = lds + turn * WAVES;
             turn ^= 1;
-            if ((threadIdx.x & 63) == 0) {
-                p[2 * (threadIdx.x >> 6)] = a;
-                p[2 * (threadIdx.x >> 6) + 1] = b;
-            }
+            if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = make_float2(a, b);
             __syncthreads();
             a = b = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                a += p[2 * w];
-                b += p[2 * w + 1];
+                a += p[w].x;
+                b += p[w].y;
             }
         }
         return make_float2(a, b);
     }
 };
 
-// Columns of chunk `i` of a thread.
-template <int WAVES>
-__device__ inline int first_col(int i) {
-    return (i * 64 * WAVES + int(threadIdx.x)) * 8;
+// A row's layout over a workgroup: CH groups of G elements a thread, in a workgroup of no more wavefronts than the row needs (WAVES
+// at most).  Group i of a thread begins with column first_col(i).
+template <int W, int GROUP, int GROUPS, bool IS_SHORT>
+struct Layout {
+    static constexpr int WAVES = W, G = GROUP, CH = GROUPS;
+    static constexpr bool SHORT = IS_SHORT;      // rows of fewer than G elements
+    static constexpr bool FULL = W == 1 || (W == 16);
+    static inline int threads(int64_t D) { return FULL ? 64 * W : 64 * int(ceil_div(D, 64 * G * CH)); }
+    __device__ static inline int first_col(int i) { return (i * (FULL ? 64 * W : int(blockDim.x)) + int(threadIdx.x)) * G; }
+};
+
+template <typename L>
+using Values = float[L::CH][L::G];
+
+template <typename L, typename F>
+__device__ inline void each(F&& f) {
+#pragma unroll
+    for (int i = 0; i < L::CH; ++i)
+#pragma unroll
+        for (int e = 0; e < L::G; ++e) f(i, e);
 }
 
-// A row's part of this thread, as it lies in memory: element e of chunk i is column first_col(i) + e.  Loads ask no questions, so
-// that the compiler knows how many are on their way: what lies past the row's end is loaded from its last eight elements (SHORT: rows
-// of fewer than eight, an element at a time), and put right by `widened`.
-template <typename E, int WAVES, int CH>
+// A row's part of this thread, as it lies in memory.  Loads ask no questions, so that the compiler knows how many are on their way:
+// what lies past the row's end is loaded from its last group (SHORT: an element at a time), and put right by `widened`.
+template <typename E, typename L>
 struct Row {
-    typename Vec8<E>::type v[CH];
-    template <bool SHORT>
+    typename Group<E, L::G>::type v[L::CH];
     __device__ inline void load(const void* matrix, int64_t m, int64_t ld, int D) {
         const E* const row = static_cast<const E*>(matrix) + m * ld;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int c = first_col<WAVES>(i);
-            if constexpr (SHORT) v[i] = load8<E>(row + c, D - c);
-            else v[i] = *reinterpret_cast<const typename Vec8<E>::any*>(row + min(c, D - 8));
+        for (int i = 0; i < L::CH; ++i) {
+            const int c = L::first_col(i);
+            if constexpr (L::SHORT) v[i] = load_group<E, L::G>(row + c, D - c);
+            else v[i] = *reinterpret_cast<const typename Group<E, L::G>::any*>(row + min(c, D - L::G));
         }
     }
     // As floats, zero past the row's end.
-    template <bool SHORT>
-    __device__ inline void widened(int D, float (&to)[CH][8]) const {
+    __device__ inline void widened(int D, Values<L>& to) const {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int c = first_col<WAVES>(i);
-            typename Vec8<E>::type q = v[i];
-            // The wavefront's last chunk lies past the row's end: some of them have to be moved.
-            if (!SHORT && __builtin_amdgcn_readfirstlane(c) + 512 > D) q = row_end<E>(q, D - c);
+        for (int i = 0; i < L::CH; ++i) {
+            const int c = L::first_col(i);
+            typename Group<E, L::G>::type q = v[i];
+            // The wavefront's last group lies past the row's end: some of them have to be moved.
+            if (!L::SHORT && __builtin_amdgcn_readfirstlane(c) + 64 * L::G > D) q = row_end<E, L::G>(q, D - c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) to[i][e] = float(q[e]);
+            for (int e = 0; e < L::G; ++e) to[i][e] = float(q[e]);
         }
     }
 };
 
-template <int WAVES, int CH, bool SHORT>
-__device__ inline void load_vector(const float* p, int D, float otherwise, float (&v)[CH][8]) {
-    if (!p) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = otherwise;
-        return;
-    }
-    Row<float, WAVES, CH> row;
-    row.template load<SHORT>(p, 0, 0, D);
-    row.template widened<SHORT>(D, v);
+template <typename L>
+__device__ inline void load_vector(const float* p, int D, float otherwise, Values<L>& v) {
+    if (!p) return each<L>([&](int i, int e) { v[i][e] = otherwise; });
+    Row<float, L> row;
+    row.load(p, 0, 0, D);
+    row.widened(D, v);
 }
 
-template <typename E, int WAVES, int CH>
-__device__ inline void store_row(E* row, int D, const float (&v)[CH][8]) {
+template <typename E, typename L>
+__device__ inline void store_row(E* row, int D, const Values<L>& v) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int c = first_col<WAVES>(i);
-        if (c < D) store8<E>(row + c, v[i], D - c);
+    for (int i = 0; i < L::CH; ++i) {
+        const int c = L::first_col(i);
+        if (c < D) store_group<E, L::G>(row + c, v[i], D - c);
     }
 }
 
-template <int CH, typename F>
-__device__ inline void each(F&& f) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f(i, e);
-}
-
-// v -> (v - mean) / sqrt(var + eps), or v / sqrt(mean(v^2) + eps); returns the factor.  Elements past the row's end stay zero.
-template <int WAVES, int CH>
-__device__ inline float normalise(int kind, float (&v)[CH][8], int D, float eps, Sums<WAVES>& sums) {
-    if (kind == BNN_NORM_LAYER) {
-        float s = 0.0f;
-        each<CH>([&](int i, int e) { s += v[i][e]; });
-        const float mean = sums(s, 0.0f).x / float(D);
-        each<CH>([&](int i, int e) { v[i][e] = first_col<WAVES>(i) + e < D ? v[i][e] - mean : 0.0f; });
-    }
+template <typename L>
+__device__ inline float sum_of(const Values<L>& v) {
     float s = 0.0f;
-    each<CH>([&](int i, int e) { s = fmaf(v[i][e], v[i][e], s); });
-    const float inv = 1.0f / sqrtf(sums(s, 0.0f).x / float(D) + eps);
-    each<CH>([&](int i, int e) { v[i][e] *= inv; });
+    each<L>([&](int i, int e) { s += v[i][e]; });
+    return s;
+}
+
+template <typename L>
+__device__ inline float sum_of_squares(const Values<L>& v) {
+    float s = 0.0f;
+    each<L>([&](int i, int e) { s = fmaf(v[i][e], v[i][e], s); });
+    return s;
+}
+
+// Elements past the row's end are, and stay, zero.
+template <typename L>
+__device__ inline void trim(Values<L>& v, int D) {
+#pragma unroll
+    for (int i = 0; i < L::CH; ++i) {
+        const int c = L::first_col(i);
+        if (__builtin_amdgcn_readfirstlane(c) + 64 * L::G <= D) continue;      // for a whole wavefront
+#pragma unroll
+        for (int e = 0; e < L::G; ++e) v[i][e] = c + e < D ? v[i][e] : 0.0f;
+    }
+}
+
+template <typename L>
+__device__ inline void take_off(float mean, Values<L>& v, int D) {
+    each<L>([&](int i, int e) { v[i][e] -= mean; });
+    trim<L>(v, D);
+}
+
+__device__ inline float one_over_root(float squares, int D, float eps) { return 1.0f / sqrtf(squares / float(D) + eps); }
+
+// v -> (v - mean) / sqrt(var + eps), or v / sqrt(mean(v^2) + eps).
+template <typename L>
+__device__ inline void normalise(int kind, Values<L>& v, int D, float eps, Sums<L::WAVES>& sums) {
+    if (kind == BNN_NORM_LAYER) take_off<L>(sums(sum_of<L>(v), 0.0f).x / float(D), v, D);
+    const float inv = one_over_root(sums(sum_of_squares<L>(v), 0.0f).x, D, eps);
+    each<L>([&](int i, int e) { v[i][e] *= inv; });
+}
+
+// Two rows at once, for as many sums as one of them takes (kind BNN_NORM_NONE: left as it is); returns the factors.
+template <typename L>
+__device__ inline float2 normalise_both(int kind_a, Values<L>& a, int kind_b, Values<L>& b, int D, float eps, Sums<L::WAVES>& sums) {
+    float2 inv = make_float2(1.0f, 1.0f);
+    if (kind_a == BNN_NORM_LAYER || kind_b == BNN_NORM_LAYER) {
+        const float2 s = sums(sum_of<L>(a), sum_of<L>(b));
+        if (kind_a == BNN_NORM_LAYER) take_off<L>(s.x / float(D), a, D);
+        if (kind_b == BNN_NORM_LAYER) take_off<L>(s.y / float(D), b, D);
+    }
+    if (kind_a != BNN_NORM_NONE || kind_b != BNN_NORM_NONE) {
+        const float2 s = sums(sum_of_squares<L>(a), sum_of_squares<L>(b));
+        if (kind_a != BNN_NORM_NONE) {
+            inv.x = one_over_root(s.x, D, eps);
+            each<L>([&](int i, int e) { a[i][e] *= inv.x; });
+        }
+        if (kind_b != BNN_NORM_NONE) {
+            inv.y = one_over_root(s.y, D, eps);
+            each<L>([&](int i, int e) { b[i][e] *= inv.y; });
+        }
+    }
     return inv;
 }
 
@@ -145,54 +204,53 @@ struct NormArgs {
 };
 
 // BETAS: a norm has one.
-template <typename E, int WAVES, int CH, bool BETAS, bool SHORT>
-__global__ __launch_bounds__(64 * WAVES) void norm_residual_kernel(const NormArgs a) {
-    __shared__ float sums_s[4 * WAVES];
-    Sums<WAVES> sums{sums_s, 0};
+template <typename E, typename L, bool BETAS>
+__global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const NormArgs a) {
+    __shared__ float2 sums_s[2 * L::WAVES];
+    Sums<L::WAVES> sums(sums_s);
     const int D = a.D;
-    float post_g[CH][8], pre_g[CH][8], post_b[BETAS ? CH : 1][8], pre_b[BETAS ? CH : 1][8];
-    Row<E, WAVES, CH> y, x, gate;
+    Values<L> post_g, pre_g, post_b, pre_b;
+    Row<E, L> y, x, gate;
     int64_t m = blockIdx.x, gate_row = m / a.rows_per_gate;
-    y.template load<SHORT>(a.y, m, a.ld_y, D);
-    if (a.x) x.template load<SHORT>(a.x, m, a.ld_x, D);
-    if (a.gate) gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
-    load_vector<WAVES, CH, SHORT>(a.post_gamma, D, 1.0f, post_g);
-    load_vector<WAVES, CH, SHORT>(a.pre_gamma, D, 1.0f, pre_g);
+    y.load(a.y, m, a.ld_y, D);
+    if (a.x) x.load(a.x, m, a.ld_x, D);
+    if (a.gate) gate.load(a.gate, gate_row, a.ld_gate, D);
+    load_vector<L>(a.post_gamma, D, 1.0f, post_g);
+    load_vector<L>(a.pre_gamma, D, 1.0f, pre_g);
     if constexpr (BETAS) {
-        load_vector<WAVES, CH, SHORT>(a.post_beta, D, 0.0f, post_b);
-        load_vector<WAVES, CH, SHORT>(a.pre_beta, D, 0.0f, pre_b);
+        load_vector<L>(a.post_beta, D, 0.0f, post_b);
+        load_vector<L>(a.pre_beta, D, 0.0f, pre_b);
     }
     for (; m < a.M; m += gridDim.x) {
-        float v[CH][8], xv[CH][8], g[CH][8];
-        y.template widened<SHORT>(D, v);
-        if (a.x) x.template widened<SHORT>(D, xv);
-        if (a.gate) gate.template widened<SHORT>(D, g);
+        Values<L> v, xv, g;
+        y.widened(D, v);
+        if (a.x) x.widened(D, xv);
+        if (a.gate) gate.widened(D, g);
         // The next row, or the last one again.
         const int64_t next = min(m + int64_t(gridDim.x), int64_t(a.M) - 1);
-        y.template load<SHORT>(a.y, next, a.ld_y, D);
-        if (a.x) x.template load<SHORT>(a.x, next, a.ld_x, D);
+        y.load(a.y, next, a.ld_y, D);
+        if (a.x) x.load(a.x, next, a.ld_x, D);
         if (a.gate && (gate_row + 1) * a.rows_per_gate <= next) {
             gate_row = next / a.rows_per_gate;
-            gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
+            gate.load(a.gate, gate_row, a.ld_gate, D);
         }
         if (a.post != BNN_NORM_NONE) {
-            normalise<WAVES, CH>(a.post, v, D, a.eps, sums);
-            each<CH>([&](int i, int e) { v[i][e] *= post_g[i][e]; });
-            if constexpr (BETAS) each<CH>([&](int i, int e) { v[i][e] += post_b[i][e]; });
+            normalise<L>(a.post, v, D, a.eps, sums);
+            each<L>([&](int i, int e) { v[i][e] *= post_g[i][e]; });
+            if constexpr (BETAS) each<L>([&](int i, int e) { v[i][e] += post_b[i][e]; });
         }
-        each<CH>([&](int i, int e) {
+        each<L>([&](int i, int e) {
             float t = v[i][e] * a.res_scale;
             if (a.gate) t *= g[i][e];
             v[i][e] = a.x ? xv[i][e] + t : t;
-            // 0 * inf of a scale that is none must not reach the sums from columns that are not there.
-            if (first_col<WAVES>(i) + e >= D) v[i][e] = 0.0f;
         });
-        if (a.r) store_row<E, WAVES, CH>(static_cast<E*>(a.r) + m * a.ld_r, D, v);
+        trim<L>(v, D);           // 0 * inf of a scale that is none must not reach the sums from columns that are not there
+        if (a.r) store_row<E, L>(static_cast<E*>(a.r) + m * a.ld_r, D, v);
         if (a.pre != BNN_NORM_NONE) {
-            normalise<WAVES, CH>(a.pre, v, D, a.eps, sums);
-            each<CH>([&](int i, int e) { v[i][e] *= pre_g[i][e]; });
-            if constexpr (BETAS) each<CH>([&](int i, int e) { v[i][e] += pre_b[i][e]; });
-            store_row<E, WAVES, CH>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
+            normalise<L>(a.pre, v, D, a.eps, sums);
+            each<L>([&](int i, int e) { v[i][e] *= pre_g[i][e]; });
+            if constexpr (BETAS) each<L>([&](int i, int e) { v[i][e] += pre_b[i][e]; });
+            store_row<E, L>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
         }
     }
 }
@@ -230,27 +288,53 @@ struct NormBackArgs {
 };
 
 // From d, the gradient of a norm's result times gamma, and the normalised row to the gradient of its input.
-template <int WAVES, int CH>
-__device__ inline void norm_gradient(int kind, float (&d)[CH][8], const float (&hat)[CH][8], float inv, int D, Sums<WAVES>& sums) {
+template <typename L>
+__device__ inline void norm_gradient(int kind, Values<L>& d, const Values<L>& hat, float inv, int D, Sums<L::WAVES>& sums) {
     float s1 = 0.0f, s2 = 0.0f;
-    each<CH>([&](int i, int e) {
+    each<L>([&](int i, int e) {
         s1 += d[i][e];
         s2 = fmaf(d[i][e], hat[i][e], s2);
     });
     const float2 s = sums(s1, s2);
     const float m1 = kind == BNN_NORM_LAYER ? s.x / float(D) : 0.0f, m2 = s.y / float(D);
-    each<CH>([&](int i, int e) { d[i][e] = inv * (d[i][e] - m1 - hat[i][e] * m2); });
+    each<L>([&](int i, int e) { d[i][e] = inv * (d[i][e] - m1 - hat[i][e] * m2); });
 }
 
-// Wavefronts a SIMD: with 16-bit rows of up to 4096 elements a few spilled registers are cheaper than a second workgroup that does
-// not fit (16384 x 4096 bfloat16: 197 us against 233), with float32 rows they are not (329 us against 422).
-template <typename E, int WAVES, int CH>
-inline constexpr int kBackwardWaves = CH == 1 && !is_f32<E> ? 4 : WAVES == 16 ? 4 : 2;
+// Vectors of a row's layout, in LDS: each thread reads what it has written.
+template <typename L>
+struct Kept {
+    static constexpr int kQuads = L::CH * L::G / 4;
+    static constexpr bool kThree = kQuads * 64 * L::WAVES * 16 * 3 < 160 * 1024;      // what fits: two or three
+    float4* lds;             // [vector][quad][thread]
+    __device__ inline void put(int which, const Values<L>& v) {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            const float* const p = &v[q * 4 / L::G][q * 4 % L::G];
+            lds[(which * kQuads + q) * (64 * L::WAVES) + threadIdx.x] = make_float4(p[0], p[1], p[2], p[3]);
+        }
+    }
+    __device__ inline void get(int which, Values<L>& v) const {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            float* const p = &v[q * 4 / L::G][q * 4 % L::G];
+            const float4 f = lds[(which * kQuads + q) * (64 * L::WAVES) + threadIdx.x];
+            p[0] = f.x;
+            p[1] = f.y;
+            p[2] = f.z;
+            p[3] = f.w;
+        }
+    }
+};
 
-template <typename E, int WAVES, int CH, bool BETAS, bool SHORT>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kBackwardWaves<E, WAVES, CH>))) void norm_residual_backward_kernel(const NormBackArgs a) {
-    __shared__ float sums_s[4 * WAVES];
-    Sums<WAVES> sums{sums_s, 0};
+// Wavefronts a SIMD: what leaves registers for the row and its sums.
+template <typename E, typename L>
+inline constexpr int kBackwardWaves = L::WAVES == 16 ? 4 : L::CH == 2 || is_f32<E> ? 2 : 4;
+
+// BETAS: a norm has one, or its gradient is wanted.
+template <typename E, typename L, bool BETAS>
+__global__ __launch_bounds__(64 * L::WAVES) __attribute__((amdgpu_waves_per_eu((kBackwardWaves<E, L>)))) void norm_residual_backward_kernel(const NormBackArgs a) {
+    __shared__ float2 sums_s[2 * L::WAVES];
+    Sums<L::WAVES> sums(sums_s);
     const int D = a.D;
     const int64_t strip = blockIdx.x, R = a.rows_per_gate;
     int64_t first, last;
@@ -263,124 +347,115 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kBac
         last = min(first + a.strips.rows, int64_t(a.M));
     }
     const bool norm = a.pre != BNN_NORM_NONE;
-    float sum_gate[CH][8] = {}, sum_pre[CH][8] = {}, sum_post[CH][8] = {};
-    float sum_pre_b[BETAS ? CH : 1][8] = {}, sum_post_b[BETAS ? CH : 1][8] = {};
-    float post_g[CH][8], pre_g[CH][8];
-    Row<E, WAVES, CH> y, r, dn, dr, gate;
+    Values<L> sum_gate = {}, sum_pre = {}, sum_post = {}, sum_pre_b = {}, sum_post_b = {};
+    __shared__ float4 kept_s[(BETAS && Kept<L>::kThree ? 3 : 2) * Kept<L>::kQuads * 64 * L::WAVES];
+    Kept<L> kept{kept_s};
+    enum { kPostGamma, kPreGamma, kPostBeta };
+    Row<E, L> y, r, dn, dr, gate;
     int64_t gate_row = 0, gate_end = 0;
     auto load = [&](int64_t m) {
-        y.template load<SHORT>(a.y, m, a.ld_y, D);
+        y.load(a.y, m, a.ld_y, D);
         if (norm) {
-            dn.template load<SHORT>(a.dn, m, a.ld_dn, D);
-            r.template load<SHORT>(a.r, m, a.ld_r, D);
+            dn.load(a.dn, m, a.ld_dn, D);
+            r.load(a.r, m, a.ld_r, D);
         }
     };
     if (first < last) {
         load(first);
-        load_vector<WAVES, CH, SHORT>(a.post_gamma, D, 1.0f, post_g);
-        load_vector<WAVES, CH, SHORT>(a.pre_gamma, D, 1.0f, pre_g);
+        Values<L> v;
+        load_vector<L>(a.post_gamma, D, 1.0f, v);
+        kept.put(kPostGamma, v);
+        load_vector<L>(a.pre_gamma, D, 1.0f, v);
+        kept.put(kPreGamma, v);
+        if constexpr (BETAS && Kept<L>::kThree) {
+            load_vector<L>(a.post_beta, D, 0.0f, v);
+            kept.put(kPostBeta, v);
+        }
     }
     for (int64_t m = first; m < last; ++m) {
-        float d[CH][8], v[CH][8];
+        Values<L> d, v, hat;
         // Of this row, needed after the first sums.
-        if (a.dr) dr.template load<SHORT>(a.dr, m, a.ld_dr, D);
+        if (a.dr) dr.load(a.dr, m, a.ld_dr, D);
         if (a.gate && m >= gate_end) {
             gate_row = m / R;
             gate_end = (gate_row + 1) * R;
-            gate.template load<SHORT>(a.gate, gate_row, a.ld_gate, D);
+            gate.load(a.gate, gate_row, a.ld_gate, D);
         }
-        y.template widened<SHORT>(D, v);
-        float hat[CH][8];
+        y.widened(D, v);
         if (norm) {
-            dn.template widened<SHORT>(D, d);
-            r.template widened<SHORT>(D, hat);
+            dn.widened(D, d);
+            r.widened(D, hat);
         }
         load(min(m + 1, last - 1));                 // the next row, or the last one again
+        if (!norm) each<L>([&](int i, int e) { hat[i][e] = 0.0f; });
+        const float2 inv = normalise_both<L>(a.pre, hat, a.post, v, D, a.eps, sums);
+        Values<L> gamma;
         if (norm) {
-            const float inv = normalise<WAVES, CH>(a.pre, hat, D, a.eps, sums);
-            each<CH>([&](int i, int e) {
+            kept.get(kPreGamma, gamma);
+            each<L>([&](int i, int e) {
                 sum_pre[i][e] = fmaf(d[i][e], hat[i][e], sum_pre[i][e]);
                 if constexpr (BETAS) sum_pre_b[i][e] += d[i][e];
-                d[i][e] *= pre_g[i][e];
+                d[i][e] *= gamma[i][e];
             });
-            norm_gradient<WAVES, CH>(a.pre, d, hat, inv, D, sums);
+            norm_gradient<L>(a.pre, d, hat, inv.x, D, sums);
         } else {
-            each<CH>([&](int i, int e) { d[i][e] = 0.0f; });
+            each<L>([&](int i, int e) { d[i][e] = 0.0f; });
         }
         if (a.dr) {
-            dr.template widened<SHORT>(D, hat);
-            each<CH>([&](int i, int e) { d[i][e] += hat[i][e]; });
+            dr.widened(D, hat);
+            each<L>([&](int i, int e) { d[i][e] += hat[i][e]; });
         }
-        if (a.dx) store_row<E, WAVES, CH>(static_cast<E*>(a.dx) + m * a.ld_dx, D, d);
+        if (a.dx) store_row<E, L>(static_cast<E*>(a.dx) + m * a.ld_dx, D, d);
 
-        float inv = 1.0f;
-        if (a.post != BNN_NORM_NONE) inv = normalise<WAVES, CH>(a.post, v, D, a.eps, sums);
-        each<CH>([&](int i, int e) { d[i][e] = first_col<WAVES>(i) + e < D ? d[i][e] * a.res_scale : 0.0f; });
+        each<L>([&](int i, int e) { d[i][e] = L::first_col(i) + e < D ? d[i][e] * a.res_scale : 0.0f; });
+        kept.get(kPostGamma, gamma);
         if (a.dgate) {
             // t = gamma * hat + beta
-            each<CH>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], v[i][e] * post_g[i][e], sum_gate[i][e]); });
-            if (a.post_beta) {
-                float beta[CH][8];
-                load_vector<WAVES, CH, SHORT>(a.post_beta, D, 0.0f, beta);
-                each<CH>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], beta[i][e], sum_gate[i][e]); });
+            each<L>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], v[i][e] * gamma[i][e], sum_gate[i][e]); });
+            if constexpr (BETAS) {
+                Values<L> beta;
+                if constexpr (Kept<L>::kThree) kept.get(kPostBeta, beta);
+                else load_vector<L>(a.post_beta, D, 0.0f, beta);
+                each<L>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], beta[i][e], sum_gate[i][e]); });
             }
             if (a.strips.per_gate == 0 && (m + 1 == last || m + 1 == gate_end)) {
-                store_row<E, WAVES, CH>(static_cast<E*>(a.dgate) + gate_row * a.ld_dgate, D, sum_gate);
-                each<CH>([&](int i, int e) { sum_gate[i][e] = 0.0f; });
+                store_row<E, L>(static_cast<E*>(a.dgate) + gate_row * a.ld_dgate, D, sum_gate);
+                each<L>([&](int i, int e) { sum_gate[i][e] = 0.0f; });
             }
         }
         if (a.gate) {
-            gate.template widened<SHORT>(D, hat);
-            each<CH>([&](int i, int e) { d[i][e] *= hat[i][e]; });
+            gate.widened(D, hat);
+            each<L>([&](int i, int e) { d[i][e] *= hat[i][e]; });
         }
         if (a.post != BNN_NORM_NONE) {
-            each<CH>([&](int i, int e) {
+            each<L>([&](int i, int e) {
                 sum_post[i][e] = fmaf(d[i][e], v[i][e], sum_post[i][e]);
                 if constexpr (BETAS) sum_post_b[i][e] += d[i][e];
-                d[i][e] *= post_g[i][e];
+                d[i][e] *= gamma[i][e];
             });
-            if (a.dy) norm_gradient<WAVES, CH>(a.post, d, v, inv, D, sums);
+            if (a.dy) norm_gradient<L>(a.post, d, v, inv.y, D, sums);
         }
-        if (a.dy) store_row<E, WAVES, CH>(static_cast<E*>(a.dy) + m * a.ld_dy, D, d);
+        if (a.dy) store_row<E, L>(static_cast<E*>(a.dy) + m * a.ld_dy, D, d);
     }
     float* const part = a.part + strip * D;
-    if (a.at_gate >= 0) store_row<float, WAVES, CH>(part + a.at_gate * a.part_step, D, sum_gate);
-    if (a.at_pre_gamma >= 0) store_row<float, WAVES, CH>(part + a.at_pre_gamma * a.part_step, D, sum_pre);
-    if (a.at_post_gamma >= 0) store_row<float, WAVES, CH>(part + a.at_post_gamma * a.part_step, D, sum_post);
+    if (a.at_gate >= 0) store_row<float, L>(part + a.at_gate * a.part_step, D, sum_gate);
+    if (a.at_pre_gamma >= 0) store_row<float, L>(part + a.at_pre_gamma * a.part_step, D, sum_pre);
+    if (a.at_post_gamma >= 0) store_row<float, L>(part + a.at_post_gamma * a.part_step, D, sum_post);
     if constexpr (BETAS) {
-        if (a.at_pre_beta >= 0) store_row<float, WAVES, CH>(part + a.at_pre_beta * a.part_step, D, sum_pre_b);
-        if (a.at_post_beta >= 0) store_row<float, WAVES, CH>(part + a.at_post_beta * a.part_step, D, sum_post_b);
+        if (a.at_pre_beta >= 0) store_row<float, L>(part + a.at_pre_beta * a.part_step, D, sum_pre_b);
+        if (a.at_post_beta >= 0) store_row<float, L>(part + a.at_post_beta * a.part_step, D, sum_post_b);
     }
 }
 
-// Calls f<WAVES, CH, SHORT>() for rows of D elements.  Forwards 16 elements a thread, for fewer wavefronts at the barriers;
-// backwards, with the sums over rows beside them, 8 where the row is short enough.
-template <bool FORWARD, typename F>
+// Calls f(layout) for rows of D elements.
+template <typename F>
 inline void with_row(int64_t D, F&& f) {
-    using std::false_type;
-    using std::integral_constant;
-    using std::true_type;
-    using One = integral_constant<int, 1>;
-    using Two = integral_constant<int, 2>;
-    if (D < 8) f(One{}, One{}, true_type{});
-    else if (D <= 512) f(One{}, One{}, false_type{});
-    else if constexpr (FORWARD) {
-        if (D <= 1024) f(One{}, Two{}, false_type{});
-        else if (D <= 2048) f(Two{}, Two{}, false_type{});
-        else if (D <= 3072) f(integral_constant<int, 3>{}, Two{}, false_type{});
-        else if (D <= 4096) f(integral_constant<int, 4>{}, Two{}, false_type{});
-        else if (D <= 6144) f(integral_constant<int, 6>{}, Two{}, false_type{});
-        else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
-        else f(integral_constant<int, 16>{}, Two{}, false_type{});
-    } else {
-        if (D <= 1024) f(Two{}, One{}, false_type{});
-        else if (D <= 2048) f(integral_constant<int, 4>{}, One{}, false_type{});
-        else if (D <= 3072) f(integral_constant<int, 6>{}, One{}, false_type{});
-        else if (D <= 4096) f(integral_constant<int, 8>{}, One{}, false_type{});
-        else if (D <= 6144) f(integral_constant<int, 6>{}, Two{}, false_type{});
-        else if (D <= 8192) f(integral_constant<int, 8>{}, Two{}, false_type{});
-        else f(integral_constant<int, 16>{}, Two{}, false_type{});
-    }
+    if (D < 8) f(Layout<1, 8, 1, true>{});
+    else if (D <= 512) f(Layout<1, 8, 1, false>{});
+    else if (D <= 1024) f(Layout<1, 8, 2, false>{});
+    else if (D <= 4096) f(Layout<4, 8, 2, false>{});
+    else if (D <= 8192) f(Layout<8, 8, 2, false>{});
+    else f(Layout<16, 8, 2, false>{});
 }
 
 bool norm_kind(int kind) { return kind == BNN_NORM_NONE || kind == BNN_NORM_RMS || kind == BNN_NORM_LAYER; }
@@ -424,12 +499,14 @@ extern "C" int bnn_norm_residual(int type, const void* y, int64_t ld_y, const vo
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool betas = post_beta || pre_beta;
     with_type(type, [&](auto e) {
-        with_row<true>(D, [&](auto waves, auto ch, auto is_short) {
+        with_row(D, [&](auto layout) {
+            using L = decltype(layout);
             // As many workgroups as are on the chip together, each walking over rows.
-            const int64_t together = 256 * (kNormWaves / waves);
-            const dim3 grid(uint32_t(M < together ? M : together)), block(64 * waves);
-            if (betas) norm_residual_kernel<decltype(e), waves, ch, true, is_short><<<grid, block, 0, s>>>(a);
-            else norm_residual_kernel<decltype(e), waves, ch, false, is_short><<<grid, block, 0, s>>>(a);
+            const int threads = L::threads(D);
+            const int64_t together = 256 * (64 * kNormWaves / threads);
+            const dim3 grid(uint32_t(M < together ? M : together)), block(uint32_t(threads), 1, 1);
+            if (betas) norm_residual_kernel<decltype(e), L, true><<<grid, block, 0, s>>>(a);
+            else norm_residual_kernel<decltype(e), L, false><<<grid, block, 0, s>>>(a);
         });
     });
     return check_launch();
@@ -485,40 +562,36 @@ extern "C" int bnn_norm_residual_backward(int type, const void* dr, int64_t ld_d
     a.part_step = a.strips.count * D;
     a.res_scale = res_scale; a.eps = eps; a.post = post; a.pre = pre; a.M = int(M); a.D = int(D);
     JoinArgs join{};
-    int vectors = 0;
+    join.N = int(D);
     auto want = [&](float* out) {
         if (!out) return -1;
-        join.out[vectors] = out;
-        return vectors++;
+        join.add(a.part + join.vectors * a.part_step, a.strips.count, out);
+        return join.vectors - 1;
     };
     a.at_post_gamma = want(dpost_gamma);
     a.at_post_beta = want(dpost_beta);
     a.at_pre_gamma = want(dpre_gamma);
     a.at_pre_beta = want(dpre_beta);
-    a.at_gate = dgate && a.strips.per_gate > 0 ? vectors : -1;
+    a.at_gate = dgate && a.strips.per_gate > 0 ? join.vectors : -1;
     if (M > 0) {
-        const bool betas = dpost_beta || dpre_beta;
+        const bool betas = post_beta || dpost_beta || dpre_beta;
         with_type(type, [&](auto e) {
-            with_row<false>(D, [&](auto waves, auto ch, auto is_short) {
-                const dim3 grid(uint32_t(a.strips.count)), block(64 * waves);
-                if (betas) norm_residual_backward_kernel<decltype(e), waves, ch, true, is_short><<<grid, block, 0, s>>>(a);
-                else norm_residual_backward_kernel<decltype(e), waves, ch, false, is_short><<<grid, block, 0, s>>>(a);
+            with_row(D, [&](auto layout) {
+                using L = decltype(layout);
+                const dim3 grid(uint32_t(a.strips.count)), block(uint32_t(L::threads(D)));
+                if (betas) norm_residual_backward_kernel<decltype(e), L, true><<<grid, block, 0, s>>>(a);
+                else norm_residual_backward_kernel<decltype(e), L, false><<<grid, block, 0, s>>>(a);
             });
         });
         if ((st = check_launch()) != BNN_OK) return st;
     }
-    join.part = a.part;
-    join.part_step = a.part_step;
-    join.per_group = int(a.strips.count);
-    join.N = int(D);
-    if (vectors > 0 && (st = join_sums<float>(join, 1, vectors, s)) != BNN_OK) return st;
     if (a.at_gate >= 0 && M > 0) {
-        join.part = a.part + a.at_gate * a.part_step;
+        join.group_part = a.part + a.at_gate * a.part_step;
+        join.groups = int(ceil_div(M, a.rows_per_gate));
         join.per_group = int(a.strips.per_gate);
-        join.out[0] = dgate;
+        join.out_groups = dgate;
         join.ld_out = ld_dgate;
-        with_type(type, [&](auto e) { st = join_sums<decltype(e)>(join, ceil_div(M, a.rows_per_gate), 1, s); });
-        return st;
     }
-    return BNN_OK;
+    with_type(type, [&](auto e) { st = join_sums<decltype(e)>(join, s); });
+    return st;
 }

@@ -20,11 +20,13 @@ inline constexpr bool is_f32 = std::is_same<E, float>::value;
 template <typename E>
 using Operand = typename std::conditional<is_f32<E>, bf16_t, E>::type;
 
-template <typename E>
-struct Vec8 {
-    typedef E type __attribute__((ext_vector_type(8)));
-    typedef E any __attribute__((ext_vector_type(8), aligned(sizeof(E))));      // the same at the type's own alignment
+template <typename E, int G>
+struct Group {
+    typedef E type __attribute__((ext_vector_type(G)));
+    typedef E any __attribute__((ext_vector_type(G), aligned(sizeof(E))));      // the same at the type's own alignment
 };
+template <typename E>
+using Vec8 = Group<E, 8>;
 
 // Calls `f` with a value of the C++ type of a bnn_type; false for a type that does not exist.
 template <typename F>
@@ -39,52 +41,62 @@ inline bool with_type(int type, F&& f) {
 
 inline int64_t type_bytes(int type) { return type == BNN_F32 ? 4 : type == BNN_BF16 || type == BNN_F16 ? 2 : 0; }
 
-// Eight elements from p on, of which the first `valid` exist; zero for the others, which are not read.  p is aligned to
+// G elements from p on, of which the first `valid` exist; zero for the others, which are not read.  p is aligned to
 // its element: a whole group is one or two 16-byte loads, which need no more than that.  The elements of a part of a group are
 // loaded all at once (the last one again for those that are not there): one by one, each would wait for the one before.
-template <typename E>
-__device__ inline typename Vec8<E>::type load8(const E* p, int64_t valid) {
-    typename Vec8<E>::type v = {};
-    if (valid >= 8) {
-        v = *reinterpret_cast<const typename Vec8<E>::any*>(p);
+template <typename E, int G>
+__device__ inline typename Group<E, G>::type load_group(const E* p, int64_t valid) {
+    typename Group<E, G>::type v = {};
+    if (valid >= G) {
+        v = *reinterpret_cast<const typename Group<E, G>::any*>(p);
     } else if (valid > 0) {
         const int last = int(valid) - 1;
-        E e[7];
+        E e[G - 1];
 #pragma unroll
-        for (int i = 0; i < 7; ++i) e[i] = p[min(i, last)];
+        for (int i = 0; i < G - 1; ++i) e[i] = p[min(i, last)];
 #pragma unroll
-        for (int i = 0; i < 7; ++i) v[i] = i <= last ? e[i] : E(0.0f);
+        for (int i = 0; i < G - 1; ++i) v[i] = i <= last ? e[i] : E(0.0f);
     }
     return v;
 }
 
-// What is left of a row from a group's first element on, `left` elements: the group as it is for 8 or more, and for fewer the
-// last ones of v - the row's last eight elements, loaded in the group's place - moved down, with zeros after them.
 template <typename E>
-__device__ inline typename Vec8<E>::type row_end(typename Vec8<E>::type v, int left) {
-    const int by = 8 - left;
+__device__ inline typename Vec8<E>::type load8(const E* p, int64_t valid) {
+    return load_group<E, 8>(p, valid);
+}
+
+// What is left of a row from a group's first element on, `left` elements: the group as it is for G or more, and for fewer the
+// last ones of v - the row's last G elements, loaded in the group's place - moved down, with zeros after them.
+template <typename E, int G = 8>
+__device__ inline typename Group<E, G>::type row_end(typename Group<E, G>::type v, int left) {
+    const int by = G - left;
 #pragma unroll
-    for (int step = 4; step > 0; step >>= 1) {
-        typename Vec8<E>::type moved = v;
+    for (int step = G / 2; step > 0; step >>= 1) {
+        typename Group<E, G>::type moved = v;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) moved[i] = i + step < 8 ? v[i + step] : E(0.0f);
+        for (int i = 0; i < G; ++i) moved[i] = i + step < G ? v[i + step] : E(0.0f);
         if (by > 0 && (by & step)) v = moved;
     }
-    return left > 0 ? v : typename Vec8<E>::type{};
+    return left > 0 ? v : typename Group<E, G>::type{};
+}
+
+template <typename E, int G>
+__device__ inline void store_group(E* p, const float (&v)[G], int64_t valid) {
+    typename Group<E, G>::type o;
+#pragma unroll
+    for (int i = 0; i < G; ++i) o[i] = E(v[i]);
+    if (valid >= G) {
+        *reinterpret_cast<typename Group<E, G>::any*>(p) = o;
+    } else {
+#pragma unroll
+        for (int i = 0; i < G - 1; ++i)
+            if (i < valid) p[i] = o[i];
+    }
 }
 
 template <typename E>
 __device__ inline void store8(E* p, const float (&v)[8], int64_t valid) {
-    typename Vec8<E>::type o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = E(v[i]);
-    if (valid >= 8) {
-        *reinterpret_cast<typename Vec8<E>::any*>(p) = o;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < valid) p[i] = o[i];
-    }
+    store_group<E, 8>(p, v, valid);
 }
 
 // The same with W of the eight, as plain floats.
