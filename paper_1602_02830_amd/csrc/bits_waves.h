@@ -27,7 +27,37 @@ struct WavesTile {
 // The word of a row of weights that 32 elements from 32 i on are in.
 __device__ inline uint32_t word_of(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
 
-template <typename E, int EPI, int FM, int FN>
+// Rows of 16-bit elements that do not begin with a 32-bit word: a 16-byte load from the middle of a word takes the cache more than
+// twice as long (93 x 295 x 4979 float16: 29.3 us, K = 4978 11.9).  So (ODD) a lane loads whole words from the one on that its
+// first element is in, one more than its elements fill, and shifts them together where its row needs that (12.7 us).  Every word
+// has an element of the row in it.  The row's last, partial run is loaded as it lies.
+struct WholeWords {
+    uint32_t by;                         // bits
+    template <typename E>
+    __device__ inline explicit WholeWords(const E* row) : by(8 * (uint32_t(reinterpret_cast<uintptr_t>(row)) & 3u)) {}
+    // Eight elements, of which `after` holds the last one.
+    template <typename V>
+    __device__ inline V operator()(const V& v, uint32_t after) const {
+        const v4u_t q = __builtin_bit_cast(v4u_t, v);
+        return __builtin_bit_cast(V, v4u_t{__builtin_amdgcn_alignbit(q[1], q[0], by), __builtin_amdgcn_alignbit(q[2], q[1], by),
+                                           __builtin_amdgcn_alignbit(q[3], q[2], by), __builtin_amdgcn_alignbit(after, q[3], by)});
+    }
+};
+template <typename V>
+__device__ inline uint32_t first_word(const V& v) {
+    return __builtin_bit_cast(v4u_t, v)[0];
+}
+template <typename E>
+__device__ inline const E* word_begin(const E* p) {
+    return reinterpret_cast<const E*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
+}
+// Some rows begin inside a word, and are longer than `longer`: below that the partial run is most of the row.
+template <typename E>
+inline bool odd_rows(const ProductArgs& a, int longer) {
+    return !is_f32<E> && a.K > longer && (!aligned_to(a.x, 4) || a.ld_x % 2 != 0);
+}
+
+template <typename E, int EPI, int FM, int FN, bool ODD>
 __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
     using S = WavesTile<E, EPI, FM, FN>;
     using O = Operand<E>;
@@ -70,13 +100,22 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
         }
     };
     E8 xv[4][FM][4];                     // [quarter of a run][block][group of eight elements]
+    uint32_t after[FM];                  // the word past a run
     auto load_x = [&](int r, int i) {
         const int64_t k = int64_t(r) * kRunK + 128 * fh + 32 * i;
         if ((r + 1) * int64_t(kRunK) <= a.K) {
 #pragma unroll
             for (int j = 0; j < FM; ++j)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) xv[i][j][s] = *reinterpret_cast<const typename Vec8<E>::any*>(xrow[j] + k + 8 * s);
+                for (int s = 0; s < 4; ++s)
+                    xv[i][j][s] = *reinterpret_cast<const typename Vec8<E>::any*>((ODD ? word_begin(xrow[j]) : xrow[j]) + k + 8 * s);
+            if constexpr (ODD) {
+                // Also where the row begins with a word: what follows it is then not looked at, and need not be there.
+                if (i == 3) {
+#pragma unroll
+                    for (int j = 0; j < FM; ++j) after[j] = *reinterpret_cast<const uint32_t*>(word_begin(xrow[j] + k + 31));
+                }
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < FM; ++j)
@@ -101,6 +140,17 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (int64_t(r) * kRunK + 32 * i >= a.K) break;                 // nothing left for either half
+            if constexpr (ODD) {
+                if ((r + 1) * int64_t(kRunK) <= a.K) {
+#pragma unroll
+                    for (int j = 0; j < FM; ++j) {
+                        const WholeWords whole(xrow[j]);
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+                            xv[i][j][s] = whole(xv[i][j][s], s < 3 ? first_word(xv[i][j][s + 1]) : i < 3 ? first_word(xv[i + 1][j][0]) : after[j]);
+                    }
+                }
+            }
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 O8 wf[FN];
@@ -194,7 +244,7 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
 constexpr int kFewRowsRunK = 512, kFewRows = 16;
 
 // FN blocks of 16 channels (gated: of each half).
-template <typename E, int EPI, int FN>
+template <typename E, int EPI, int FN, bool ODD>
 __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a) {
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
@@ -227,7 +277,14 @@ __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a)
         typename Vec8<E>::type xv[16];
         if (k0 + kFewRowsRunK <= a.K) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) xv[i] = *reinterpret_cast<const typename Vec8<E>::any*>(xrow + k + 8 * i);
+            for (int i = 0; i < 16; ++i)
+                xv[i] = *reinterpret_cast<const typename Vec8<E>::any*>((ODD ? word_begin(xrow) : xrow) + k + 8 * i);
+            if constexpr (ODD) {
+                const uint32_t after = *reinterpret_cast<const uint32_t*>(word_begin(xrow + k + 127));
+                const WholeWords whole(xrow);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) xv[i] = whole(xv[i], i < 15 ? first_word(xv[i + 1]) : after);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) xv[i] = load8<E>(xrow + k + 8 * i, a.K - k - 8 * i);
@@ -275,7 +332,16 @@ template <typename E, int EPI, int FN>
 int launch_few_rows(const ProductArgs& a, int waves, hipStream_t s) {
     const int64_t blocks = ceil_div(a.N, 16 * FN);
     if (blocks > max_blocks(64 * waves)) return BNN_ERR_UNSUPPORTED;
-    bits_few_rows_kernel<E, EPI, FN><<<dim3(uint32_t(blocks)), dim3(64 * waves), size_t(waves) * FN * kHalves<EPI> * 1024, s>>>(a);
+    const dim3 grid{uint32_t(blocks)}, block{uint32_t(64 * waves)};
+    const size_t lds = size_t(waves) * FN * kHalves<EPI> * 1024;
+    if constexpr (!is_f32<E>) {
+        // Up to four rows are few lines, and the extra word costs more (1 x 4095 -> 4096: 4.4 us against 4.9).
+        if (a.M > 4 && odd_rows<E>(a, 2 * kFewRowsRunK)) {
+            bits_few_rows_kernel<E, EPI, FN, true><<<grid, block, lds, s>>>(a);
+            return check_launch();
+        }
+    }
+    bits_few_rows_kernel<E, EPI, FN, false><<<grid, block, lds, s>>>(a);
     return check_launch();
 }
 
@@ -285,7 +351,14 @@ int launch_waves(ProductArgs a, int waves, hipStream_t s) {
     const int64_t tiles_m = ceil_div(a.M, S::BM), tiles_n = ceil_div(kBackward<EPI> ? a.half : a.N, S::BN);
     if (tiles_m * tiles_n > max_blocks(64 * waves)) return BNN_ERR_UNSUPPORTED;
     a.map = tile_map(tiles_m, tiles_n);
-    bits_waves_kernel<E, EPI, FM, FN><<<dim3(uint32_t(tiles_m * tiles_n)), dim3(64 * waves), S::lds_bytes(waves), s>>>(a);
+    const dim3 grid(uint32_t(tiles_m * tiles_n)), block(64 * waves);
+    if constexpr (!is_f32<E>) {
+        if (odd_rows<E>(a, kRunK)) {
+            bits_waves_kernel<E, EPI, FM, FN, true><<<grid, block, S::lds_bytes(waves), s>>>(a);
+            return check_launch();
+        }
+    }
+    bits_waves_kernel<E, EPI, FM, FN, false><<<grid, block, S::lds_bytes(waves), s>>>(a);
     return check_launch();
 }
 

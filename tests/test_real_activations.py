@@ -208,6 +208,18 @@ def test_linear_strides_and_alignment(M, N, K, gap, shift, T):
     assert torch.equal(got, out)
 
 
+# Rows of 16-bit elements that begin inside a 32-bit word, all of them or every other one, and end anywhere; what lies around them is NaN.
+@gpu
+@pytest.mark.parametrize("T", ["bf16", "f16"])
+@pytest.mark.parametrize("gap,shift", [(0, 0), (0, 1), (1, 0), (1, 1), (2, 1), (7, 3)])
+@pytest.mark.parametrize("M,K", [(3, 2047), (5, 1025), (16, 1536), (11, 2050), (20, 257), (40, 512), (70, 775), (33, 1279)])
+def test_rows_that_begin_inside_a_word(M, K, gap, shift, T):
+    T = TYPES[T]
+    p = Product(M, 150, K, T, seed=13, gap=gap, shift=shift)
+    close(bnn.linear_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_GELU), *linear_want(p, "gelu"), "linear")
+    close(bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU), *gated_want(p, "silu"), "gated")
+
+
 @gpu
 @pytest.mark.parametrize("T", TYPES)
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu", "sigmoid", "none"])
@@ -309,6 +321,18 @@ def test_gated_backward(M, F, K, act, T):
 @pytest.mark.parametrize("M,N,K", [(1000, 4090, 100), (2040, 4090, 70), (4090, 4090, 65), (70, 4090, 3100), (40, 2100, 2000), (4000, 100, 90),
                                    (1500, 3, 5), (70, 5, 300), (70, 300, 5)])
 def test_linear_backward_large_tiles(M, N, K, act, T):
+    T = TYPES[T]
+    p = Product(M, N, K, T, seed=7)
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+    check_backward(p, act, False, dy, bnn.linear_bits_backward(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act]))
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("M,N,K", [(6000, 300, 521), (9001, 131, 255), (700, 300, 200), (2100, 1030, 260)])
+def test_linear_backward_parts_of_the_rows(M, N, K, act, T):
+    """The weights' gradient joined from parts of the rows, in tiles of 64 and of 128."""
     T = TYPES[T]
     p = Product(M, N, K, T, seed=7)
     dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
