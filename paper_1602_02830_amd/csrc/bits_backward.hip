@@ -81,22 +81,47 @@ constexpr int kStrips = 256;       // strips of rows for the column sums without
 
 inline int64_t round_up(int64_t v, int64_t to) { return ceil_div(v, to) * to; }
 
-// How dw is made: tiles of 256, 128 or 64 rows and columns, and over how many parts of the rows.  Tiles of 256 are the
-// fastest where they fill the chip (4096 x 4096 x 4096: 126 us, tiles of 128 169; with half as many of them 126 and 85), those of 64 where
-// those of 128 do not (1000 x 1024 x 1024: 11.0 us against 14.2).  Where even they are few, rows are split and the parts joined:
-// a product of 16384 rows and 512 x 512 would be 64 tiles of 512 steps, 190 us.
+// How dw is made: tiles of 256, 128 or 64 rows and columns, and over how many parts of the rows, whose sums are then joined.
+//
+// By an estimate in microseconds: a round of the chip - so many workgroups as are on it together - takes a start and so much for
+// each step of 32 rows, half a round of tiles of 128 less; parts cost a launch and their way through memory.  It takes what is, or is
+// within 6 % of, the fastest of all that were tried at 23 sizes (a whole backward pass, us): 4096 x 4096 x 4096 bfloat16 with tiles of
+// 256 in one part 280, in two 334, tiles of 128 319; 16384 x 1024 x 1024 with tiles of 128 in four parts 120, of 64 in two 155;
+// 15213 x 5896 x 385 float32 128 in four 1218, in one 1330, 64 in one 1638; 1000 x 1024 x 1024 bfloat16 64 in one 31, in two 35.
+// One size misses it by 12 % (3488 x 712 x 3968: 106, with two parts 94).
 struct GradPlan {
-    int tile, splits, split_rows;
+    int tile = 64, splits = 1, split_rows;
     bool general;
-    GradPlan(bool f32, int64_t M, int64_t cols, int64_t K) {
-        auto tiles = [&](int64_t t) { return ceil_div(cols, t) * ceil_div(K, t); };
-        general = cols < 8 || K < 8;
-        tile = general ? 64 : !f32 && tiles(256) >= 192 ? 256 : tiles(128) >= 256 ? 128 : 64;
-        const int64_t most = M / (8 * kGradStep), wanted = tiles(tile) > 0 ? 512 / tiles(tile) : 1;
-        const int64_t parts = wanted < most ? wanted : most;
-        split_rows = int(round_up(ceil_div(M, parts > 1 ? parts : 1), kGradStep));
-        splits = int(parts > 1 ? ceil_div(M, split_rows) : 1);
-        if (splits == 1) split_rows = int(M);
+    GradPlan(bool f32, int64_t M, int64_t cols, int64_t channels, int64_t K) : split_rows(int(M)), general(cols < 8 || K < 8) {
+        struct Kind {
+            int tile, together;
+            float step, start;
+        };
+        static constexpr Kind kKinds[2][3] = {{{256, 256, 0.98f, 8.0f}, {128, 512, 0.60f, 5.0f}, {64, 512, 0.35f, 1.0f}},
+                                              {{128, 256, 2.0f, 8.0f}, {64, 512, 1.2f, 3.0f}, {0, 0, 0.0f, 0.0f}}};
+        const float piece_us = float(channels) * float(K) * (8.0f / 4.7e6f);
+        float least = 0.0f;
+        for (const Kind& kind : kKinds[f32 ? 1 : 0]) {
+            if (kind.tile == 0 || (general && kind.tile != 64)) continue;
+            const int64_t tiles = ceil_div(cols, kind.tile) * ceil_div(K, kind.tile);
+            for (int parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+                if (parts > 1 && parts * int64_t(8 * kGradStep) > M) break;
+                const int64_t groups = tiles * parts, rest = groups % kind.together;
+                const float rounds = float(groups / kind.together) +
+                                     (rest == 0 ? 0.0f : kind.tile == 128 && 2 * rest <= kind.together && !f32 ? 0.6f : 1.0f);
+                const float us = rounds * (float(ceil_div(ceil_div(M, parts), kGradStep)) * kind.step + kind.start) +
+                                 (parts > 1 ? 3.0f + float(parts) * piece_us : 0.0f);
+                if (least == 0.0f || us < least) {
+                    least = us;
+                    tile = kind.tile;
+                    splits = parts;
+                }
+            }
+        }
+        if (splits > 1) {
+            split_rows = int(round_up(ceil_div(M, splits), kGradStep));
+            splits = int(ceil_div(M, split_rows));
+        }
     }
 };
 
@@ -108,7 +133,7 @@ struct Plan {
     bool recompute;
     GradPlan grad;
     Plan(int64_t size, int64_t M, int64_t cols, int64_t K, int act, bool gated)
-        : recompute(gated || act != BNN_ACT_NONE), grad(size == 4, M, recompute ? round_up(cols, 64) * (gated ? 2 : 1) : cols, K) {
+        : recompute(gated || act != BNN_ACT_NONE), grad(size == 4, M, recompute ? round_up(cols, 64) * (gated ? 2 : 1) : cols, gated ? 2 * cols : cols, K) {
         halves = gated ? 2 : 1;
         half = round_up(cols, 64);
         ds_cols = half * halves;
