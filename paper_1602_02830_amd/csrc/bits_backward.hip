@@ -139,7 +139,7 @@ struct Plan {
         ds_cols = half * halves;
         wt_ld = round_up(ds_cols / 32, 4);
         const int64_t channels = halves * cols;
-        form = product_form(size == 4, false, M, channels);
+        form = product_form(size == 4, M, cols, int(halves));
         strip = round_up(ceil_div(M > 0 ? M : 1, kStrips), 4);
         // Tiles of a form with 64-bit offsets have 128 rows: never more of them than of the smaller of the two.
         const int64_t rows = rows_of_form(form);
@@ -241,7 +241,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         ProductArgs a{};
         a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx;
         a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
-        if ((st = launch_form<E, kLinear>(a, product_form(is_f32<E>, true, M, K), s)) != BNN_OK) return st;
+        if ((st = launch_form<E, kLinear>(a, product_form(is_f32<E>, M, K, 1), s)) != BNN_OK) return st;
     }
     const bool scale_by_k = dscale && !p.recompute;
     if ((dw || scale_by_k) && cols > 0 && K > 0) {

@@ -19,7 +19,8 @@ int launch_product(ProductArgs a, hipStream_t s) {
     return check_launch();
 }
 
-// The form of a product, by its sizes alone.
+// The form of a product, by its sizes alone: tiles of 16 rows by a wavefront each where there are few of them (their file has the
+// figures), then the following.
 //
 // Tiles have 256 channels and 256, 128 or 64 rows, and the time of one is a start of 7 - 10 us and a step of 64 elements of K,
 // measured in us: 1.6 (256 rows, one a compute unit), 0.75 - 1.0 (128 rows, one) and 0.55 (64 rows, one a compute unit; 1.14 with
@@ -28,13 +29,15 @@ int launch_product(ProductArgs a, hipStream_t s) {
 // (500 x 3062 x 784: 8.3 us against 12.1; 256 x 4096 x 4096: 15.5 against 38; 1000 x 4096 x 784, 256 tiles: 16.8 against 14.1).
 // float32 has three times the products a step: 64 rows, or 128 from two rounds of them on (4000 x 4096 x 1000: 103 us against 98);
 // 1000 x 4096 x 784 takes 26 us against 38 of wavefronts, 500 x 3062 x 784 (96 tiles) 20.6 against 18.3.
-enum Form { kFewRowsForm, kWavesForm, kTile64, kTile128, kTile256 };
+enum Form { kSmallForm, kWavesForm, kTile64, kTile128, kTile256 };
 
-inline int64_t rows_of_form(Form f) { return f == kTile256 ? 256 : f == kTile128 ? 128 : f == kTile64 ? 64 : 32; }
+inline int64_t rows_of_form(Form f) { return f == kTile256 ? 256 : f == kTile128 ? 128 : f == kTile64 ? 64 : f == kWavesForm ? 32 : 16; }
 
-inline Form product_form(bool f32, bool forward, int64_t M, int64_t channels) {
+// N columns of `halves` rows of weights each.
+inline Form product_form(bool f32, int64_t M, int64_t N, int halves) {
     constexpr int64_t kUnits = 256;
-    if (forward && M <= kFewRows) return kFewRowsForm;
+    if (M <= kSmallRows || ceil_div(M, kSmallRows) * ceil_div(N, 16) <= 2 * kUnits) return kSmallForm;
+    const int64_t channels = halves * N;
     const int64_t across = ceil_div(channels, 256), t64 = ceil_div(M, 64) * across, t128 = ceil_div(M, 128) * across, t256 = ceil_div(M, 256) * across;
     if (t64 < (f32 ? 128 : 224)) return kWavesForm;
     if (f32) return t128 >= 2 * kUnits ? kTile128 : kTile64;
@@ -59,16 +62,14 @@ inline int64_t rows_of_tile(Form form, int64_t ld_x) {
 template <typename E, int EPI>
 int launch_form(const ProductArgs& a, Form form, hipStream_t s) {
     constexpr int HALVES = kHalves<EPI>;
-    if constexpr (!kBackward<EPI>) {
-        if (form == kFewRowsForm) {
-            const int waves = int(a.K >= 8 * kFewRowsRunK ? 8 : a.K <= kFewRowsRunK ? 1 : ceil_div(a.K, kFewRowsRunK));
-            // Rows are read again for every 16 channels: two blocks a workgroup where there are enough for that (16 rows of
-            // 2 x 8192 x 4096: 8.5 us against 11.2; one row 6.7 against 6.7, and 4096 x 8192 with one block 5.1 against 6.7).
-            if (a.M > 4 && a.N >= 256 * 32) return launch_few_rows<E, EPI, 2>(a, waves, s);
-            return launch_few_rows<E, EPI, 1>(a, waves, s);
-        }
+    if (form == kSmallForm) {
+        const int waves = int(a.K >= 8 * kSmallRunK ? 8 : a.K <= kSmallRunK ? 1 : ceil_div(a.K, kSmallRunK));
+        // Rows are read again for every 16 channels: two blocks a workgroup where there are enough for that (16 rows of
+        // 2 x 8192 x 4096: 8.5 us against 11.2; one row 6.7 against 6.7, and 4096 x 8192 with one block 5.1 against 6.7).
+        if (a.M > 4 && a.N >= 256 * 32) return launch_small<E, EPI, 2>(a, waves, s);
+        return launch_small<E, EPI, 1>(a, waves, s);
     }
-    if (form == kWavesForm || form == kFewRowsForm) {
+    if (form == kWavesForm) {
         const int waves = int(a.K >= 4 * kRunK ? 4 : a.K <= kRunK ? 1 : ceil_div(a.K, kRunK));
         // 128 channels a tile where there is one for every compute unit and K is long (256 x 4096 x 4096: 15.5 us against 21;
         // 64 x 4096 x 8192, 64 tiles: 23.5 against 20.3).

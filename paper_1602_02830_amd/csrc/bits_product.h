@@ -67,7 +67,7 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
         activate<FAST, W>(a.act, z, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += r[i];
-        store_some<E, W>(y, v, valid);
+        store_group<E, W>(y, v, valid);
     } else if constexpr (EPI == kGated) {
         if (valid <= 0) return;
         float z[W], v[W];
@@ -76,7 +76,7 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
         activate<FAST, W>(a.act, z, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] *= fmaf(s[1][i], scale[1][i], bias[1][i]);
-        store_some<E, W>(y, v, valid);
+        store_group<E, W>(y, v, valid);
     } else {
         if (n >= a.half) return;
         float d[W], z[W], f[W], slope[W], out[HALVES][W];
@@ -103,7 +103,7 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
         }
         // Columns from N up to `half` are written as zeros.
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) store_some<E, W>(y + int64_t(h) * a.half, out[h], W);
+        for (int h = 0; h < HALVES; ++h) store_group<E, W>(y + int64_t(h) * a.half, out[h], W);
     }
 }
 

@@ -236,23 +236,28 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
     }
 }
 
-// ---- up to 16 rows -------------------------------------------------------------------------------------------------
+// ---- tiles of 16 rows ---------------------------------------------------------------------------------------------
 // Blocks of 16 channels, so that narrow layers still have a workgroup for every compute unit, and runs of 512 elements of K, of
 // which a quarter of a wavefront has 128: one 16-byte load of each row of weights.  All of a run's loads are on their way before
 // the first arrives, so a call takes one trip to memory for each run that a wavefront has, and the widening of the weights.
+// Beyond 16 rows these tiles are twice as many as those above, with half as much of x to look up for each: faster as long as two rounds
+// of the chip hold them (64 x 8192 -> 512, 128 of them: 10.3 us against 19.5; 128 x 4096 -> 1024, 512: 10.4 against 11.7;
+// 256 x 4096 -> 1024, 1024: 17.8 against 11.9).
 
-constexpr int kFewRowsRunK = 512, kFewRows = 16;
+constexpr int kSmallRunK = 512, kSmallRows = 16;
 
 // FN blocks of 16 channels (gated: of each half).
 template <typename E, int EPI, int FN, bool ODD>
-__global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
     constexpr int HALVES = kHalves<EPI>, BLOCKS = FN * HALVES, TERMS = kTermsOf<E>;
+    constexpr bool BACK = kBackward<EPI>;
     extern __shared__ __attribute__((aligned(16))) float4 part_s[];       // [wavefront][block][lane]
     __shared__ float scale_s[BLOCKS * 16], bias_s[BLOCKS * 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int r16 = lane & 15, quarter = lane >> 4, n0 = int(blockIdx.x) * (16 * FN), kw = (a.K + 31) >> 5;
+    const int r16 = lane & 15, quarter = lane >> 4, kw = (a.K + 31) >> 5;
+    const int tm = int(blockIdx.y), n0 = int(blockIdx.x) * (16 * FN), m = tm * kSmallRows + r16;
 
     // Block b: columns n0 + 16 (b % FN) of half b / FN.
     for (int c = tid; c < BLOCKS * 16; c += blockDim.x) {
@@ -262,9 +267,9 @@ __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a)
         bias_s[c] = col < a.N && a.bias ? a.bias[at] : 0.0f;
     }
     const Widening<O> minus_weights;
-    const E* const xrow = static_cast<const E*>(a.x) + int64_t(min(r16, a.M - 1)) * a.ld_x;
+    const E* const xrow = static_cast<const E*>(a.x) + int64_t(min(m, a.M - 1)) * a.ld_x;
     v4f_t acc[BLOCKS] = {};
-    for (int64_t k0 = int64_t(wave) * kFewRowsRunK; k0 < a.K; k0 += int64_t(waves) * kFewRowsRunK) {
+    for (int64_t k0 = int64_t(wave) * kSmallRunK; k0 < a.K; k0 += int64_t(waves) * kSmallRunK) {
         const int64_t k = k0 + 128 * quarter;
         const int w0 = int(k >> 5);
         uint4 w[BLOCKS];
@@ -275,7 +280,7 @@ __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a)
             else w[b] = make_uint4(row[min(w0, kw - 1)], row[min(w0 + 1, kw - 1)], row[min(w0 + 2, kw - 1)], 0u);
         }
         typename Vec8<E>::type xv[16];
-        if (k0 + kFewRowsRunK <= a.K) {
+        if (k0 + kSmallRunK <= a.K) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 xv[i] = *reinterpret_cast<const typename Vec8<E>::any*>((ODD ? word_begin(xrow) : xrow) + k + 8 * i);
@@ -302,15 +307,15 @@ __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a)
             }
         }
     }
-    // Lane: columns 4 quarter .. 4 quarter + 3 of row r16 of each block.
-    if (r16 < a.M) {
+    // Lane: columns 4 quarter .. 4 quarter + 3 of row m of each block.
+    if (m < a.M) {
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) part_s[(wave * BLOCKS + b) * 64 + lane] = make_float4(acc[b][0], acc[b][1], acc[b][2], acc[b][3]);
     }
     __syncthreads();
     for (int f = wave; f < FN; f += waves) {
-        if (r16 >= a.M) continue;
-        float s[HALVES][4] = {}, none_s[HALVES][4] = {}, none_z[HALVES][4] = {};
+        if (!BACK && m >= a.M) continue;           // backwards all lanes are in the sums, those of no row with nothing
+        float s[HALVES][4] = {}, sum_s[HALVES][4] = {}, sum_z[HALVES][4] = {};
         const float *scale[HALVES], *bias[HALVES];
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
@@ -324,24 +329,41 @@ __global__ __launch_bounds__(512) void bits_few_rows_kernel(const ProductArgs a)
                 s[h][3] -= p.w;
             }
         }
-        finish<E, EPI, 4>(a, r16, n0 + f * 16 + 4 * quarter, s, scale, bias, none_s, none_z);
+        finish<E, EPI, 4>(a, m, n0 + f * 16 + 4 * quarter, s, scale, bias, sum_s, sum_z);
+        if constexpr (BACK) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int off = 8; off > 0; off >>= 1) {
+                        sum_s[h][i] += __shfl_xor(sum_s[h][i], off);
+                        sum_z[h][i] += __shfl_xor(sum_z[h][i], off);
+                    }
+                    const int col = n0 + f * 16 + 4 * quarter + i;
+                    if (r16 != 0 || col >= a.N) continue;
+                    const int64_t at = int64_t(tm) * a.channels + int64_t(h) * a.N + col;
+                    if (a.part_scale) a.part_scale[at] = sum_s[h][i];
+                    if (a.part_bias) a.part_bias[at] = sum_z[h][i];
+                }
+        }
     }
 }
 
 template <typename E, int EPI, int FN>
-int launch_few_rows(const ProductArgs& a, int waves, hipStream_t s) {
-    const int64_t blocks = ceil_div(a.N, 16 * FN);
-    if (blocks > max_blocks(64 * waves)) return BNN_ERR_UNSUPPORTED;
-    const dim3 grid{uint32_t(blocks)}, block{uint32_t(64 * waves)};
+int launch_small(const ProductArgs& a, int waves, hipStream_t s) {
+    const int64_t blocks = ceil_div(kBackward<EPI> ? a.half : a.N, 16 * FN), tiles_m = ceil_div(a.M, kSmallRows);
+    if (blocks * tiles_m > max_blocks(64 * waves) || tiles_m > 65535) return BNN_ERR_UNSUPPORTED;
+    const dim3 grid{uint32_t(blocks), uint32_t(tiles_m)}, block{uint32_t(64 * waves)};
     const size_t lds = size_t(waves) * FN * kHalves<EPI> * 1024;
     if constexpr (!is_f32<E>) {
         // Up to four rows are few lines, and the extra word costs more (1 x 4095 -> 4096: 4.4 us against 4.9).
-        if (a.M > 4 && odd_rows<E>(a, 2 * kFewRowsRunK)) {
-            bits_few_rows_kernel<E, EPI, FN, true><<<grid, block, lds, s>>>(a);
+        if (a.M > 4 && odd_rows<E>(a, 2 * kSmallRunK)) {
+            bits_small_kernel<E, EPI, FN, true><<<grid, block, lds, s>>>(a);
             return check_launch();
         }
     }
-    bits_few_rows_kernel<E, EPI, FN, false><<<grid, block, lds, s>>>(a);
+    bits_small_kernel<E, EPI, FN, false><<<grid, block, lds, s>>>(a);
     return check_launch();
 }
 

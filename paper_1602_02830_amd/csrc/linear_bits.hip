@@ -22,7 +22,7 @@ namespace {
 template <int EPI>
 int forward(int type, const ProductArgs& a, void* stream) {
     int status = BNN_ERR_INVALID_ARG;
-    const Form form = product_form(type == BNN_F32, true, a.M, int64_t(a.N) * kHalves<EPI>);
+    const Form form = product_form(type == BNN_F32, a.M, a.N, kHalves<EPI>);
     with_type(type, [&](auto e) { status = launch_form<decltype(e), EPI>(a, form, static_cast<hipStream_t>(stream)); });
     return status;
 }

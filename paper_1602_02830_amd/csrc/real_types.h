@@ -99,30 +99,11 @@ __device__ inline void store8(E* p, const float (&v)[8], int64_t valid) {
     store_group<E, 8>(p, v, valid);
 }
 
-// The same with W of the eight, as plain floats.
 template <typename E, int W>
 __device__ inline void load_some(const E* p, int64_t valid, float (&v)[W]) {
-    typename Vec8<E>::type q = {};
-    if constexpr (W == 8) {
-        q = load8<E>(p, valid);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (i < valid) q[i] = p[i];
-    }
+    const auto q = load_group<E, W>(p, valid);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = float(q[i]);
-}
-
-template <typename E, int W>
-__device__ inline void store_some(E* p, const float (&v)[W], int64_t valid) {
-    if constexpr (W == 8) {
-        store8<E>(p, v, valid);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (i < valid) p[i] = E(v[i]);
-    }
 }
 
 // ---- activations, float32 --------------------------------------------------------------------------------------
