@@ -425,7 +425,8 @@ int bnn_gated_bits_backward(int type, const void *dh, int64_t ld_dh, const void 
  *   y, x (or NULL: 0), r, n [M][ld] of `type`, rows of D; gate [ceil(M / rows_per_gate)][ld_gate] of `type` or NULL (1);
  *   post, pre: bnn_norm, with gamma [D] or NULL (1) and beta [D] or NULL (0; only with BNN_NORM_LAYER).
  * r may be NULL (not wanted) or x itself (same address and leading dimension); n must be NULL exactly if pre is
- * BNN_NORM_NONE.  n is taken of the unrounded r.  rows_per_gate >= 1 also where gate is NULL.
+ * BNN_NORM_NONE.  n is taken of the unrounded r.  rows_per_gate >= 1 also where gate is NULL.  Rows longer than 16384
+ * elements are BNN_ERR_UNSUPPORTED, here and backwards: a workgroup holds a row in its registers.
  */
 int bnn_norm_residual(int type, const void *y, int64_t ld_y, const void *x, int64_t ld_x, const void *gate,
                       int64_t ld_gate, int64_t rows_per_gate, float res_scale, int post, const float *post_gamma,

@@ -3,6 +3,8 @@
 //   1. the gradient before the scale, ds = dz * scale, in the activations' type.  With an activation (or a gate) the product
 //      of the forward pass is made again and its epilogue turns the sums into ds and the column sums for dscale and dbias
 //      while they are in registers; without one, dz is dy: a pass over dy makes ds and dbias (nothing at all without a scale).
+//      Rounding ds to 16 bits is what lets the next two products run on 16-bit matrix instructions, and halves its way through
+//      memory; their sums, and the column sums, which are taken before it, have 32 bits.
 //   2. dx = ds w: the same tile product as forwards, on the weights' bits transposed (a 16th or a 32nd of an operand's bytes).
 //   3. dw = ds^T x.  Without an activation it is made of dy itself, the scale put on the sums, and
 //      dscale[n] = sum_k w[n][k] sum_m dy[m][n] x[m][k] comes out of the same sums.

@@ -245,12 +245,6 @@ __device__ inline uint32_t spread_high(uint32_t w) {
     return b | (b << 15);
 }
 
-// One byte of a word: 8 elements.
-__device__ inline uint32_t spread_byte(uint32_t w, int byte) {
-    const uint32_t b = __builtin_amdgcn_ubfe(w, 8 * byte, 8);
-    return b | (b << 15);
-}
-
 __device__ inline v16f_t mfma16(Vec8<bf16_t>::type a, Vec8<bf16_t>::type b, v16f_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
