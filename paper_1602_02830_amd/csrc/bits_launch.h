@@ -71,9 +71,9 @@ int launch_form(const ProductArgs& a, Form form, hipStream_t s) {
     }
     if (form == kWavesForm) {
         const int waves = int(a.K >= 4 * kRunK ? 4 : a.K <= kRunK ? 1 : ceil_div(a.K, kRunK));
-        // 128 channels a tile where there is one for every compute unit and K is long (256 x 4096 x 4096: 15.5 us against 21;
-        // 64 x 4096 x 8192, 64 tiles: 23.5 against 20.3).
-        if (!is_f32<E> && a.K >= 2048 && ceil_div(a.M, 32) * ceil_div(int64_t(a.N) * HALVES, 128) >= 256)
+        // 128 channels a tile where there are more tiles of 64 than compute units and a run for every wavefront (154 x 4942 ->
+        // 5199: 16.5 us against 21.7; 64 x 4096 -> 8192, 256 tiles of 64: 14.5 against 12.1; 500 x 784 -> 3062: 8.8 against 7.9).
+        if (!is_f32<E> && a.K >= 4 * kRunK && ceil_div(a.M, 32) * ceil_div(int64_t(a.N) * HALVES, 64) > 256)
             return launch_waves<E, EPI, 1, 4>(a, waves, s);
         return launch_waves<E, EPI, 1, 2>(a, waves, s);
     }

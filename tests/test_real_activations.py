@@ -329,6 +329,20 @@ def test_linear_backward_large_tiles(M, N, K, act, T):
 
 @gpu
 @pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M,F,K", [(200, 1500, 1101), (90, 2900, 1300)])
+def test_products_in_tiles_of_128_channels_without_lds(M, F, K, T):
+    T = TYPES[T]
+    p = Product(M, 2 * F, K, T, seed=15)
+    close(bnn.linear_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_GELU), *linear_want(p, "gelu"), "linear")
+    close(bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU), *gated_want(p, "silu"), "gated")
+    for gated in (False, True):
+        dy = torch.randn(M, F if gated else 2 * F, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+        f = bnn.gated_bits_backward if gated else bnn.linear_bits_backward
+        check_backward(p, "silu", gated, dy, f(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU))
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
 @pytest.mark.parametrize("act", ["none", "silu"])
 @pytest.mark.parametrize("M,N,K", [(6000, 300, 521), (9001, 131, 255), (700, 300, 200), (2100, 1030, 260)])
 def test_linear_backward_parts_of_the_rows(M, N, K, act, T):
