@@ -403,7 +403,8 @@ int bnn_gated_bits(int type, const void *x, int64_t ld_x, const uint32_t *w, int
  *                                backward propagation's g_W)
  *   dscale[n] = sum_m dz s,  dbias[n] = sum_m dz     float32
  * (dresidual is dy.)  Any of dx, dw, dscale, dbias may be NULL: not wanted.  dz * scale is rounded to `type` before the two
- * products that read it.  Sums over rows are made in an order that depends on the sizes alone.
+ * products that read it (float16: times a power of two, from the largest finite magnitudes of the operands, that keeps it
+ * among the normal numbers, and that both products' sums are divided by).  Sums over rows are made in an order that depends on the sizes alone.
  * workspace: 16-byte aligned device memory of at least the bytes that the _workspace function returns for the same sizes
  * (-1 for sizes or a type that the call would refuse); what it holds before and after means nothing.
  */

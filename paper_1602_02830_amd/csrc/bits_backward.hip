@@ -4,7 +4,8 @@
 //      of the forward pass is made again and its epilogue turns the sums into ds and the column sums for dscale and dbias
 //      while they are in registers; without one, dz is dy: a pass over dy makes ds and dbias (nothing at all without a scale).
 //      Rounding ds to 16 bits is what lets the next two products run on 16-bit matrix instructions, and halves its way through
-//      memory; their sums, and the column sums, which are taken before it, have 32 bits.
+//      memory; their sums, and the column sums, which are taken before it, have 32 bits.  float16 gradients are stored times a power
+//      of two (stored_gradient.h) whose bounds are looked up first, in the launch that transposes the weights.
 //   2. dx = ds w: the same tile product as forwards, on the weights' bits transposed (a 16th or a 32nd of an operand's bytes).
 //   3. dw = ds^T x.  Without an activation it is made of dy itself, the scale put on the sums, and
 //      dscale[n] = sum_k w[n][k] sum_m dy[m][n] x[m][k] comes out of the same sums.
@@ -23,35 +24,81 @@ namespace {
 // A workgroup turns 256 rows x 128 columns: each half wavefront blocks of 32 x 32 in registers, LDS puts words of a row together.
 constexpr int kTurnWords = 8, kTurnK = 128;
 
-__global__ __launch_bounds__(256) void transpose_weights_kernel(const uint32_t* w, int64_t ld_w, int F, int half, int halves, int K,
-                                                                uint32_t* out, int64_t ld_out, int blocks_k) {
+struct TurnArgs {
+    const uint32_t* w;
+    uint32_t* out;
+    int64_t ld_w, ld_out;
+    int F, half, halves, K, blocks_k;
+    int blocks;                // workgroups that transpose; 0: none is wanted
+};
+
+__device__ inline void transpose_weights(const TurnArgs& a) {
     __shared__ uint32_t turned[kTurnK][kTurnWords + 1];
     const int tid = threadIdx.x, half_wave = tid >> 5, l = tid & 31;
-    const int bn = blockIdx.x / uint32_t(blocks_k), bk = int(blockIdx.x) - bn * blocks_k;
-    const int word0 = bn * kTurnWords, k0 = bk * kTurnK, words = half * halves / 32, kw = (K + 31) >> 5;
+    const int bn = blockIdx.x / uint32_t(a.blocks_k), bk = int(blockIdx.x) - bn * a.blocks_k;
+    const int word0 = bn * kTurnWords, k0 = bk * kTurnK, words = a.half * a.halves / 32, kw = (a.K + 31) >> 5;
 #pragma unroll
     for (int i = 0; i < kTurnWords * 4 / 8; ++i) {
         const int b = i * 8 + half_wave, wn = b >> 2, q = b & 3;
-        const int c = (word0 + wn) * 32 + l, second = c >= half ? 1 : 0, f = c - second * half;
+        const int c = (word0 + wn) * 32 + l, second = c >= a.half ? 1 : 0, f = c - second * a.half;
         const int kword = (k0 >> 5) + q;
         uint32_t v = 0;
-        if (word0 + wn < words && f < F && kword < kw) v = w[(int64_t(second) * F + f) * ld_w + kword];
+        if (word0 + wn < words && f < a.F && kword < kw) v = a.w[(int64_t(second) * a.F + f) * a.ld_w + kword];
         turned[q * 32 + l][wn] = transpose_bits_32_lanes(v);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTurnK * kTurnWords / 256; ++i) {
         const int id = i * 256 + tid, row = id / kTurnWords, wn = id % kTurnWords;
-        if (k0 + row < K && word0 + wn < words) out[int64_t(k0 + row) * ld_out + word0 + wn] = turned[row][wn];
+        if (k0 + row < a.K && word0 + wn < words) a.out[int64_t(k0 + row) * a.ld_out + word0 + wn] = turned[row][wn];
     }
+}
+
+// ---- bounds of float16 gradients (stored_gradient.h) ---------------------------------------------------------------
+
+struct BoundArgs {
+    const f16_t *dy, *x;
+    const float *scale, *bias;
+    float* parts;              // as GradientBounds has them
+    int64_t ld_dy, ld_x, M;
+    int cols, K, channels;
+    int of_dy, of_x;
+    int blocks;                // workgroups that look, one at the scale, one at the bias, then at dy and x; 0: none
+};
+
+__device__ inline void look_for_bounds(const BoundArgs& a, int block) {
+    __shared__ float wave_s[4];
+    const uint32_t tid = threadIdx.x;
+    float m = block == 0 && !a.scale ? 1.0f : 0.0f;
+    if (block < 2) {
+        const float* const v = block == 0 ? a.scale : a.bias;
+        if (v) m = largest_of_matrix(v, 0, 1, a.channels, tid, 256);
+    } else if (block < 2 + a.of_dy) {
+        m = largest_of_matrix(a.dy, a.ld_dy, a.M, a.cols, uint32_t(block - 2) * 256 + tid, uint32_t(a.of_dy) * 256);
+    } else {
+        m = largest_of_matrix(a.x, a.ld_x, a.M, a.K, uint32_t(block - 2 - a.of_dy) * 256 + tid, uint32_t(a.of_x) * 256);
+    }
+    m = largest_of_wave(m);
+    if ((tid & 63) == 0) wave_s[tid >> 6] = m;
+    __syncthreads();
+    if (tid == 0) a.parts[block] = fmaxf(fmaxf(wave_s[0], wave_s[1]), fmaxf(wave_s[2], wave_s[3]));
+}
+
+// What the products need and what does not wait for them, in one launch: workgroups that transpose, then those that look.
+__global__ __launch_bounds__(256) void prepare_kernel(const TurnArgs t, const BoundArgs b) {
+    if (int(blockIdx.x) < t.blocks) transpose_weights(t);
+    else look_for_bounds(b, int(blockIdx.x) - t.blocks);
 }
 
 // ---- dy * scale and the column sums of dy ------------------------------------------------------------------------
 // A workgroup takes `strip` rows x 512 columns, a thread eight columns of every fourth row.
 template <typename E>
 __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t ld_dy, const float* scale, E* ds, int64_t ld_ds,
-                                                            float* part, int M, int N, int strip, int blocks_n) {
+                                                            float* part, int M, int N, int strip, int blocks_n,
+                                                            const GradientBounds bounds, float* unit_out) {
     __shared__ float sums_s[4][512];
+    const float factor = StoredFactor<false>(bounds)(0, BNN_ACT_NONE);
+    if (unit_out && blockIdx.x == 0 && threadIdx.x == 0) *unit_out = 1.0f / factor;
     const int tid = threadIdx.x, c = tid & 63, r = tid >> 6;
     const int bm = blockIdx.x / uint32_t(blocks_n), bn = int(blockIdx.x) - bm * blocks_n;
     const int n = bn * 512 + c * 8;
@@ -65,7 +112,7 @@ __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             sum[i] += float(v[i]);
-            o[i] = float(v[i]) * sc[i];
+            o[i] = float(v[i]) * sc[i] * factor;
         }
         if (ds && n < ld_ds) store8<E>(ds + m * ld_ds + n, o, 8);
     }
@@ -130,18 +177,19 @@ struct GradPlan {
 // Everything a call puts into its workspace, by sizes alone.  cols: columns of dy (gated: F).
 struct Plan {
     int64_t half, halves, ds_cols, wt_ld, strip, part_rows;
-    int64_t ds_at, wt_at, scale_at, bias_at, pieces_at, bytes;
+    int64_t ds_at, wt_at, scale_at, bias_at, pieces_at, bounds_at, unit_at, bytes;
     Form form;
     bool recompute;
     GradPlan grad;
-    Plan(int64_t size, int64_t M, int64_t cols, int64_t K, int act, bool gated)
-        : recompute(gated || act != BNN_ACT_NONE), grad(size == 4, M, recompute ? round_up(cols, 64) * (gated ? 2 : 1) : cols, gated ? 2 * cols : cols, K) {
+    Plan(int type, int64_t M, int64_t cols, int64_t K, int act, bool gated)
+        : recompute(gated || act != BNN_ACT_NONE), grad(type == BNN_F32, M, recompute ? round_up(cols, 64) * (gated ? 2 : 1) : cols, gated ? 2 * cols : cols, K) {
+        const int64_t size = type_bytes(type);
         halves = gated ? 2 : 1;
         half = round_up(cols, 64);
         ds_cols = half * halves;
         wt_ld = round_up(ds_cols / 32, 4);
         const int64_t channels = halves * cols;
-        form = product_form(size == 4, M, cols, int(halves));
+        form = product_form(type == BNN_F32, M, cols, int(halves));
         strip = round_up(ceil_div(M > 0 ? M : 1, kStrips), 4);
         // Tiles of a form with 64-bit offsets have 128 rows: never more of them than of the smaller of the two.
         const int64_t rows = rows_of_form(form);
@@ -158,6 +206,8 @@ struct Plan {
         scale_at = take(scale_rows * channels * 4);
         bias_at = take(part_rows * channels * 4);
         pieces_at = take(grad.splits > 1 ? grad.splits * channels * K * 4 : 0);
+        bounds_at = take(type == BNN_F16 ? kMostBoundParts * int64_t(sizeof(float)) : 0);
+        unit_at = take(type == BNN_F16 ? int64_t(sizeof(float)) : 0);
     }
 };
 
@@ -206,17 +256,45 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
     join.N = int(channels);
     const void* g = ds;                // what dx is made of
     int64_t ld_g = p.ds_cols, cols_g = p.ds_cols, part_rows = p.part_rows;
+    const bool make_ds = p.recompute || (scale && dx);
+    TurnArgs turn{};
+    if (dx && M > 0 && K > 0 && cols > 0) {
+        const int64_t blocks_n = ceil_div(p.ds_cols / 32, kTurnWords), blocks_k = ceil_div(K, kTurnK);
+        if (blocks_n * blocks_k > max_blocks(256) - kMostBoundParts) return BNN_ERR_UNSUPPORTED;
+        turn = TurnArgs{w, wt, ld_w, p.wt_ld, int(cols), int(p.half), int(p.halves), int(K), int(blocks_k), int(blocks_n * blocks_k)};
+    }
+    GradientBounds bounds{};
+    float* unit = nullptr;             // one over what ds is multiplied with, where it is
+    BoundArgs look{};
+    if constexpr (std::is_same<E, f16_t>::value) {
+        if (make_ds && (dx || dw) && M > 0 && K > 0 && cols > 0) {
+            float* const parts = reinterpret_cast<float*>(ws + p.bounds_at);
+            // Four groups of eight elements a thread, as far as there are workgroups.
+            auto workgroups = [&](int64_t columns) {
+                const int64_t n = ceil_div(M * ceil_div(columns, 8), 1024);
+                return int(n < kMostLookers ? n : kMostLookers);
+            };
+            bounds = GradientBounds{parts, workgroups(cols), gated ? workgroups(K) : 0};
+            unit = reinterpret_cast<float*>(ws + p.unit_at);
+            look = BoundArgs{static_cast<const E*>(dy), static_cast<const E*>(x), scale, bias, parts, ld_dy, ld_x, M, int(cols), int(K),
+                             int(channels), bounds.of_dy, bounds.of_x, 2 + bounds.of_dy + bounds.of_x};
+        }
+    }
+    if (turn.blocks + look.blocks > 0) {
+        prepare_kernel<<<dim3(uint32_t(turn.blocks + look.blocks)), dim3(256), 0, s>>>(turn, look);
+        if ((st = check_launch()) != BNN_OK) return st;
+    }
     if (p.recompute && M > 0 && cols > 0) {
         ProductArgs a{};
         a.x = x; a.ld_x = ld_x; a.w = w; a.ld_w = ld_w; a.scale = scale; a.bias = bias; a.act = act;
         a.dy = dy; a.ld_dy = ld_dy; a.y = ds; a.ld_y = p.ds_cols; a.half = int(p.half); a.channels = int(channels);
         a.part_scale = dscale ? part_scale : nullptr;
         a.part_bias = dbias ? part_bias : nullptr;
+        a.bounds = bounds; a.unit_out = unit;
         a.M = int(M); a.N = int(cols); a.K = int(K);
         part_rows = ceil_div(M, rows_of_tile<E>(p.form, ld_x));
         st = gated ? launch_form<E, kGatedBack>(a, p.form, s) : launch_form<E, kLinearBack>(a, p.form, s);
     } else if (!p.recompute) {
-        const bool make_ds = scale && dx;
         if (!make_ds) {
             g = dy;
             ld_g = ld_dy;
@@ -227,21 +305,14 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
             if (p.part_rows * blocks_n > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
             scale_and_sum_kernel<E><<<dim3(uint32_t(p.part_rows * blocks_n)), dim3(256), 0, s>>>(
                 static_cast<const E*>(dy), ld_dy, scale, make_ds ? ds : nullptr, p.ds_cols, dbias ? part_bias : nullptr, int(M),
-                int(cols), int(p.strip), int(blocks_n));
+                int(cols), int(p.strip), int(blocks_n), bounds, unit);
             st = check_launch();
         }
     }
     if (st != BNN_OK) return st;
     if (dx && M > 0 && K > 0) {
-        if (cols > 0) {
-            const int64_t blocks_n = ceil_div(p.ds_cols / 32, kTurnWords), blocks_k = ceil_div(K, kTurnK);
-            if (blocks_n * blocks_k > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
-            transpose_weights_kernel<<<dim3(uint32_t(blocks_n * blocks_k)), dim3(256), 0, s>>>(
-                w, ld_w, int(cols), int(p.half), int(p.halves), int(K), wt, p.wt_ld, int(blocks_k));
-            if ((st = check_launch()) != BNN_OK) return st;
-        }
         ProductArgs a{};
-        a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx;
+        a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx; a.unit = unit;
         a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
         if ((st = launch_form<E, kLinear>(a, product_form(is_f32<E>, M, K, 1), s)) != BNN_OK) return st;
     }
@@ -251,6 +322,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         a.g = p.recompute ? ds : dy; a.ld_g = p.recompute ? p.ds_cols : ld_dy;
         a.x = x; a.ld_x = ld_x; a.dw = dw; a.ld_dw = ld_dw;
         a.row_scale = p.recompute ? nullptr : scale;
+        a.unit = p.recompute ? unit : nullptr;
         a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w;
         a.M = int(M); a.K = int(K); a.cols = int(p.recompute ? p.ds_cols : cols); a.half = int(p.half); a.F = int(cols);
         a.channels = int(channels);
@@ -288,7 +360,7 @@ int check_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64
     if (!aligned_to(dy, size) || !aligned_to(dx, size) || !aligned_to(dw, size) || !aligned_to(dscale, 4) || !aligned_to(dbias, 4) ||
         !aligned_to(ws, 16))
         return BNN_ERR_ALIGNMENT;
-    const int64_t need = Plan(size, M, cols, K, act, gated).bytes;
+    const int64_t need = Plan(type, M, cols, K, act, gated).bytes;
     if (ws_bytes < need || (need > 0 && !ws)) return BNN_ERR_INVALID_ARG;
     return BNN_OK;
 }
@@ -299,7 +371,7 @@ int run_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t
     int st = check_backward(type, dy, ld_dy, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M, cols, K,
                             gated, ws, ws_bytes);
     if (st != BNN_OK) return st;
-    const Plan p(type_bytes(type), M, cols, K, act, gated);
+    const Plan p(type, M, cols, K, act, gated);
     with_type(type, [&](auto e) {
         st = backward<decltype(e)>(p, gated, dy, ld_dy, x, ld_x, w, ld_w, scale, bias, act, dx, ld_dx, dw, ld_dw, dscale, dbias, M,
                                    cols, K, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
@@ -312,12 +384,12 @@ int run_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t
 
 extern "C" int64_t bnn_linear_bits_backward_workspace(int type, int64_t M, int64_t N, int64_t K, int act) {
     using namespace bnn;
-    return check_sizes(type, M, N, K, act, false) == BNN_OK ? Plan(type_bytes(type), M, N, K, act, false).bytes : -1;
+    return check_sizes(type, M, N, K, act, false) == BNN_OK ? Plan(type, M, N, K, act, false).bytes : -1;
 }
 
 extern "C" int64_t bnn_gated_bits_backward_workspace(int type, int64_t M, int64_t F, int64_t K, int act) {
     using namespace bnn;
-    return check_sizes(type, M, F, K, act, true) == BNN_OK ? Plan(type_bytes(type), M, F, K, act, true).bytes : -1;
+    return check_sizes(type, M, F, K, act, true) == BNN_OK ? Plan(type, M, F, K, act, true).bytes : -1;
 }
 
 extern "C" int bnn_linear_bits_backward(int type, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const uint32_t* w,

@@ -12,7 +12,7 @@
 #pragma once
 
 #include "gemm_staging.h"
-#include "real_types.h"
+#include "stored_gradient.h"
 
 namespace bnn {
 
@@ -32,6 +32,9 @@ struct ProductArgs {
     int channels;              // backward: rows of w
     int act;
     TileMap map;
+    const float* unit;         // what stands for the scale where there is none, or null: 1
+    GradientBounds bounds;     // backward, float16: what ds is multiplied with follows from them
+    float* unit_out;           // backward: gets one over that factor, or null
 };
 
 enum Epilogue {
@@ -49,10 +52,10 @@ template <int EPI>
 inline constexpr bool kBackward = EPI == kLinearBack || EPI == kGatedBack;
 
 // The epilogue of W = 8 (or 4) consecutive columns from n on of row m, from their sums (gated: of both halves).  scale, bias: of
-// the columns of each half.  Backwards, sum_s and sum_z grow by dz * s and dz.
+// the columns of each half.  Backwards, ds is stored times `factor`, and sum_s and sum_z grow by dz * s and dz.
 template <typename E, int EPI, int W>
 __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&s)[kHalves<EPI>][W], const float* const (&scale)[kHalves<EPI>],
-                              const float* const (&bias)[kHalves<EPI>], float (&sum_s)[kHalves<EPI>][W], float (&sum_z)[kHalves<EPI>][W]) {
+                              const float* const (&bias)[kHalves<EPI>], float factor, float (&sum_s)[kHalves<EPI>][W], float (&sum_z)[kHalves<EPI>][W]) {
     constexpr bool FAST = !is_f32<E>;
     constexpr int HALVES = kHalves<EPI>;
     E* const y = static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n;
@@ -96,7 +99,7 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
                 // A column that is not there counts nothing, whatever its sums are.
-                out[h][i] = i < valid ? dz[h] * scale[h][i] : 0.0f;
+                out[h][i] = i < valid ? dz[h] * scale[h][i] * factor : 0.0f;
                 sum_s[h][i] += i < valid ? dz[h] * s[h][i] : 0.0f;
                 sum_z[h][i] += i < valid ? dz[h] : 0.0f;
             }
@@ -106,6 +109,25 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
         for (int h = 0; h < HALVES; ++h) store_group<E, W>(y + int64_t(h) * a.half, out[h], W);
     }
 }
+
+// The factor of stored gradients, in the two halves of StoredFactor; the first workgroup leaves one over it for the products that read them.
+template <bool STORED, bool GATED>
+struct Factor {
+    StoredFactor<GATED> of;
+    __device__ inline explicit Factor(const ProductArgs& a) : of(a.bounds) {}
+    __device__ inline float operator()(const ProductArgs& a) const {
+        const float factor = of(a.K, a.act);
+        if (a.unit_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.unit_out = 1.0f / factor;
+        return factor;
+    }
+};
+template <bool GATED>
+struct Factor<false, GATED> {
+    __device__ inline explicit Factor(const ProductArgs&) {}
+    __device__ inline float operator()(const ProductArgs&) const { return 1.0f; }
+};
+template <typename E, int EPI>
+using FactorOf = Factor<std::is_same<E, f16_t>::value && kBackward<EPI>, EPI == kGatedBack>;
 
 // TN wavefronts along the channels, TM along the rows, 32-row blocks FN x FM for each.
 template <typename E, int EPI, int TM, int TN, int FM, int FN>
@@ -233,13 +255,16 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
 #pragma unroll
         for (int f = 0; f < FN; ++f) wf[f] = minus_weights(s < 2 ? spread_low(w[f]) : spread_high(w[f]), s & 1);
     };
+    const FactorOf<E, EPI> factor_parts(a);
+    float factor = 1.0f;
     auto load_scales = [&]() {
+        factor = factor_parts(a);
         for (int c = tid; c < S::CN; c += S::kThreads) {
             const int b = c >> 5, w_ = b / FN, f = b % FN;
             const int col = n0 + (GATED ? w_ * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : b * 32) + (c & 31);
             const int64_t row = int64_t(GATED && f >= FN / 2 ? a.N : 0) + col;
             const bool there = col < a.N;
-            scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
+            scale_s[c] = !there ? 1.0f : a.scale ? a.scale[row] : a.unit ? *a.unit : 1.0f;
             bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
         }
     };
@@ -349,7 +374,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
                         sums[h][4 * q + 2] = v.z;
                         sums[h][4 * q + 3] = v.w;
                     }
-                finish<E, EPI, 8>(a, m0 + (wm * FM + j) * 32 + row, block_col(f) + 8 * cq, sums, scale, bias, sum_s, sum_z);
+                finish<E, EPI, 8>(a, m0 + (wm * FM + j) * 32 + row, block_col(f) + 8 * cq, sums, scale, bias, factor, sum_s, sum_z);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }

@@ -74,12 +74,13 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
     tile_of_block(blockIdx.x, a.map, tm, tn);
     const int m0 = tm * S::BM, n0 = tn * S::BN, kw = (a.K + 31) >> 5;
 
+    const FactorOf<E, EPI> factor_parts(a);
     // Block f of the tile: columns n0 + 32 (f % FY) of half f / FY.
     for (int c = tid; c < S::CN; c += blockDim.x) {
         const int f = c >> 5, col = n0 + (f % FY) * 32 + (c & 31);
         const int64_t row = int64_t(f / FY) * a.N + col;
         const bool there = col < a.N;
-        scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
+        scale_s[c] = !there ? 1.0f : a.scale ? a.scale[row] : a.unit ? *a.unit : 1.0f;
         bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
     }
     const uint32_t* wrow[FN];
@@ -131,6 +132,7 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) load_x(wave, i);
     }
+    const float factor = factor_parts(a);                  // while those are on their way
     for (int r = wave; r < runs; r += waves) {
         uint4 wc[FN];
 #pragma unroll
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
             scale[h] = scale_s + c0 + 32 * FY * h;
             bias[h] = bias_s + c0 + 32 * FY * h;
         }
-        finish<E, EPI, 8>(a, m0 + j * 32 + fr, n0 + c0, sums, scale, bias, sum_s, sum_z);
+        finish<E, EPI, 8>(a, m0 + j * 32 + fr, n0 + c0, sums, scale, bias, factor, sum_s, sum_z);
         if constexpr (BACK) {
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
@@ -259,11 +261,12 @@ __global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
     const int r16 = lane & 15, quarter = lane >> 4, kw = (a.K + 31) >> 5;
     const int tm = int(blockIdx.y), n0 = int(blockIdx.x) * (16 * FN), m = tm * kSmallRows + r16;
 
+    const FactorOf<E, EPI> factor_parts(a);
     // Block b: columns n0 + 16 (b % FN) of half b / FN.
     for (int c = tid; c < BLOCKS * 16; c += blockDim.x) {
         const int b = c >> 4, col = n0 + (b % FN) * 16 + (c & 15);
         const int64_t at = int64_t(b / FN) * a.N + col;
-        scale_s[c] = col < a.N && a.scale ? a.scale[at] : 1.0f;
+        scale_s[c] = col >= a.N ? 1.0f : a.scale ? a.scale[at] : a.unit ? *a.unit : 1.0f;
         bias_s[c] = col < a.N && a.bias ? a.bias[at] : 0.0f;
     }
     const Widening<O> minus_weights;
@@ -307,6 +310,7 @@ __global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
             }
         }
     }
+    const float factor = factor_parts(a);
     // Lane: columns 4 quarter .. 4 quarter + 3 of row m of each block.
     if (m < a.M) {
 #pragma unroll
@@ -329,7 +333,7 @@ __global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
                 s[h][3] -= p.w;
             }
         }
-        finish<E, EPI, 4>(a, m, n0 + f * 16 + 4 * quarter, s, scale, bias, sum_s, sum_z);
+        finish<E, EPI, 4>(a, m, n0 + f * 16 + 4 * quarter, s, scale, bias, factor, sum_s, sum_z);
         if constexpr (BACK) {
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)

@@ -505,6 +505,49 @@ def test_products_repeat_and_take_other_streams():
     assert torch.equal(h, bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased))
 
 
+@gpu
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", ["none", "silu", "sigmoid"])
+@pytest.mark.parametrize("dy_std", [1e-3, 1e-4, 1e-5, 1e-6])
+@pytest.mark.parametrize("M,N,K", [(12, 1024, 200), (70, 2048, 130), (300, 4096, 96)])
+def test_float16_backward_keeps_small_gradients(M, N, K, dy_std, act, gated):
+    """dy far below 1 and a channel scale of 1/64: dz * scale lies among float16's subnormals, or below them.  The error is that of
+    roundings relative to 2^-11 alone (three times what independent ones give in the mean square), and of a result's own end."""
+    p = Product(M, N, K, torch.float16, seed=17)
+    p.scale = (torch.rand(N, generator=torch.Generator().manual_seed(5)) + 0.5) / 64
+    p.scaled = p.scale.to(DEV)
+    cols = N // 2 if gated else N
+    dy = torch.randn(M, cols, generator=torch.Generator().manual_seed(2)).mul_(dy_std).half()
+    call = bnn.gated_bits_backward if gated else bnn.linear_bits_backward
+    got = call(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act])
+    want, spread = backward_want(p, act, gated, dy)
+    for k in ("dx", "dw"):
+        err = (got[k].cpu().double() - want[k][0]).square().mean().sqrt()
+        bound = 3 * (spread[k].mean() + TINY[p.T] ** 2 / 3).sqrt() + 1e-6 * want[k][0].square().mean().sqrt()
+        assert err <= bound, (k, err.item(), bound.item(), want[k][0].square().mean().sqrt().item())
+
+
+@gpu
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_float16_backward_of_large_gradients(act, gated):
+    """Gradients up to float16's largest, an infinite one and a NaN in rows of their own: the others are as they are without them."""
+    M, N, K = 70, 64, 2000
+    p = Product(M, N, K, torch.float16, seed=19)
+    cols = N // 2 if gated else N
+    dy = torch.randn(M, cols, generator=torch.Generator().manual_seed(2)).mul_(1e4).clamp_(-65504, 65504).half()
+    dy[3, 5] = 65504.0
+    call = bnn.gated_bits_backward if gated else bnn.linear_bits_backward
+    got = call(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act])
+    check_backward(p, act, gated, dy, got, ("dx",))
+    dy[1, 2], dy[2, 7] = float("inf"), float("nan")
+    spoilt = call(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act])
+    assert not torch.isfinite(spoilt["dx"][1:3]).any()
+    want = backward_want(p, act, gated, dy)[0]["dx"]
+    rows = [0] + list(range(3, M))
+    close(spoilt["dx"][rows], want[0][rows], want[1][rows], "other rows")
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------
 
 class Norm:
