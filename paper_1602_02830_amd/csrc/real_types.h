@@ -136,7 +136,9 @@ __device__ inline void activate(int act, const float (&z)[W], float (&f)[W]) {
         case BNN_ACT_RELU: return all([](float v) { return v > 0.0f ? v : v != v ? v : 0.0f; });
         case BNN_ACT_SILU: return all([](float v) { return over<FAST>(v, 1.0f + exp_of<FAST>(-v)); });
         case BNN_ACT_SIGMOID: return all([](float v) { return over<FAST>(1.0f, 1.0f + exp_of<FAST>(-v)); });
-        case BNN_ACT_GELU: return all([](float v) { return 0.5f * v * (1.0f + erff(v * kSqrtHalf)); });
+        // 1 + erf(u) = erfc(-u): below zero the sum would cancel (at z = -5, 4 % of the result, and nothing is left from -5.5 on).
+        // The sum was faster where the epilogue counts: 4096 x 784 -> 2 x 4096 bfloat16 73 us, 77 with this.
+        case BNN_ACT_GELU: return all([](float v) { return 0.5f * v * erfcf(-v * kSqrtHalf); });
         // 0.5 z (1 + tanh u) = z / (1 + e^(-2u))
         case BNN_ACT_GELU_TANH:
             return all([](float v) { return over<FAST>(v, 1.0f + exp_of<FAST>(-kTwoSqrt2OverPi * (v + 0.044715f * v * v * v))); });
@@ -170,7 +172,7 @@ __device__ inline void activate_both(int act, const float (&z)[W], float (&f)[W]
             });
         case BNN_ACT_GELU:
             return all([](float v, float& y, float& dy) {
-                const float c = 0.5f * (1.0f + erff(v * kSqrtHalf));
+                const float c = 0.5f * erfcf(-v * kSqrtHalf);
                 y = v * c;
                 dy = c + v * kInvSqrt2Pi * exp_of<FAST>(-0.5f * v * v);
             });

@@ -548,6 +548,28 @@ def test_float16_backward_of_large_gradients(act, gated):
     close(spoilt["dx"][rows], want[0][rows], want[1][rows], "other rows")
 
 
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("act", ["gelu"])
+def test_tails_of_activations_keep_their_digits(act, T):
+    """One product of one element a row, so that z is exact.  Relative to the result: a few units of the functions, and what a unit in
+    the exponent's argument (z^2 / 2, or z) makes of them."""
+    T = TYPES[T]
+    z = torch.cat([torch.linspace(-12, 12, 193), torch.linspace(-3, 20, 47)]).to(T)
+    w = torch.ones(1, 1, dtype=torch.int32, device=DEV)
+    x = z.unsqueeze(1).to(DEV)
+    z64 = z.double().unsqueeze(1)
+    f, df = phi(z64, act)
+    df = df if act == "gelu" else torch.exp(-z64) / (1 + torch.exp(-z64)) ** 2
+    # Of the derivative of gelu's two terms, which have opposite signs below zero, the sum of the magnitudes.
+    size = 0.5 * torch.special.erfc(-z64 / math.sqrt(2)) + z64.abs() * torch.exp(-0.5 * z64 ** 2) / math.sqrt(2 * math.pi) if act == "gelu" else df
+    units = (16 + 2 * (z64 ** 2 if act == "gelu" else z64.abs())) * F32
+    close(bnn.linear_bits(x, w, act=ACTS[act]), f, rounded(f, units * f.abs(), T), act)
+    got = bnn.linear_bits_backward(torch.ones_like(x), x, w, act=ACTS[act])["dx"]
+    err = units * size
+    close(got, df, rounded(df, err + ROUND[T] * (df.abs() + err), T), "slope")
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------
 
 class Norm:
