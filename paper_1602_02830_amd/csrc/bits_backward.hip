@@ -84,9 +84,11 @@ __device__ inline void look_for_bounds(const BoundArgs& a, int block) {
     if (tid == 0) a.parts[block] = fmaxf(fmaxf(wave_s[0], wave_s[1]), fmaxf(wave_s[2], wave_s[3]));
 }
 
-// What the products need and what does not wait for them, in one launch: workgroups that transpose, then those that look.
+// What the products need and what does not wait for them, in one launch: workgroups that transpose, then those that look.  LOOK: there
+// are some, whose loads in flight take registers: 5 wavefronts a SIMD instead of 8.
+template <bool LOOK>
 __global__ __launch_bounds__(256) void prepare_kernel(const TurnArgs t, const BoundArgs b) {
-    if (int(blockIdx.x) < t.blocks) transpose_weights(t);
+    if (!LOOK || int(blockIdx.x) < t.blocks) transpose_weights(t);
     else look_for_bounds(b, int(blockIdx.x) - t.blocks);
 }
 
@@ -281,7 +283,9 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         }
     }
     if (turn.blocks + look.blocks > 0) {
-        prepare_kernel<<<dim3(uint32_t(turn.blocks + look.blocks)), dim3(256), 0, s>>>(turn, look);
+        const dim3 grid(uint32_t(turn.blocks + look.blocks)), block(256);
+        if (look.blocks > 0) prepare_kernel<true><<<grid, block, 0, s>>>(turn, look);
+        else prepare_kernel<false><<<grid, block, 0, s>>>(turn, look);
         if ((st = check_launch()) != BNN_OK) return st;
     }
     if (p.recompute && M > 0 && cols > 0) {

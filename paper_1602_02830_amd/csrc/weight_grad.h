@@ -18,7 +18,6 @@ struct WeightGradArgs {
     const void* x;             // [M][ld_x]
     void* dw;                  // [F or 2 F][ld_dw], or null: only the sums are wanted
     const float* row_scale;    // [F] or null
-    const float* unit;         // what stands for it where there is none, or null: 1
     const uint32_t* w;         // the weights' bits [F][ld_w] for dscale, or null
     float* part;               // [tiles_k][F]: sum over the tile's k of dw / row_scale * w
     float* pieces;             // [splits][F or 2 F][K]: float32 sums over a part of the rows each, instead of dw and part
@@ -29,6 +28,7 @@ struct WeightGradArgs {
     int channels;              // rows of dw
     int splits, split_rows;    // rows of M that a workgroup sums: a multiple of kGradStep
     TileMap map;
+    const float* unit;         // what stands for row_scale where there is none, or null: 1
 };
 
 constexpr int kGradStep = 32;          // rows a step
