@@ -167,8 +167,10 @@ __device__ inline void activate_both(int act, const float (&z)[W], float (&f)[W]
             });
         case BNN_ACT_SIGMOID:
             return all([](float v, float& y, float& dy) {
-                y = over<FAST>(1.0f, 1.0f + exp_of<FAST>(-v));
-                dy = y * (1.0f - y);
+                // 1 - s = e s, which keeps its digits where s is almost 1, and is infinity times 0 far below zero.
+                const float e = exp_of<FAST>(-v);
+                y = over<FAST>(1.0f, 1.0f + e);
+                dy = y * (v > 0.0f ? e * y : 1.0f - y);
             });
         case BNN_ACT_GELU:
             return all([](float v, float& y, float& dy) {

@@ -550,7 +550,7 @@ def test_float16_backward_of_large_gradients(act, gated):
 
 @gpu
 @pytest.mark.parametrize("T", TYPES)
-@pytest.mark.parametrize("act", ["gelu"])
+@pytest.mark.parametrize("act", ["gelu", "sigmoid"])
 def test_tails_of_activations_keep_their_digits(act, T):
     """One product of one element a row, so that z is exact.  Relative to the result: a few units of the functions, and what a unit in
     the exponent's argument (z^2 / 2, or z) makes of them."""
