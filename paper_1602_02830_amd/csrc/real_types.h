@@ -281,7 +281,11 @@ inline constexpr int kTermsOf = is_f32<E> ? 3 : 1;
 // A float32 is the sum of three bfloat16 exactly (24 significant bits, 8 each).  Each term is what is left cut off after 8
 // bits: all have the sign of the value, so no sum of some of them is larger than it and overflows where it does not.  An infinity
 // stays in the first term alone, and so does a NaN (whose upper half is kept from being an infinity's).
-template <typename E>
+//
+// NONZERO: for products of such terms with one another, where a term of zero would make a NaN of the other factor's infinity: no term of
+// a value that is not zero is.  A first or second term that leaves nothing is one unit smaller in its last place, so that the third
+// is below 2^-14 of the value, and an infinity has ones of its sign in its other terms.
+template <typename E, bool NONZERO = false>
 __device__ inline void terms_of(const typename Vec8<E>::type& v, typename Vec8<Operand<E>>::type (&t)[kTermsOf<E>]) {
     if constexpr (is_f32<E>) {
         v4u_t d[3];
@@ -292,9 +296,18 @@ __device__ inline void terms_of(const typename Vec8<E>::type& v, typename Vec8<O
             for (int e = 0; e < 2; ++e) {
                 const float x = v[2 * i + e];
                 top[e] = cut_off(x);
-                rest[e] = __builtin_fabsf(x) < __builtin_inff() ? x - top[e] : 0.0f;
-                top[e] = x != x ? x + x : top[e];
-                middle[e] = cut_off(rest[e]);
+                if constexpr (NONZERO) {
+                    const bool finite = __builtin_fabsf(x) < __builtin_inff();
+                    if (finite && top[e] == x && x != 0.0f) top[e] = __uint_as_float(__float_as_uint(x) - 0x10000u);
+                    rest[e] = finite ? x - top[e] : __builtin_copysignf(2.0f, x);
+                    top[e] = x != x ? x + x : top[e];
+                    middle[e] = cut_off(rest[e]);
+                    if (middle[e] == rest[e] && x != 0.0f) middle[e] = finite ? __uint_as_float(__float_as_uint(rest[e]) - 0x10000u) : 0.5f * rest[e];
+                } else {
+                    rest[e] = __builtin_fabsf(x) < __builtin_inff() ? x - top[e] : 0.0f;
+                    top[e] = x != x ? x + x : top[e];
+                    middle[e] = cut_off(rest[e]);
+                }
             }
             d[0][i] = upper_halves(top[0], top[1]);
             d[1][i] = upper_halves(middle[0], middle[1]);

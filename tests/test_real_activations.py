@@ -570,6 +570,33 @@ def test_tails_of_activations_keep_their_digits(act, T):
     close(got, df, rounded(df, err + ROUND[T] * (df.abs() + err), T), "slope")
 
 
+@gpu
+@pytest.mark.parametrize("M,N,K", [(40, 70, 90), (9001, 131, 255), (70, 5, 300)])
+def test_infinities_in_the_weights_gradient(M, N, K):
+    """float32: what an infinity is multiplied with has terms that are zero."""
+    p = Product(M, N, K, torch.float32, seed=23, scale=False, bias=False)
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2))
+    dy[2:6] = torch.tensor([1.0, -0.5, 0.75, 3.0]).unsqueeze(1)             # of few bits
+    dy[2, 1] = 0.0
+    inf = float("inf")
+    p.x[2, 7], p.x[3, 8], p.x[30, 9] = inf, -inf, inf                          # by the few bits, by any number
+    p.x[4, 10], p.x[5, 10] = inf, inf                                          # of one sign each: infinite
+    p.x[6], dy[6, 3], dy[31, 4] = 2.0, -inf, inf
+    p.x[6, 11], p.x[31, 12] = inf, 0.0
+    p.xd.copy_(p.x)
+    dw = bnn.linear_bits_backward(dy.to(DEV), p.xd, p.wd)["dw"].cpu().double()
+    want = dy.double().t() @ p.x.double()
+    assert torch.equal(torch.isnan(dw), torch.isnan(want)) and torch.isnan(want).any()
+    there = ~torch.isnan(want)
+    assert torch.equal(torch.isinf(dw[there]), torch.isinf(want[there])) and torch.isinf(want).sum() > 2 * N
+    inside = torch.isinf(want)
+    assert torch.equal(dw[inside], want[inside])
+    fin = torch.isfinite(want)
+    clean = torch.where(torch.isfinite(p.x), p.x, 0.0).double(), torch.where(torch.isfinite(dy), dy, 0.0).double()
+    tol = (M + 8) * F32 * (clean[1].abs().t() @ clean[0].abs())
+    close(dw[fin], want[fin], rounded(want[fin], tol[fin], torch.float32), "finite")
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------
 
 class Norm:
