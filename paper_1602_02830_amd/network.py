@@ -286,10 +286,10 @@ class BinaryFeedForward:
         self.gate, self.res_scale, self.eps = gate, float(res_scale), float(eps)
         self.grads = {}
         self.set_weights(w_in, w_out)
-        self._kept = None
 
     def set_weights(self, w_in, w_out):
-        """Packs the weights (again, after a training step)."""
+        """Packs the weights (again, after a training step).  What a forward() before has kept belongs to the old ones: dropped."""
+        self._kept = None
         self.w_in, self.w_out = B.pack_sign(w_in), B.pack_sign(w_out)
         self.scale_in, self.scale_out = w_in.abs().mean(1), w_out.abs().mean(1)
 

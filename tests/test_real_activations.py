@@ -866,6 +866,24 @@ def test_block_learns():
     assert min(losses[-10:]) < 0.8 * losses[0], losses[::10]
 
 
+def small_block(T=torch.bfloat16, gate=True, D=64, F=96):
+    g = torch.Generator().manual_seed(3)
+    w_in, w_out = (torch.randn(*s, generator=g).mul_(0.1).to(DEV) for s in ((2 * F, D), (D, F)))
+    gate = (1 + 0.1 * torch.randn(1, D, generator=g)).to(T).to(DEV) if gate else None
+    block = bnn.BinaryFeedForward(w_in, w_out, pre_gamma=torch.rand(D, generator=g).add_(0.5).to(DEV), gate=gate)
+    x = torch.randn(20, D, generator=g).to(T).to(DEV)
+    return block, x, (w_in, w_out)
+
+
+@gpu
+def test_block_with_new_weights_has_nothing_to_differentiate():
+    block, x, (w_in, w_out) = small_block()
+    r, after = block.forward(x, block.first_norm(x), keep=True)
+    block.set_weights(-w_in, w_out)
+    with pytest.raises(RuntimeError, match="forward"):
+        block.backward(torch.ones_like(r), torch.zeros_like(after))
+
+
 @gpu
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_a_captured_graph_replays_what_the_calls_compute(M):
