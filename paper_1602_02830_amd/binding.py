@@ -640,6 +640,12 @@ def _weights(x: torch.Tensor, w_bits: torch.Tensor):
         raise ValueError("packed weights have fewer words per row than x has columns")
 
 
+def _count_write(t: torch.Tensor | None):
+    """A caller's tensor is written: torch's count of that moves on, so that who kept the tensor can tell."""
+    if t is not None and not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _at(t: torch.Tensor | None):
     """Address and leading dimension of a matrix; (None, 0) where there is none."""
     return (None, 0) if t is None else (t.data_ptr(), _ld(t))
@@ -671,12 +677,14 @@ def linear_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | Non
     (M, K), N = x.shape, w_bits.shape[0]
     if residual is not None:
         _sized(residual, M, N, "residual", x)
+    given = out
     if out is None:
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
     _sized(out, M, N, "out", x)
     _check("bnn_linear_bits",
            lib.bnn_linear_bits(_TYPES[x.dtype], *_at(x), *_at(w_bits), _vector(scale, N, "scale", x), _vector(bias, N, "bias", x), act,
                                *_at(residual), *_at(out), M, N, K, _stream(x)))
+    _count_write(given)
     return out
 
 
@@ -698,12 +706,14 @@ def gated_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None
     _real(x, "x")
     _weights(x, w_bits)
     (M, K), F = x.shape, _halves(w_bits)
+    given = out
     if out is None:
         out = torch.empty((M, F), dtype=x.dtype, device=x.device)
     _sized(out, M, F, "out", x)
     _check("bnn_gated_bits",
            lib.bnn_gated_bits(_TYPES[x.dtype], *_at(x), *_at(w_bits), _vector(scale, 2 * F, "scale", x),
                               _vector(bias, 2 * F, "bias", x), act, *_at(out), M, F, K, _stream(x)))
+    _count_write(given)
     return out
 
 
@@ -784,6 +794,7 @@ def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Te
         if rows_per_gate < 1:
             raise ValueError("rows_per_gate must be positive")
         _sized(gate, -(-M // rows_per_gate), D, "gate", y)
+    given = out, out_n
     if out is None and need_r:
         out = torch.empty((M, D), dtype=y.dtype, device=y.device)
     if out is not None:
@@ -800,6 +811,8 @@ def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Te
                                  _vector(post_gamma, D, "post_gamma", y), _vector(post_beta, D, "post_beta", y), pre,
                                  _vector(pre_gamma, D, "pre_gamma", y), _vector(pre_beta, D, "pre_beta", y), eps,
                                  *_at(out), *_at(out_n), M, D, _stream(y)))
+    for t in given:
+        _count_write(t)
     return out, out_n
 
 

@@ -448,6 +448,11 @@ struct Weighted {
     }
 };
 
+// A caller's tensor is written: torch's count of that moves on, so that who kept the tensor can tell.
+void count_write(const Matrix& m) {
+    if (m.t && !m.t->is_inference()) m.t->unsafeGetTensorImpl()->bump_version();
+}
+
 // (x, w_bits, scale, bias, act, residual, out)
 PyObject* linear_bits(PyObject* const* a) {
     Weighted p;
@@ -456,6 +461,7 @@ PyObject* linear_bits(PyObject* const* a) {
     if (!p.read(a) || !small_integer(a[4], act) || !read_real(a[6], out, p.x.t, p.x.rows, p.w.rows) ||
         (a[5] != Py_None && !read_real(a[5], residual, p.x.t, p.x.rows, p.w.rows)))
         return long_way();
+    count_write(out);
     return launch(*out.t, [&](void* s) {
         return entry.linear_bits(p.type, p.x.data, p.x.ld, p.w.as<uint32_t>(), p.w.ld, p.scale, p.bias, act, residual.data,
                                  residual.ld, out.data, out.ld, p.x.rows, p.w.rows, p.x.cols, s);
@@ -469,6 +475,7 @@ PyObject* gated_bits(PyObject* const* a) {
     int act;
     if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[4], act) || !read_real(a[5], out, p.x.t, p.x.rows, p.w.rows / 2))
         return long_way();
+    count_write(out);
     return launch(*out.t, [&](void* s) {
         return entry.gated_bits(p.type, p.x.data, p.x.ld, p.w.as<uint32_t>(), p.w.ld, p.scale, p.bias, act, out.data, out.ld,
                                 p.x.rows, p.w.rows / 2, p.x.cols, s);
@@ -498,6 +505,8 @@ PyObject* norm_residual(PyObject* const* a) {
         !read_vector(a[9], D, *y.t, pre_beta) || !read_real(a[12], out, y.t, M, D) || (pre == 0) != (a[13] == Py_None) ||
         (a[13] != Py_None && !read_real(a[13], out_n, y.t, M, D)))
         return long_way();
+    count_write(out);
+    count_write(out_n);
     return launch(*out.t, [&](void* s) {
         return entry.norm_residual(real_type(y.t->scalar_type()), y.data, y.ld, x.data, x.ld, gate.data, gate.ld, rows_per_gate,
                                    res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, out.data, out.ld,

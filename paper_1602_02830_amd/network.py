@@ -261,6 +261,11 @@ class BinaryConvNet:
 
 
 
+def _writes(t: torch.Tensor):
+    """torch's count of the writes to a tensor (inference tensors have none)."""
+    return None if t.is_inference() else t._version
+
+
 class BinaryFeedForward:
     """One feed-forward block of a language model with one-bit weights on a real stream, with the norms, gate and
     residual scale around it:
@@ -269,8 +274,8 @@ class BinaryFeedForward:
 
     Weights are binarized with Eq. (1) and packed once; a channel's scale is the mean magnitude of its real weights.  forward()
     takes the stream and the normalised input that the block before made of it (first_norm() for the first block) and gives
-    those for the next one; with one row it is the block's form for single tokens.  backward() follows a forward() of the same
-    rows: the gradients of the real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights,
+    those for the next one; with one row it is the block's form for single tokens.  backward() is that of the last
+    forward(keep=True), whose n and r have to be as they were then (it raises if they were written over): the gradients of the real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights,
     here with the channel's scale, handed to the real ones), of scales, gammas and gate.
 
     w_in: float32 device weights [2F][D], the gate's rows first; w_out: [D][F]; gammas: float32 [D] or None (1);
@@ -303,14 +308,17 @@ class BinaryFeedForward:
         y = B.linear_bits(h, self.w_out, self.scale_out)
         r, after = B.norm_residual(y, x, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma,
                                    None, self.eps, max(x.shape[0], 1))
-        self._kept = (n, h, y, r) if keep else None
+        # n and r are the caller's, who may write over them before backward() (r in place is the next sum's documented place).
+        self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
         return r, after
 
     def backward(self, dr: torch.Tensor | None, dn_after: torch.Tensor):
         """Gradients of r (by every way but n') and of n' -> (dx, dn); the parameters' gradients are left in self.grads."""
         if self._kept is None:
             raise RuntimeError("backward() needs a forward(keep=True) before it")
-        n, h, y, r = self._kept
+        n, h, y, r, *writes = self._kept
+        if writes != [_writes(n), _writes(r)]:
+            raise RuntimeError("backward() needs the input n and the result r of forward(keep=True) as they were: one was written over")
         got = B.norm_residual_backward(dr, dn_after, y, r, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
                                        self.next_gamma, None, self.eps, max(y.shape[0], 1))
         out = B.linear_bits_backward(got["dy"], h, self.w_out, self.scale_out)

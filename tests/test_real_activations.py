@@ -885,6 +885,42 @@ def test_block_with_new_weights_has_nothing_to_differentiate():
 
 
 @gpu
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("which", ["n", "r", "a view of r"])
+def test_block_refuses_what_was_written_over(which, native, monkeypatch):
+    """The stream and the normalised input are the caller's: written over in between, they would give wrong gradients."""
+    block, x, _ = small_block()
+    if not native:
+        monkeypatch.setattr(binding, "_calls", None)
+    n = block.first_norm(x)
+    r, after = block.forward(x, n, keep=True)
+    dr, dn = torch.ones_like(r), torch.zeros_like(after)
+    block.backward(dr, dn)                                             # as they were: no complaint
+    if which == "n":
+        bnn.linear_bits(n, torch.ones(n.shape[1], 2, dtype=torch.int32, device=DEV), out=n.clone())       # read only
+        block.backward(dr, dn)
+        bnn.gated_bits(x, torch.ones(2 * n.shape[1], 2, dtype=torch.int32, device=DEV), out=n)
+    else:
+        out = r if which == "r" else r[3:7]
+        bnn.norm_residual(dr[:out.shape[0]], out, out=out)             # the documented place of the next sum
+    with pytest.raises(RuntimeError, match="written over"):
+        block.backward(dr, dn)
+
+
+@gpu
+def test_block_in_inference_mode():
+    block, x, _ = small_block()
+    want = block.forward(x, block.first_norm(x))
+    with torch.inference_mode():
+        y = x.clone()
+        got = block.forward(y, block.first_norm(y), keep=True)
+        assert bnn.norm_residual(y, y, out=y)[0] is y
+        block.backward(torch.ones_like(y), torch.zeros_like(y))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert bnn.norm_residual(x, x, out=y)[0] is y                      # an inference tensor outside of that mode
+
+
+@gpu
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_a_captured_graph_replays_what_the_calls_compute(M):
     """Forwards and backwards in one graph, replayed with other inputs in the same buffers, with eager work between."""
