@@ -275,8 +275,10 @@ class BinaryFeedForward:
     Weights are binarized with Eq. (1) and packed once; a channel's scale is the mean magnitude of its real weights.  forward()
     takes the stream and the normalised input that the block before made of it (first_norm() for the first block) and gives
     those for the next one; with one row it is the block's form for single tokens.  backward() is that of the last
-    forward(keep=True), whose n and r have to be as they were then (it raises if they were written over): the gradients of the real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights,
-    here with the channel's scale, handed to the real ones), of scales, gammas and gate.
+    forward(keep=True), whose n and r have to be as they were then (it raises if they were written over): the gradients of the
+    real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights, here with the channel's
+    scale, handed to the real ones), of scales, gammas and gate.  The norm that made n is the block's before, with its
+    next_gamma; that of first_norm() is differentiated by first_norm_backward().
 
     w_in: float32 device weights [2F][D], the gate's rows first; w_out: [D][F]; gammas: float32 [D] or None (1);
     gate: [1][D] in the stream's type, shared by all rows, or None.
@@ -301,6 +303,13 @@ class BinaryFeedForward:
     def first_norm(self, x: torch.Tensor) -> torch.Tensor:
         """pre(x): what the first block of a stack reads beside the stream."""
         return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, need_r=False)[1]
+
+    def first_norm_backward(self, x: torch.Tensor, dn: torch.Tensor, dr: torch.Tensor | None = None) -> torch.Tensor:
+        """The backward pass of first_norm(x), after backward(), whose (dx, dn) it takes as (dr, dn): the gradient of the stream x
+        by both ways; grads["pre_gamma"] is left beside the others."""
+        got = B.norm_residual_backward(dr, dn, x, x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, need_dx=False)
+        self.grads["pre_gamma"] = got["dpre_gamma"]
+        return got["dy"]
 
     def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
         """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""

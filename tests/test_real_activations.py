@@ -921,6 +921,36 @@ def test_block_in_inference_mode():
 
 
 @gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("M", [1, 50])
+def test_block_gradient_through_the_first_norm(M, T):
+    T = TYPES[T]
+    D, F = 96, 160
+    g = torch.Generator().manual_seed(M)
+    w_in, w_out = torch.randn(2 * F, D, generator=g) * 0.1, torch.randn(D, F, generator=g) * 0.1
+    gammas = [1 + 0.1 * torch.randn(D, generator=g) for _ in range(3)]
+    gate = (1 + 0.1 * torch.randn(1, D, generator=g)).to(T)
+    x, dr, dn = (torch.randn(M, D, generator=g).to(T) for _ in range(3))
+    block = bnn.BinaryFeedForward(w_in.to(DEV), w_out.to(DEV), bnn.ACT_SILU, *(v.to(DEV) for v in gammas), gate.to(DEV), 0.7)
+    xd = x.to(DEV)
+    block.forward(xd, block.first_norm(xd), keep=True)
+    dx, dn_in = block.backward(dr.to(DEV), dn.to(DEV))
+    total = block.first_norm_backward(xd, dn_in, dx)
+    alone = block.first_norm_backward(xd, dn_in)
+    d = lambda t: t.double().requires_grad_(True)
+    sign = lambda w: torch.where(w >= 0, 1.0, -1.0).double()
+    lx, lg = d(x), d(gammas[0])
+    n = norm64(lx, "rms", lg, None)
+    wr, wa = block64(lx, n, sign(w_in), sign(w_out), block.scale_in.cpu().double(), block.scale_out.cpu().double(), gate.double(),
+                     gammas[1].double(), gammas[2].double(), "silu")
+    ((wr * dr.double()).sum() + (wa * dn.double()).sum()).backward()
+    # As the block's other gradients, with two more roundings on the way: of n forwards and of its gradient backwards.
+    for got, want, what in ((total, lx.grad, "dx"), (block.grads["pre_gamma"], lg.grad, "pre_gamma"), (total - alone, dx.cpu().double(), "sum")):
+        err = (got.detach().cpu().double() - want).norm() / want.norm()
+        assert err <= 10 * ROUND[T] + 1e-5, (what, err)
+
+
+@gpu
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_a_captured_graph_replays_what_the_calls_compute(M):
     """Forwards and backwards in one graph, replayed with other inputs in the same buffers, with eager work between."""
