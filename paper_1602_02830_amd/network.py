@@ -311,11 +311,15 @@ class BinaryFeedForward:
         self.grads["pre_gamma"] = got["dpre_gamma"]
         return got["dy"]
 
+    def _gate_of(self, y: torch.Tensor):
+        """The gate's row for the rows of y: none for none."""
+        return self.gate if y.shape[0] else None
+
     def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
         """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""
         h = B.gated_bits(n, self.w_in, self.scale_in, None, self.act)
         y = B.linear_bits(h, self.w_out, self.scale_out)
-        r, after = B.norm_residual(y, x, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma,
+        r, after = B.norm_residual(y, x, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma,
                                    None, self.eps, max(x.shape[0], 1))
         # n and r are the caller's, who may write over them before backward() (r in place is the next sum's documented place).
         self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
@@ -328,10 +332,11 @@ class BinaryFeedForward:
         n, h, y, r, *writes = self._kept
         if writes != [_writes(n), _writes(r)]:
             raise RuntimeError("backward() needs the input n and the result r of forward(keep=True) as they were: one was written over")
-        got = B.norm_residual_backward(dr, dn_after, y, r, self.gate, self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
+        got = B.norm_residual_backward(dr, dn_after, y, r, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
                                        self.next_gamma, None, self.eps, max(y.shape[0], 1))
+        dgate = torch.zeros_like(self.gate) if self.gate is not None and y.shape[0] == 0 else got["dgate"]
         out = B.linear_bits_backward(got["dy"], h, self.w_out, self.scale_out)
         gated = B.gated_bits_backward(out["dx"], n, self.w_in, self.scale_in, None, self.act)
         self.grads = {"w_in": gated["dw"], "w_out": out["dw"], "scale_in": gated["dscale"], "scale_out": out["dscale"],
-                      "gate": got["dgate"], "post_gamma": got["dpost_gamma"], "next_gamma": got["dpre_gamma"]}
+                      "gate": dgate, "post_gamma": got["dpost_gamma"], "next_gamma": got["dpre_gamma"]}
         return got["dx"], gated["dx"]

@@ -951,6 +951,20 @@ def test_block_gradient_through_the_first_norm(M, T):
 
 
 @gpu
+@pytest.mark.parametrize("gate", [True, False])
+def test_block_without_rows(gate):
+    block, x, _ = small_block(gate=gate)
+    e = x[:0]
+    r, after = block.forward(e, block.first_norm(e), keep=True)
+    assert r.shape == after.shape == e.shape
+    dx, dn = block.backward(torch.empty_like(r), torch.empty_like(after))
+    assert dx.shape == dn.shape == e.shape
+    for k, v in block.grads.items():
+        assert (v is None) == (k in ("post_gamma", "next_gamma") or k == "gate" and not gate), k
+        assert v is None or not v.any(), k
+
+
+@gpu
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_a_captured_graph_replays_what_the_calls_compute(M):
     """Forwards and backwards in one graph, replayed with other inputs in the same buffers, with eager work between."""
