@@ -17,6 +17,7 @@ import warnings
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libbnn_hip.so")
@@ -663,14 +664,82 @@ def _workspace(workspace: torch.Tensor | None, size: int, like: torch.Tensor, fn
     return workspace
 
 
+def _recorded(*inputs) -> bool:
+    """Whether torch records what is done with these tensors."""
+    return any(t is not None and t.requires_grad for t in inputs) and torch.is_grad_enabled()
+
+
+class _LinearBits(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_bits, scale, bias, act, residual):
+        ctx.save_for_backward(x, w_bits, scale, bias)
+        ctx.act = act
+        return linear_bits(x, w_bits, scale, bias, act, residual)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return *_product_gradients(ctx, linear_bits_backward, dy), None, dy if ctx.needs_input_grad[5] else None
+
+
+class _GatedBits(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_bits, scale, bias, act):
+        ctx.save_for_backward(x, w_bits, scale, bias)
+        ctx.act = act
+        return gated_bits(x, w_bits, scale, bias, act)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh):
+        return *_product_gradients(ctx, gated_bits_backward, dh), None
+
+
+def _product_gradients(ctx, call, dy):
+    """Of x, w_bits (none: it holds bits), scale and bias."""
+    need_x, _, need_scale, need_bias = ctx.needs_input_grad[:4]
+    if not (need_x or need_scale or need_bias):
+        return None, None, None, None
+    got = call(dy.contiguous(), *ctx.saved_tensors, ctx.act, need_dx=need_x, need_dw=False)
+    return got["dx"], None, got["dscale"] if need_scale else None, got["dbias"] if need_bias else None
+
+
+class _NormResidual(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate):
+        r, n = norm_residual(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate)
+        ctx.save_for_backward(y, r if pre != NORM_NONE else None, gate, post_gamma, post_beta, pre_gamma, pre_beta)
+        ctx.kinds = res_scale, post, pre, eps, rows_per_gate
+        ctx.set_materialize_grads(False)
+        return r, n
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dr, dn):
+        if dr is None and dn is None:
+            return (None,) * 12
+        y, r, gate, post_gamma, post_beta, pre_gamma, pre_beta = ctx.saved_tensors
+        res_scale, post, pre, eps, rows_per_gate = ctx.kinds
+        if pre != NORM_NONE:
+            dn = torch.zeros_like(r) if dn is None else dn.contiguous()
+        got = norm_residual_backward(None if dr is None else dr.contiguous(), dn, y, r, gate, res_scale, post, post_gamma, post_beta,
+                                     pre, pre_gamma, pre_beta, eps, rows_per_gate, need_dx=ctx.needs_input_grad[1])
+        grads = (got["dy"], got["dx"], got["dgate"], None, None, got["dpost_gamma"], got["dpost_beta"], None, got["dpre_gamma"],
+                 got["dpre_beta"], None, None)
+        return tuple(g if need else None for g, need in zip(grads, ctx.needs_input_grad))
+
+
 def linear_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                 act: int = ACT_NONE, residual: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """bnn_linear_bits: real x [M][K], packed weights [N][ceil(K/32)] -> act(scale * (x w^T) + bias) + residual [M][N].
-    `out` may be `residual`."""
+    `out` may be `residual`.  Without `out`, torch differentiates the result with respect to x, scale, bias and residual (of the
+    packed weights linear_bits_backward gives a gradient); what is written to `out` is not recorded."""
     if out is not None and _calls is not None:
         st = _calls.linear_bits(x, w_bits, scale, bias, act, residual, out)
         if st == 0 or _took("bnn_linear_bits", st):
             return out
+    if out is None and _recorded(x, scale, bias, residual):
+        return _LinearBits.apply(x, w_bits, scale, bias, act, residual)
     lib = load_library()
     _real(x, "x")
     _weights(x, w_bits)
@@ -697,11 +766,13 @@ def _halves(w_bits: torch.Tensor) -> int:
 def gated_bits(x: torch.Tensor, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                act: int = ACT_SILU, out: torch.Tensor | None = None) -> torch.Tensor:
     """bnn_gated_bits: real x [M][K], packed weights [2F][ceil(K/32)] (the gate's rows first) -> act(z_gate) * z_up [M][F]
-    with z = scale * (x w^T) + bias."""
+    with z = scale * (x w^T) + bias.  Differentiated as linear_bits is."""
     if out is not None and _calls is not None:
         st = _calls.gated_bits(x, w_bits, scale, bias, act, out)
         if st == 0 or _took("bnn_gated_bits", st):
             return out
+    if out is None and _recorded(x, scale, bias):
+        return _GatedBits.apply(x, w_bits, scale, bias, act)
     lib = load_library()
     _real(x, "x")
     _weights(x, w_bits)
@@ -779,12 +850,16 @@ def norm_residual(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Te
                   eps: float = 1e-5, rows_per_gate: int = 1, out: torch.Tensor | None = None, out_n: torch.Tensor | None = None,
                   need_r: bool = True):
     """bnn_norm_residual: (r, n) with r = x + res_scale * gate * post(y) and n = pre(r); n is None without a `pre` norm, r where
-    it is not needed.  Row m has the gate's row m // rows_per_gate.  `out` may be `x`."""
+    it is not needed.  Row m has the gate's row m // rows_per_gate.  `out` may be `x`.  Without `out` and `out_n`, torch
+    differentiates both results with respect to every tensor; what is written to those two is not recorded."""
     if out is not None and _calls is not None:
         st = _calls.norm_residual(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
                                   out, out_n)
         if st == 0 or _took("bnn_norm_residual", st):
             return out, out_n
+    if out is None and out_n is None and _recorded(y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta):
+        r, n = _NormResidual.apply(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate)
+        return (r if need_r else None), n
     lib = load_library()
     _real(y, "y")
     M, D = y.shape

@@ -278,7 +278,8 @@ class BinaryFeedForward:
     forward(keep=True), whose n and r have to be as they were then (it raises if they were written over): the gradients of the
     real weights by the straight-through estimator (Alg. 1: the gradient of the binarized weights, here with the channel's
     scale, handed to the real ones), of scales, gammas and gate.  The norm that made n is the block's before, with its
-    next_gamma; that of first_norm() is differentiated by first_norm_backward().
+    next_gamma; that of first_norm() is differentiated by first_norm_backward().  torch's own differentiation does not see the block: of
+    the real weights it would know the scales alone.
 
     w_in: float32 device weights [2F][D], the gate's rows first; w_out: [D][F]; gammas: float32 [D] or None (1);
     gate: [1][D] in the stream's type, shared by all rows, or None.
@@ -294,16 +295,19 @@ class BinaryFeedForward:
         self.grads = {}
         self.set_weights(w_in, w_out)
 
+    @torch.no_grad()
     def set_weights(self, w_in, w_out):
         """Packs the weights (again, after a training step).  What a forward() before has kept belongs to the old ones: dropped."""
         self._kept = None
         self.w_in, self.w_out = B.pack_sign(w_in), B.pack_sign(w_out)
         self.scale_in, self.scale_out = w_in.abs().mean(1), w_out.abs().mean(1)
 
+    @torch.no_grad()
     def first_norm(self, x: torch.Tensor) -> torch.Tensor:
         """pre(x): what the first block of a stack reads beside the stream."""
         return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, need_r=False)[1]
 
+    @torch.no_grad()
     def first_norm_backward(self, x: torch.Tensor, dn: torch.Tensor, dr: torch.Tensor | None = None) -> torch.Tensor:
         """The backward pass of first_norm(x), after backward(), whose (dx, dn) it takes as (dr, dn): the gradient of the stream x
         by both ways; grads["pre_gamma"] is left beside the others."""
@@ -315,6 +319,7 @@ class BinaryFeedForward:
         """The gate's row for the rows of y: none for none."""
         return self.gate if y.shape[0] else None
 
+    @torch.no_grad()
     def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
         """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""
         h = B.gated_bits(n, self.w_in, self.scale_in, None, self.act)
@@ -325,6 +330,7 @@ class BinaryFeedForward:
         self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
         return r, after
 
+    @torch.no_grad()
     def backward(self, dr: torch.Tensor | None, dn_after: torch.Tensor):
         """Gradients of r (by every way but n') and of n' -> (dx, dn); the parameters' gradients are left in self.grads."""
         if self._kept is None:

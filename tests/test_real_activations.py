@@ -1007,6 +1007,83 @@ def test_a_captured_graph_replays_what_the_calls_compute(M):
             assert torch.equal(a, b)
 
 
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+def test_torch_differentiates_the_products(T):
+    T = TYPES[T]
+    p = Product(20, 48, 70, T, seed=29)
+    w_up = torch.cat([p.wd, -p.wd])
+    lin = torch.nn.Linear(70, 70).to(DEV, T)
+    x = lin(p.xd)
+    scale, bias, both = p.scaled.clone().requires_grad_(), p.biased.clone().requires_grad_(), torch.rand(96, device=DEV, requires_grad=True)
+    res = torch.randn(20, 48, device=DEV).to(T).requires_grad_()
+    y = bnn.linear_bits(x, p.wd, scale, bias, bnn.ACT_GELU, res)
+    h = bnn.gated_bits(x, w_up, both, None, bnn.ACT_SILU)
+    assert y.requires_grad and h.requires_grad
+    dy, dh = torch.randn(20, 48, device=DEV).to(T), torch.randn(20, 48, device=DEV).to(T)
+    torch.autograd.backward([y, h], [dy, dh], inputs=[x, scale, bias, res, both, lin.weight])
+    a = bnn.linear_bits_backward(dy, x.detach(), p.wd, p.scaled, p.biased, bnn.ACT_GELU)
+    b = bnn.gated_bits_backward(dh, x.detach(), w_up, both.detach(), None, bnn.ACT_SILU)
+    assert torch.equal(x.grad, a["dx"] + b["dx"])
+    assert torch.equal(scale.grad, a["dscale"]) and torch.equal(bias.grad, a["dbias"]) and torch.equal(both.grad, b["dscale"])
+    assert torch.equal(res.grad, dy) and lin.weight.grad.any()
+    # a gradient that is one number for all; of the scale alone
+    s = p.scaled.clone().requires_grad_()
+    bnn.linear_bits(p.xd, p.wd, s).sum().backward()
+    want = bnn.linear_bits_backward(torch.ones(20, 48, device=DEV).to(T), p.xd, p.wd, p.scaled)["dscale"]
+    assert torch.equal(s.grad, want)
+    with torch.no_grad():
+        assert not bnn.linear_bits(x, p.wd, scale).requires_grad
+    assert torch.equal(bnn.linear_bits(x, p.wd, scale, bias, bnn.ACT_GELU, res, out=torch.empty_like(res)), y)
+    with pytest.raises(RuntimeError):
+        g, = torch.autograd.grad(bnn.linear_bits(x.detach().requires_grad_(), p.wd).float().square().sum(), both, allow_unused=False)
+
+
+@gpu
+@pytest.mark.parametrize("post,pre", [("rms", "rms"), ("layer", "layer"), ("rms", "none"), ("none", "rms")])
+def test_torch_differentiates_the_norms(post, pre):
+    n = Norm(30, 70, 7, torch.float32, post, pre, seed=4)
+    leaf = lambda t: None if t is None else t.to(DEV).requires_grad_()
+    y, x, gate = leaf(n.y.clone()), leaf(n.x.clone()), leaf(n.gate.clone())
+    v = {k: leaf(None if t is None else t.clone()) for k, t in n.vec.items()}
+
+    def call(**kw):
+        return bnn.norm_residual(y, x, gate, 0.5, NORMS[post], v["post_gamma"], v["post_beta"], NORMS[pre], v["pre_gamma"], v["pre_beta"],
+                                 1e-5, n.R, **kw)
+
+    def check(want):
+        for t, k in ((y, "dy"), (x, "dx"), (gate, "dgate"), *((v[k], "d" + k) for k in v)):
+            assert (t is None) == (want[k] is None)
+            if t is not None:
+                assert torch.equal(t.grad, want[k]), k
+                t.grad = None
+
+    r, nn = call()
+    torch.autograd.backward([r] + ([nn] if nn is not None else []), [n.dr.to(DEV)] + ([n.dn.to(DEV)] if nn is not None else []))
+    check(n.back(r.detach().cpu()))
+    if pre != "none":                                                  # by one of the results alone
+        nothing, nn = call(need_r=False)
+        assert nothing is None
+        nn.backward(n.dn.to(DEV))
+        check(n.back(r.detach().cpu(), dr=False))
+        call()[0].backward(n.dr.to(DEV))
+        n.dn.zero_()
+        check(n.back(r.detach().cpu()))
+    out = torch.empty_like(y)
+    assert not call(out=out, out_n=torch.empty_like(y) if pre != "none" else None)[0].requires_grad
+
+
+@gpu
+def test_torch_does_not_record_the_block():
+    block, x, (w_in, w_out) = small_block()
+    block.post_gamma = torch.nn.Parameter(torch.ones(64, device=DEV))
+    block.set_weights(w_in.requires_grad_(), w_out)
+    x.requires_grad_()
+    r, after = block.forward(x, block.first_norm(x), keep=True)
+    dx, dn = block.backward(torch.ones_like(r), torch.zeros_like(after))
+    assert not any(t.requires_grad for t in (r, after, dx, dn, block.scale_in, *(g for g in block.grads.values() if g is not None)))
+
+
 # ---- refusals ------------------------------------------------------------------------------------------------------
 
 def test_entry_points_refuse_before_any_launch():
