@@ -73,8 +73,10 @@ int launch_form(const ProductArgs& a, Form form, hipStream_t s) {
         const int waves = int(a.K >= 4 * kRunK ? 4 : a.K <= kRunK ? 1 : ceil_div(a.K, kRunK));
         // 128 channels a tile where there are more tiles of 64 than compute units and a run for every wavefront (154 x 4942 ->
         // 5199: 16.5 us against 21.7; 64 x 4096 -> 8192, 256 tiles of 64: 14.5 against 12.1; 500 x 784 -> 3062: 8.8 against 7.9).
-        if (!is_f32<E> && a.K >= 4 * kRunK && ceil_div(a.M, 32) * ceil_div(int64_t(a.N) * HALVES, 64) > 256)
-            return launch_waves<E, EPI, 1, 4>(a, waves, s);
+        if constexpr (!is_f32<E>) {
+            if (a.K >= 4 * kRunK && ceil_div(a.M, 32) * ceil_div(int64_t(a.N) * HALVES, 64) > 256)
+                return launch_waves<E, EPI, 1, 4>(a, waves, s);
+        }
         return launch_waves<E, EPI, 1, 2>(a, waves, s);
     }
     if (far_rows<E>(a.ld_x)) return launch_product<E, EPI, 2, 2, 2, 2, true>(a, s);
