@@ -597,6 +597,51 @@ def test_infinities_in_the_weights_gradient(M, N, K):
     close(dw[fin], want[fin], rounded(want[fin], tol[fin], torch.float32), "finite")
 
 
+# More than four rows and 8192 columns: two blocks of 16 channels a workgroup (gated: four), of one wavefront or several, with rows that begin
+# anywhere.
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("gap,shift", [(0, 0), (1, 1)])
+@pytest.mark.parametrize("M,N,K", [(5, 8192, 70), (16, 8209, 1500), (5, 8209, 4100), (16, 8192, 2051)])
+def test_few_rows_of_many_channels(M, N, K, gap, shift, T):
+    T = TYPES[T]
+    p = Product(M, N, K, T, seed=31, gap=gap, shift=shift)
+    r = torch.randn(M, N, generator=torch.Generator().manual_seed(1)).to(T)
+    close(bnn.linear_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_GELU, r.to(DEV)), *linear_want(p, "gelu", r), "linear")
+    p = Product(M, 2 * N, K, T, seed=31, gap=gap, shift=shift)
+    close(bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU), *gated_want(p, "silu"), "gated")
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(5, 8192, 70), (16, 8209, 1100)])
+def test_backward_of_few_rows_of_many_channels(M, N, K, gated, T):
+    T = TYPES[T]
+    p = Product(M, N * (1 + gated), K, T, seed=31, gap=1)
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+    call = bnn.gated_bits_backward if gated else bnn.linear_bits_backward
+    check_backward(p, "silu", gated, dy, call(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, bnn.ACT_SILU))
+
+
+# The weights' gradient in tiles of 128 in parts of the rows, of 256 (16 bits) and 128 (float32) in parts, and of 256 and 128 in one part of more
+# steps than buffers; in the second the products are tiles of 256 and 128 rows with weights past 512 and 1024 elements.
+@gpu
+@pytest.mark.parametrize("M,N,K,T", [(3001, 1100, 700, "bf16"), (3001, 1100, 700, "f16"), (3001, 1100, 700, "f32"), (4090, 4090, 1100, "bf16"),
+                                     (4090, 4090, 1100, "f32"), (520, 4000, 4080, "f16"), (520, 4000, 4080, "f32")])
+@pytest.mark.parametrize("form", ["linear none", "linear silu", "gated silu"])
+def test_backward_in_large_tiles_of_many_steps(M, N, K, T, form):
+    T = TYPES[T]
+    kind, act = form.split()
+    p = Product(M, N, K, T, seed=33)
+    if kind == "gated":
+        dh = torch.randn(M, N // 2, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+        close(bnn.gated_bits(p.xd, p.wd, p.scaled, p.biased, ACTS[act]), *gated_want(p, act), "forwards")
+        return check_backward(p, act, True, dh, bnn.gated_bits_backward(dh.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act]))
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(2)).mul_(0.1).to(T)
+    check_backward(p, act, False, dy, bnn.linear_bits_backward(dy.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act]))
+
+
 # ---- norms -------------------------------------------------------------------------------------------------------
 
 class Norm:
@@ -792,6 +837,98 @@ def test_product_rows_past_2_31_elements():
     y = bnn.linear_bits(x, p.wd, p.scaled, p.biased)
     close(y[-3:], *linear_want(p, "none"), "last rows")
     assert torch.equal(y[:-3], p.biased.bfloat16().expand(M - 3, N))
+
+
+def strips(M, D, R):
+    """Rows of a strip of the backward pass, and whether a gate is several of them (as the launcher has it)."""
+    target = 4096 if D <= 512 else 2048 if D <= 1024 else 1024 if D <= 2048 else 512 if D <= 4096 else 256
+    rows = -(-M // target)
+    R = min(R, M)
+    return (rows // R * R, False) if R <= rows else (-(-R // -(-R // rows)), True)
+
+
+def walkers(D):
+    """Workgroups of the forward pass, which walk over the rows."""
+    threads = 64 if D <= 1024 else 64 * -(-D // 1024) if D <= 8192 else 1024
+    return 256 * (1024 // threads)
+
+
+@gpu
+@pytest.mark.parametrize("gate_rows", ["1", "2", "above a strip", "700", "all"])
+@pytest.mark.parametrize("M,D,T", [(9001, 7, "f32"), (9001, 65, "bf16"), (5000, 600, "f32"), (2501, 1500, "f16"), (2600, 2049, "f32"),
+                                   (2600, 2049, "bf16"), (1700, 5000, "f16"), (700, 9000, "bf16"), (700, 9000, "f32")])
+def test_norms_of_more_rows_than_workgroups(M, D, T, gate_rows):
+    """A workgroup has several rows: the next one's loads, the gate's row that changes on the way, the sums over rows.  What belongs to
+    a row is what the row gets by itself, bit for bit; the sums are compared with the definition."""
+    T = TYPES[T]
+    R = {"above a strip": strips(M, D, 1)[0] + 1, "all": M}.get(gate_rows) or int(gate_rows)
+    rows, several = strips(M, D, R)
+    assert M > walkers(D) and rows > 1 and several == (R > strips(M, D, 1)[0])
+    post, pre = ("layer", "rms") if R % 2 else ("rms", "layer")
+    n = Norm(M, D, R, T, post, pre, seed=6)
+    dev = lambda t: None if t is None else t.to(DEV)
+    v = {k: dev(t) for k, t in n.vec.items()}
+    y, x, gate, dr, dn = dev(n.y), dev(n.x), dev(n.gate), dev(n.dr), dev(n.dn)
+    per_row = gate.repeat_interleave(R, 0)[:M]
+    post_args = (NORMS[post], v["post_gamma"], v["post_beta"])
+    pre_args = (NORMS[pre], v["pre_gamma"], v["pre_beta"], 1e-5)
+    r, nn = bnn.norm_residual(y, x, gate, 0.5, *post_args, *pre_args, R)
+    got = bnn.norm_residual_backward(dr, dn, y, r, gate, 0.5, *post_args, *pre_args, R)
+    for a in range(0, M, 200):                                         # as few rows as there are workgroups and strips for
+        b = min(a + 200, M)
+        assert strips(200, D, 1)[0] == 1 and walkers(D) >= 200
+        own = bnn.norm_residual(y[a:b], x[a:b], per_row[a:b], 0.5, *post_args, *pre_args, 1)
+        assert torch.equal(own[0], r[a:b]) and torch.equal(own[1], nn[a:b]), a
+        back = bnn.norm_residual_backward(dr[a:b], dn[a:b], y[a:b], r[a:b], per_row[a:b], 0.5, *post_args, *pre_args, 1)
+        assert torch.equal(back["dx"], got["dx"][a:b]) and torch.equal(back["dy"], got["dy"][a:b]), a
+    # The definition in 64 bits, differentiated at the rounded stream.
+    lv = {k: None if t is None else t.double().requires_grad_() for k, t in {"y": y, "x": x, "gate": gate, **v}.items()}
+    r64 = stream64(n, lv)
+    rr = r64 + (r.double() - r64).detach()
+    hat_r = norm64(rr, pre, 1.0, None)
+    ((rr * dr.double()).sum() + (norm64(rr, pre, lv["pre_gamma"], lv["pre_beta"]) * dn.double()).sum()).backward()
+    # A term of a sum over rows is a gradient times a normalised element; float32 errors of either are units of the largest it was
+    # made of (of the gradient: dr, and dn gamma / sqrt(var) of the row), and their sums' errors no more than all of them.
+    unit = (64 + math.sqrt(D)) * F32
+    with torch.no_grad():
+        inv = 1 / torch.sqrt(((rr - rr.mean(1, keepdim=True)) if pre == "layer" else rr).square().mean(1, keepdim=True) + 1e-5)
+        d, g = lv["x"].grad, 0.5 * per_row.double()
+        d_size = d.abs() + dr.double().abs() + 3 * inv * (dn.double() * lv["pre_gamma"]).abs().amax(1, keepdim=True)
+        hat_y = norm64(lv["y"], post, 1.0, None)
+        t = norm64(lv["y"], post, lv["post_gamma"], lv["post_beta"])
+        hat_size, y_size = hat_r.abs() + hat_r.abs().amax(1, keepdim=True), hat_y.abs() + hat_y.abs().amax(1, keepdim=True)
+        by_gate = lambda s: torch.stack([s[a:a + R].sum(0) for a in range(0, M, R)])
+        sums = {"dpre_gamma": (lv["pre_gamma"], (dn.double().abs() * hat_size).sum(0)), "dpre_beta": (lv["pre_beta"], dn.double().abs().sum(0)),
+                "dpost_gamma": (lv["post_gamma"], (g.abs() * d_size * y_size).sum(0)), "dpost_beta": (lv["post_beta"], (g.abs() * d_size).sum(0))}
+        for k, (leaf, size) in sums.items():
+            assert (leaf is None) == (got[k] is None), k
+            if leaf is not None:
+                close(got[k], leaf.grad.cpu(), (unit * size).cpu(), k)
+        want, err = lv["gate"].grad.cpu(), (unit * by_gate(0.5 * d_size * (t.abs() + t.abs().amax(1, keepdim=True)))).cpu()
+        close(got["dgate"], want, rounded(want, err, T), "dgate")
+
+
+@gpu
+@pytest.mark.parametrize("T", TYPES)
+def test_backward_calls_through_ctypes_and_natively(T, monkeypatch):
+    T = TYPES[T]
+    p = Product(90, 2 * 77, 131, T, gap=3, shift=1)
+    n = Norm(50, 203, 10, T, "layer", "rms", gap=3)
+    r = torch.randn(50, 203, generator=torch.Generator().manual_seed(5)).to(T)
+    dy = p.place(torch.randn(90, 154, generator=torch.Generator().manual_seed(2)).to(T))
+    assert binding.load_library() and binding._calls is not None
+
+    def all_of_them():
+        return [bnn.linear_bits_backward(dy, p.xd, p.wd, p.scaled, p.biased, bnn.ACT_GELU),
+                bnn.linear_bits_backward(dy, p.xd, p.wd, p.scaled, need_dw=False),
+                bnn.gated_bits_backward(dy[:, :77], p.xd, p.wd, p.scaled, None, bnn.ACT_SILU, need_dx=False), n.back(r)]
+
+    natively = all_of_them()
+    monkeypatch.setattr(binding, "_calls", None)
+    for a, b in zip(natively, all_of_them()):
+        assert a.keys() == b.keys()
+        for k in a:
+            assert (a[k] is None) == (b[k] is None) and (a[k] is None or torch.equal(a[k], b[k])), k
 
 
 # ---- the block -------------------------------------------------------------------------------------------------------
