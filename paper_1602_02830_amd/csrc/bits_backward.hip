@@ -97,10 +97,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(const TurnArgs t, const Bo
 template <typename E>
 __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t ld_dy, const float* scale, E* ds, int64_t ld_ds,
                                                             float* part, int M, int N, int strip, int blocks_n,
-                                                            const GradientBounds bounds, float* unit_out) {
+                                                            const GradientBounds bounds, float* units, int units_count) {
     __shared__ float sums_s[4][512];
     const float factor = StoredFactor<false>(bounds)(0, BNN_ACT_NONE);
-    if (unit_out && blockIdx.x == 0 && threadIdx.x == 0) *unit_out = 1.0f / factor;
+    leave_units(units, units_count, factor);
     const int tid = threadIdx.x, c = tid & 63, r = tid >> 6;
     const int bm = blockIdx.x / uint32_t(blocks_n), bn = int(blockIdx.x) - bm * blocks_n;
     const int n = bn * 512 + c * 8;
@@ -179,7 +179,7 @@ struct GradPlan {
 // Everything a call puts into its workspace, by sizes alone.  cols: columns of dy (gated: F).
 struct Plan {
     int64_t half, halves, ds_cols, wt_ld, strip, part_rows;
-    int64_t ds_at, wt_at, scale_at, bias_at, pieces_at, bounds_at, unit_at, bytes;
+    int64_t ds_at, wt_at, scale_at, bias_at, pieces_at, bounds_at, units_at, bytes;
     Form form;
     bool recompute;
     GradPlan grad;
@@ -209,7 +209,7 @@ struct Plan {
         bias_at = take(part_rows * channels * 4);
         pieces_at = take(grad.splits > 1 ? grad.splits * channels * K * 4 : 0);
         bounds_at = take(type == BNN_F16 ? kMostBoundParts * int64_t(sizeof(float)) : 0);
-        unit_at = take(type == BNN_F16 ? int64_t(sizeof(float)) : 0);
+        units_at = take(type == BNN_F16 ? (K > channels ? K : channels) * 4 : 0);
     }
 };
 
@@ -266,7 +266,8 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         turn = TurnArgs{w, wt, ld_w, p.wt_ld, int(cols), int(p.half), int(p.halves), int(K), int(blocks_k), int(blocks_n * blocks_k)};
     }
     GradientBounds bounds{};
-    float* unit = nullptr;             // one over what ds is multiplied with, where it is
+    float* units = nullptr;            // one over what ds is multiplied with, where it is, for each channel of dx and dw
+    int units_count = 0;
     BoundArgs look{};
     if constexpr (std::is_same<E, f16_t>::value) {
         if (make_ds && (dx || dw) && M > 0 && K > 0 && cols > 0) {
@@ -277,7 +278,8 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
                 return int(n < kMostLookers ? n : kMostLookers);
             };
             bounds = GradientBounds{parts, workgroups(cols), gated ? workgroups(K) : 0};
-            unit = reinterpret_cast<float*>(ws + p.unit_at);
+            units = reinterpret_cast<float*>(ws + p.units_at);
+            units_count = int(K > channels ? K : channels);
             look = BoundArgs{static_cast<const E*>(dy), static_cast<const E*>(x), scale, bias, parts, ld_dy, ld_x, M, int(cols), int(K),
                              int(channels), bounds.of_dy, bounds.of_x, 2 + bounds.of_dy + bounds.of_x};
         }
@@ -289,12 +291,12 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         if ((st = check_launch()) != BNN_OK) return st;
     }
     if (p.recompute && M > 0 && cols > 0) {
-        ProductArgs a{};
+        BackwardArgs a{};
         a.x = x; a.ld_x = ld_x; a.w = w; a.ld_w = ld_w; a.scale = scale; a.bias = bias; a.act = act;
         a.dy = dy; a.ld_dy = ld_dy; a.y = ds; a.ld_y = p.ds_cols; a.half = int(p.half); a.channels = int(channels);
         a.part_scale = dscale ? part_scale : nullptr;
         a.part_bias = dbias ? part_bias : nullptr;
-        a.bounds = bounds; a.unit_out = unit;
+        a.bounds = bounds; a.units = units; a.units_count = units_count;
         a.M = int(M); a.N = int(cols); a.K = int(K);
         part_rows = ceil_div(M, rows_of_tile<E>(p.form, ld_x));
         st = gated ? launch_form<E, kGatedBack>(a, p.form, s) : launch_form<E, kLinearBack>(a, p.form, s);
@@ -309,14 +311,14 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
             if (p.part_rows * blocks_n > max_blocks(256)) return BNN_ERR_UNSUPPORTED;
             scale_and_sum_kernel<E><<<dim3(uint32_t(p.part_rows * blocks_n)), dim3(256), 0, s>>>(
                 static_cast<const E*>(dy), ld_dy, scale, make_ds ? ds : nullptr, p.ds_cols, dbias ? part_bias : nullptr, int(M),
-                int(cols), int(p.strip), int(blocks_n), bounds, unit);
+                int(cols), int(p.strip), int(blocks_n), bounds, units, units_count);
             st = check_launch();
         }
     }
     if (st != BNN_OK) return st;
     if (dx && M > 0 && K > 0) {
         ProductArgs a{};
-        a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx; a.unit = unit;
+        a.x = g; a.ld_x = ld_g; a.w = wt; a.ld_w = p.wt_ld; a.y = dx; a.ld_y = ld_dx; a.scale = units;
         a.M = int(M); a.N = int(K); a.K = int(cols > 0 ? cols_g : 0);
         if ((st = launch_form<E, kLinear>(a, product_form(is_f32<E>, M, K, 1), s)) != BNN_OK) return st;
     }
@@ -325,8 +327,7 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
         WeightGradArgs a{};
         a.g = p.recompute ? ds : dy; a.ld_g = p.recompute ? p.ds_cols : ld_dy;
         a.x = x; a.ld_x = ld_x; a.dw = dw; a.ld_dw = ld_dw;
-        a.row_scale = p.recompute ? nullptr : scale;
-        a.unit = p.recompute ? unit : nullptr;
+        a.row_scale = p.recompute ? units : scale;
         a.w = scale_by_k ? w : nullptr; a.ld_w = ld_w;
         a.M = int(M); a.K = int(K); a.cols = int(p.recompute ? p.ds_cols : cols); a.half = int(p.half); a.F = int(cols);
         a.channels = int(channels);

@@ -10,7 +10,7 @@ int check_product(int type, const void* x, int64_t ld_x, const uint32_t* w, int6
 
 // a.M, a.N > 0.
 template <typename E, int EPI, int TM, int TN, int FM, int FN, bool FAR = false>
-int launch_product(ProductArgs a, hipStream_t s) {
+int launch_product(ArgsOf<EPI> a, hipStream_t s) {
     using S = ProductTile<E, EPI, TM, TN, FM, FN>;
     const int64_t tiles_m = ceil_div(a.M, S::BM), tiles_n = ceil_div(kBackward<EPI> ? a.half : a.N, S::BN);
     if (tiles_m * tiles_n > max_blocks(S::kThreads)) return BNN_ERR_UNSUPPORTED;
@@ -60,7 +60,7 @@ inline int64_t rows_of_tile(Form form, int64_t ld_x) {
 }
 
 template <typename E, int EPI>
-int launch_form(const ProductArgs& a, Form form, hipStream_t s) {
+int launch_form(const ArgsOf<EPI>& a, Form form, hipStream_t s) {
     constexpr int HALVES = kHalves<EPI>;
     if (form == kSmallForm) {
         const int waves = int(a.K >= 8 * kSmallRunK ? 8 : a.K <= kSmallRunK ? 1 : ceil_div(a.K, kSmallRunK));

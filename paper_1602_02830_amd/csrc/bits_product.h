@@ -32,9 +32,13 @@ struct ProductArgs {
     int channels;              // backward: rows of w
     int act;
     TileMap map;
-    const float* unit;         // what stands for the scale where there is none, or null: 1
-    GradientBounds bounds;     // backward, float16: what ds is multiplied with follows from them
-    float* unit_out;           // backward: gets one over that factor, or null
+};
+
+// What backward passes have besides, so that forward calls, which wait for their arguments too, have no more of them.
+struct BackwardArgs : ProductArgs {
+    GradientBounds bounds;     // float16: what ds is multiplied with follows from them
+    float* units;              // [units_count] get one over that factor: the scale of the products that read ds
+    int units_count;
 };
 
 enum Epilogue {
@@ -50,6 +54,9 @@ template <int EPI>
 inline constexpr int kHalves = EPI == kGated || EPI == kGatedBack ? 2 : 1;
 template <int EPI>
 inline constexpr bool kBackward = EPI == kLinearBack || EPI == kGatedBack;
+
+template <int EPI>
+using ArgsOf = typename std::conditional<kBackward<EPI>, BackwardArgs, ProductArgs>::type;
 
 // The epilogue of W = 8 (or 4) consecutive columns from n on of row m, from their sums (gated: of both halves).  scale, bias: of
 // the columns of each half.  Backwards, ds is stored times `factor`, and sum_s and sum_z grow by dz * s and dz.
@@ -110,14 +117,14 @@ __device__ inline void finish(const ProductArgs& a, int m, int n, const float (&
     }
 }
 
-// The factor of stored gradients, in the two halves of StoredFactor; the first workgroup leaves one over it for the products that read them.
+// The factor of stored gradients, in the two halves of StoredFactor; the workgroups leave one over it for the products that read them.
 template <bool STORED, bool GATED>
 struct Factor {
     StoredFactor<GATED> of;
-    __device__ inline explicit Factor(const ProductArgs& a) : of(a.bounds) {}
-    __device__ inline float operator()(const ProductArgs& a) const {
+    __device__ inline explicit Factor(const BackwardArgs& a) : of(a.bounds) {}
+    __device__ inline float operator()(const BackwardArgs& a) const {
         const float factor = of(a.K, a.act);
-        if (a.unit_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.unit_out = 1.0f / factor;
+        leave_units(a.units, a.units_count, factor);
         return factor;
     }
 };
@@ -157,7 +164,7 @@ struct ProductTile {
 };
 
 template <typename E, int EPI, int TM, int TN, int FM, int FN, bool FAR = false>
-__global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const ArgsOf<EPI> a) {
     using S = ProductTile<E, EPI, TM, TN, FM, FN>;
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
@@ -264,7 +271,7 @@ __global__ __launch_bounds__(64 * TM * TN) void bits_product_kernel(const Produc
             const int col = n0 + (GATED ? w_ * (16 * FN) + (f % (FN / 2 > 0 ? FN / 2 : 1)) * 32 : b * 32) + (c & 31);
             const int64_t row = int64_t(GATED && f >= FN / 2 ? a.N : 0) + col;
             const bool there = col < a.N;
-            scale_s[c] = !there ? 1.0f : a.scale ? a.scale[row] : a.unit ? *a.unit : 1.0f;
+            scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
             bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
         }
     };

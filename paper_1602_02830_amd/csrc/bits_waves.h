@@ -58,7 +58,7 @@ inline bool odd_rows(const ProductArgs& a, int longer) {
 }
 
 template <typename E, int EPI, int FM, int FN, bool ODD>
-__global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(512) void bits_waves_kernel(const ArgsOf<EPI> a) {
     using S = WavesTile<E, EPI, FM, FN>;
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(512) void bits_waves_kernel(const ProductArgs a) {
         const int f = c >> 5, col = n0 + (f % FY) * 32 + (c & 31);
         const int64_t row = int64_t(f / FY) * a.N + col;
         const bool there = col < a.N;
-        scale_s[c] = !there ? 1.0f : a.scale ? a.scale[row] : a.unit ? *a.unit : 1.0f;
+        scale_s[c] = there && a.scale ? a.scale[row] : 1.0f;
         bias_s[c] = there && a.bias ? a.bias[row] : 0.0f;
     }
     const uint32_t* wrow[FN];
@@ -250,7 +250,7 @@ constexpr int kSmallRunK = 512, kSmallRows = 16;
 
 // FN blocks of 16 channels (gated: of each half).
 template <typename E, int EPI, int FN, bool ODD>
-__global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
+__global__ __launch_bounds__(512) void bits_small_kernel(const ArgsOf<EPI> a) {
     using O = Operand<E>;
     using O8 = typename Vec8<O>::type;
     constexpr int HALVES = kHalves<EPI>, BLOCKS = FN * HALVES, TERMS = kTermsOf<E>;
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
     for (int c = tid; c < BLOCKS * 16; c += blockDim.x) {
         const int b = c >> 4, col = n0 + (b % FN) * 16 + (c & 15);
         const int64_t at = int64_t(b / FN) * a.N + col;
-        scale_s[c] = col >= a.N ? 1.0f : a.scale ? a.scale[at] : a.unit ? *a.unit : 1.0f;
+        scale_s[c] = col < a.N && a.scale ? a.scale[at] : 1.0f;
         bias_s[c] = col < a.N && a.bias ? a.bias[at] : 0.0f;
     }
     const Widening<O> minus_weights;
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(512) void bits_small_kernel(const ProductArgs a) {
 }
 
 template <typename E, int EPI, int FN>
-int launch_small(const ProductArgs& a, int waves, hipStream_t s) {
+int launch_small(const ArgsOf<EPI>& a, int waves, hipStream_t s) {
     const int64_t blocks = ceil_div(kBackward<EPI> ? a.half : a.N, 16 * FN), tiles_m = ceil_div(a.M, kSmallRows);
     if (blocks * tiles_m > max_blocks(64 * waves) || tiles_m > 65535) return BNN_ERR_UNSUPPORTED;
     const dim3 grid{uint32_t(blocks), uint32_t(tiles_m)}, block{uint32_t(64 * waves)};
@@ -372,7 +372,7 @@ int launch_small(const ProductArgs& a, int waves, hipStream_t s) {
 }
 
 template <typename E, int EPI, int FM, int FN>
-int launch_waves(ProductArgs a, int waves, hipStream_t s) {
+int launch_waves(ArgsOf<EPI> a, int waves, hipStream_t s) {
     using S = WavesTile<E, EPI, FM, FN>;
     const int64_t tiles_m = ceil_div(a.M, S::BM), tiles_n = ceil_div(kBackward<EPI> ? a.half : a.N, S::BN);
     if (tiles_m * tiles_n > max_blocks(64 * waves)) return BNN_ERR_UNSUPPORTED;

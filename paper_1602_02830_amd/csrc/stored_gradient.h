@@ -12,7 +12,7 @@
 // 2^e brings the bound to between 2^14 and 2^15, half of float16's largest and 2^28 above its smallest normal number.  The bound is loose,
 // for Gaussian operands by 2^6 to 2^12 and with outliers by 2^10 more; what it leaves is still normal, or rounded to 2^-24 of values of
 // 2^-12.  bfloat16 has float32's exponents and needs none of it.  Looking costs a pass over dy, gated over x too, beside the transposition of
-// the weights: 500 x 784 -> 2 x 1531 41.5 us with it and 40.3 without, 3762 x 911 -> 2 x 256 67.1 and 62.8.
+// the weights: 500 x 784 -> 2 x 1531 42.0 us with it and 40.4 without, 3762 x 911 -> 2 x 256 66.5 and 63.0.
 #pragma once
 
 #include "real_types.h"
@@ -77,6 +77,12 @@ public:
         return __uint_as_float(uint32_t(127 + min(max(e, -100), 100)) << 23);
     }
 };
+
+// One over the factor, once for each channel of a product that reads stored gradients.  By all workgroups together, one along y.
+__device__ inline void leave_units(float* units, int count, float factor) {
+    if (blockIdx.y != 0) return;
+    for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < count; i += int64_t(gridDim.x) * blockDim.x) units[i] = 1.0f / factor;
+}
 
 // The largest finite magnitude of the groups of eight elements from `first` on, `step` apart, counted row by row.
 template <typename E>

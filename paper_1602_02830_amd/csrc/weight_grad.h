@@ -19,7 +19,7 @@ struct WeightGradArgs {
     const void* g;             // [M][ld_g]
     const void* x;             // [M][ld_x]
     void* dw;                  // [F or 2 F][ld_dw], or null: only the sums are wanted
-    const float* row_scale;    // [F] or null
+    const float* row_scale;    // [F or 2 F] or null
     const uint32_t* w;         // the weights' bits [F][ld_w] for dscale, or null
     float* part;               // [tiles_k][F]: sum over the tile's k of dw / row_scale * w
     float* pieces;             // [splits][F or 2 F][K]: float32 sums over a part of the rows each, instead of dw and part
@@ -30,7 +30,6 @@ struct WeightGradArgs {
     int channels;              // rows of dw
     int splits, split_rows;    // rows of M that a workgroup sums: a multiple of kGradStep
     TileMap map;
-    const float* unit;         // what stands for row_scale where there is none, or null: 1
 };
 
 constexpr int kGradStep = 32;          // rows a step
@@ -223,13 +222,12 @@ __global__ __launch_bounds__(64 * TK * TN) void weight_grad_kernel(const WeightG
     }
 
     // Lane l has k = 16 fh .. 16 fh + 15 of column n = fr of each block.
-    const float one = a.unit ? *a.unit : 1.0f;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int c = n0 + (wn * FN + j) * 32 + fr, second = c >= a.half ? 1 : 0, f = c - second * a.half;
         const bool there = c < a.cols && f < a.F;
         const int64_t n = int64_t(second) * a.F + f;
-        const float scale = there && a.row_scale ? a.row_scale[n] : one;
+        const float scale = there && a.row_scale ? a.row_scale[n] : 1.0f;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < FK; ++i) {
@@ -281,7 +279,7 @@ template <typename E>
 __global__ __launch_bounds__(256) void join_pieces_kernel(const WeightGradArgs a, float* dscale) {
     __shared__ float sums_s[4];
     const int64_t n = blockIdx.x;
-    const float scale = a.row_scale ? a.row_scale[n] : a.unit ? *a.unit : 1.0f;
+    const float scale = a.row_scale ? a.row_scale[n] : 1.0f;
     float sum = 0.0f;
     for (int64_t k = int64_t(threadIdx.x) * 8; k < a.K; k += 256 * 8) {
         float v[8] = {};
