@@ -302,12 +302,11 @@ class BinaryFeedForward:
         self.w_in, self.w_out = B.pack_sign(w_in), B.pack_sign(w_out)
         self.scale_in, self.scale_out = w_in.abs().mean(1), w_out.abs().mean(1)
 
-    @torch.no_grad()
     def first_norm(self, x: torch.Tensor) -> torch.Tensor:
         """pre(x): what the first block of a stack reads beside the stream."""
-        return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, need_r=False)[1]
+        n = x.new_empty(x.shape)
+        return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, out_n=n, need_r=False)[1]
 
-    @torch.no_grad()
     def first_norm_backward(self, x: torch.Tensor, dn: torch.Tensor, dr: torch.Tensor | None = None) -> torch.Tensor:
         """The backward pass of first_norm(x), after backward(), whose (dx, dn) it takes as (dr, dn): the gradient of the stream x
         by both ways; grads["pre_gamma"] is left beside the others."""
@@ -319,18 +318,18 @@ class BinaryFeedForward:
         """The gate's row for the rows of y: none for none."""
         return self.gate if y.shape[0] else None
 
-    @torch.no_grad()
     def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
         """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""
-        h = B.gated_bits(n, self.w_in, self.scale_in, None, self.act)
-        y = B.linear_bits(h, self.w_out, self.scale_out)
-        r, after = B.norm_residual(y, x, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma,
-                                   None, self.eps, max(x.shape[0], 1))
+        M = x.shape[0]
+        h, y, r, after = (x.new_empty((M, cols)) for cols in (self.F, self.D, self.D, self.D))       # calls with `out` are not recorded
+        B.gated_bits(n, self.w_in, self.scale_in, None, self.act, out=h)
+        B.linear_bits(h, self.w_out, self.scale_out, out=y)
+        B.norm_residual(y, x, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma, None,
+                        self.eps, max(M, 1), out=r, out_n=after)
         # n and r are the caller's, who may write over them before backward() (r in place is the next sum's documented place).
         self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
         return r, after
 
-    @torch.no_grad()
     def backward(self, dr: torch.Tensor | None, dn_after: torch.Tensor):
         """Gradients of r (by every way but n') and of n' -> (dx, dn); the parameters' gradients are left in self.grads."""
         if self._kept is None:
