@@ -5,7 +5,7 @@
 // thread), so that the statistics of y, the new stream r and the statistics of r need nothing but two to four sums over the
 // workgroup.  Variances are sums of squared distances from the mean, taken after it.  Workgroups walk over rows, the next row's loads
 // on their way while one is worked on.  With 8 elements a thread and twice the wavefronts at each barrier the same rows took longer
-// (10000 x 2049 float32 backwards: 155 us against 125), with 4 longer still.
+// (10000 x 2049 float32 backwards, root-mean-square norms: 155 us against 125, and 116 without a gate), with 4 longer still.
 //
 // Forwards the gammas and betas stay in registers: read for every row, these 32-bit vectors were as much traffic to the caches as
 // a row of 16-bit elements.  16384 x 4096 bfloat16, root-mean-square norms and a gate: 114 us, 4.7 TB/s, as fast as a large copy.
@@ -13,9 +13,10 @@
 // Backwards y and r are both at hand from the start, and their norms share their sums; then follow one pair of sums for the
 // gradient of each norm.  A workgroup walks a strip of rows and keeps the sums over rows (of the gammas, betas and the gate) in
 // registers, the gammas and the beta in LDS; strips' sums are joined by a second launch in a fixed order.  16384 x 4096 bfloat16:
-// 178 us, 4.5 TB/s; 10000 x 2049 float32 with layer norms and all their gradients 178 us, 2.8 TB/s, where the sums over rows and
-// three elements in four of 3 wavefronts' lanes are what costs.  Rows past 8192 elements do not fit the registers (4000 x 16000
-// bfloat16: 552 us, 1.4 TB/s; forwards 118 us).
+// 176 us, 4.6 TB/s; 10000 x 2049 float32 with layer norms, a gate and all their gradients 179 us, 2.8 TB/s: five sums over rows instead of
+// two, for which 256 registers are 36 bytes a lane too few, in three wavefronts of whose 3072 places a third are empty.  Rows past 8192
+// elements do not fit the registers: 324 - 596 bytes a lane go to scratch memory (4000 x 16000 bfloat16: 555 us, 1.4 TB/s), forwards
+// 28 - 316 (118 us).
 #include "join_sums.h"
 
 namespace bnn {
