@@ -57,31 +57,51 @@ __device__ inline void transpose_weights(const TurnArgs& a) {
 // ---- bounds of float16 gradients (stored_gradient.h) ---------------------------------------------------------------
 
 struct BoundArgs {
-    const f16_t *dy, *x;
+    const f16_t *dy, *x;       // x: null where the bound does not need it
     const float *scale, *bias;
     float* parts;              // as GradientBounds has them
     int64_t ld_dy, ld_x, M;
     int cols, K, channels;
-    int of_dy, of_x;
-    int blocks;                // workgroups that look, one at the scale, one at the bias, then at dy and x; 0: none
+    int lanes;                 // of a wavefront that take a row together: a power of two, 8 at least
+    int lookers;
+    int blocks;                // workgroups: one at the scale, one at the bias, and the lookers; 0: none
 };
 
 __device__ inline void look_for_bounds(const BoundArgs& a, int block) {
-    __shared__ float wave_s[4];
-    const uint32_t tid = threadIdx.x;
-    float m = block == 0 && !a.scale ? 1.0f : 0.0f;
+    __shared__ float2 wave_s[4];
+    const int tid = threadIdx.x;
+    float most = 0.0f, both = 0.0f;
     if (block < 2) {
         const float* const v = block == 0 ? a.scale : a.bias;
-        if (v) m = largest_of_matrix(v, 0, 1, a.channels, tid, 256);
-    } else if (block < 2 + a.of_dy) {
-        m = largest_of_matrix(a.dy, a.ld_dy, a.M, a.cols, uint32_t(block - 2) * 256 + tid, uint32_t(a.of_dy) * 256);
+        if (v) most = largest_of_row(v + int64_t(tid >> 6) * (a.channels / 4), tid < 192 ? a.channels / 4 : a.channels - 3 * (a.channels / 4), tid & 63, 64);
+        else most = block == 0 ? 1.0f : 0.0f;
     } else {
-        m = largest_of_matrix(a.x, a.ld_x, a.M, a.K, uint32_t(block - 2 - a.of_dy) * 256 + tid, uint32_t(a.of_x) * 256);
+        const int per_block = 256 / a.lanes, lane = tid & (a.lanes - 1);
+        for (int64_t m = int64_t(block - 2) * per_block + tid / a.lanes; m < a.M; m += int64_t(a.lookers) * per_block) {
+            if (!a.x) {
+                most = fmaxf(most, largest_of_row(a.dy + m * a.ld_dy, a.cols, lane, a.lanes));
+                continue;
+            }
+            RowMagnitude<f16_t, false> dy(a.dy + m * a.ld_dy, a.cols, lane, a.lanes);
+            RowMagnitude<f16_t, true> x(a.x + m * a.ld_x, a.K, lane, a.lanes);
+            for (int first = 0; first < max(dy.groups, x.groups); first += 4 * a.lanes) {
+                if (first < dy.groups) dy.load(first);
+                if (first < x.groups) x.load(first);
+                if (first < dy.groups) dy.take(first);
+                if (first < x.groups) x.take(first);
+            }
+            const float largest = dy.over_lanes();
+            most = fmaxf(most, largest);
+            both = fmaxf(both, largest * x.over_lanes());
+        }
     }
-    m = largest_of_wave(m);
-    if ((tid & 63) == 0) wave_s[tid >> 6] = m;
+    most = largest_of_wave(most);
+    both = largest_of_wave(both);
+    if ((tid & 63) == 0) wave_s[tid >> 6] = make_float2(most, both);
     __syncthreads();
-    if (tid == 0) a.parts[block] = fmaxf(fmaxf(wave_s[0], wave_s[1]), fmaxf(wave_s[2], wave_s[3]));
+    if (tid != 0) return;
+    a.parts[block] = fmaxf(fmaxf(wave_s[0].x, wave_s[1].x), fmaxf(wave_s[2].x, wave_s[3].x));
+    if (block >= 2) a.parts[block + a.lookers] = fmaxf(fmaxf(wave_s[0].y, wave_s[1].y), fmaxf(wave_s[2].y, wave_s[3].y));
 }
 
 // What the products need and what does not wait for them, in one launch: workgroups that transpose, then those that look.  LOOK: there
@@ -99,7 +119,7 @@ __global__ __launch_bounds__(256) void scale_and_sum_kernel(const E* dy, int64_t
                                                             float* part, int M, int N, int strip, int blocks_n,
                                                             const GradientBounds bounds, float* units, int units_count) {
     __shared__ float sums_s[4][512];
-    const float factor = StoredFactor<false>(bounds)(0, BNN_ACT_NONE);
+    const float factor = StoredFactor<false>(bounds)(BNN_ACT_NONE);
     leave_units(units, units_count, factor);
     const int tid = threadIdx.x, c = tid & 63, r = tid >> 6;
     const int bm = blockIdx.x / uint32_t(blocks_n), bn = int(blockIdx.x) - bm * blocks_n;
@@ -272,16 +292,16 @@ int backward(const Plan& p, bool gated, const void* dy, int64_t ld_dy, const voi
     if constexpr (std::is_same<E, f16_t>::value) {
         if (make_ds && (dx || dw) && M > 0 && K > 0 && cols > 0) {
             float* const parts = reinterpret_cast<float*>(ws + p.bounds_at);
-            // Four groups of eight elements a thread, as far as there are workgroups.
-            auto workgroups = [&](int64_t columns) {
-                const int64_t n = ceil_div(M * ceil_div(columns, 8), 1024);
-                return int(n < kMostLookers ? n : kMostLookers);
-            };
-            bounds = GradientBounds{parts, workgroups(cols), gated ? workgroups(K) : 0};
+            // A wavefront a row while there is one for each; then as few lanes as load a row in one go, four groups of eight elements each.
+            const int64_t longest = gated && K > cols ? K : cols;
+            int lanes = 64;
+            while (M > 4 * kMostLookers && lanes > 8 && longest <= (lanes / 2) * 32) lanes /= 2;
+            const int64_t wanted = ceil_div(M * lanes, 256);
+            bounds = GradientBounds{parts, int(wanted < kMostLookers ? wanted : kMostLookers)};
             units = reinterpret_cast<float*>(ws + p.units_at);
             units_count = int(K > channels ? K : channels);
-            look = BoundArgs{static_cast<const E*>(dy), static_cast<const E*>(x), scale, bias, parts, ld_dy, ld_x, M, int(cols), int(K),
-                             int(channels), bounds.of_dy, bounds.of_x, 2 + bounds.of_dy + bounds.of_x};
+            look = BoundArgs{static_cast<const E*>(dy), gated ? static_cast<const E*>(x) : nullptr, scale, bias, parts, ld_dy, ld_x, M,
+                             int(cols), int(K), int(channels), lanes, bounds.lookers, 2 + bounds.lookers};
         }
     }
     if (turn.blocks + look.blocks > 0) {

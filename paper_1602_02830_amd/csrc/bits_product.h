@@ -123,7 +123,7 @@ struct Factor {
     StoredFactor<GATED> of;
     __device__ inline explicit Factor(const BackwardArgs& a) : of(a.bounds) {}
     __device__ inline float operator()(const BackwardArgs& a) const {
-        const float factor = of(a.K, a.act);
+        const float factor = of(a.act);
         leave_units(a.units, a.units_count, factor);
         return factor;
     }

@@ -7,25 +7,27 @@
 // made of the largest finite magnitudes of dy, x, scale and bias:
 //
 //   linear:  |ds| <= max|dy| 1.2 max|scale|                                         (slopes of all activations are below 1.2)
-//   gated:   |ds| <= max|dh| max(1.2 Z, 1 for a sigmoid) max|scale|,  Z = max|scale| K max|x| + max|bias| >= |z|
+//   gated:   |ds| <= max over rows m of |dh_m| max(1.2 Z_m, 1 for a sigmoid) max|scale|,  Z_m = max|scale| sum_k |x_mk| + max|bias| >= |z_m|
 //
-// 2^e brings the bound to between 2^14 and 2^15, half of float16's largest and 2^28 above its smallest normal number.  The bound is loose,
-// for Gaussian operands by 2^6 to 2^12 and with outliers by 2^10 more; what it leaves is still normal, or rounded to 2^-24 of values of
-// 2^-12.  bfloat16 has float32's exponents and needs none of it.  Looking costs a pass over dy, gated over x too, beside the transposition of
-// the weights: 500 x 784 -> 2 x 1531 42.0 us with it and 40.4 without, 3762 x 911 -> 2 x 256 66.5 and 63.0.
+// 2^e brings the bound to between 2^14 and 2^15, half of float16's largest and 2^28 above its smallest normal number.  The bound is loose, for
+// Gaussian operands of 4096 columns by 2^9; with outliers a thousand times as large in some rows of x and of dh, the other rows' ds are
+// normal numbers still (with max|x| K in the place of the row's sum they were not, and lost digits).  bfloat16 has float32's exponents and needs
+// none of it.  Powers of two change no digit of a normal number.  Looking costs a pass over dy, gated over x too, beside the transposition of
+// the weights: 500 x 784 -> 2 x 1531 43.2 us with it and 40.4 without, 3762 x 911 -> 2 x 256 68.8 and 63.0.
 #pragma once
 
 #include "real_types.h"
 
 namespace bnn {
 
-// The largest finite magnitudes: of the scale (1 without one), of the bias, then what each workgroup found that looked at dy, and at x.
+// The largest finite magnitudes: of the scale (1 without one), of the bias, then what each workgroup found that looked at rows of dy, and
+// (gated) what each found of a row's dy times the sum of its x.
 struct GradientBounds {
     const float* parts;
-    int of_dy, of_x;           // workgroups; of_dy == 0: ds is stored as it is
+    int lookers;               // workgroups; 0: ds is stored as it is
 };
 
-constexpr int kMostLookers = 256;       // workgroups that look at one of the matrices
+constexpr int kMostLookers = 256;
 constexpr int kMostBoundParts = 2 + 2 * kMostLookers;
 
 // |v|, or 0 where that is infinite or no number: such an element spoils what it reaches at any factor, and must not spoil the rest.
@@ -34,10 +36,29 @@ __device__ inline float finite_magnitude(float v) {
     return a < __builtin_inff() ? a : 0.0f;
 }
 
+// What `join` makes of the values of each aligned group of 8, 16, 32 or 64 lanes, in every lane of it, by lane permutes.
+template <typename F>
+__device__ inline float over_group(float v, int lanes, F&& join) {
+    auto from = [&](auto control) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    v = join(v, from(std::integral_constant<int, 0xB1>{}));       // quad_perm [1,0,3,2]
+    v = join(v, from(std::integral_constant<int, 0x4E>{}));       // quad_perm [2,3,0,1]
+    v = join(v, from(std::integral_constant<int, 0x141>{}));      // row_half_mirror
+    if (lanes >= 16) v = join(v, from(std::integral_constant<int, 0x140>{}));      // row_mirror
+    if (lanes >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    if (lanes >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = join(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    return v;
+}
+
 __device__ inline float largest_of_wave(float m) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-    return m;
+    return over_group(m, 64, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // The factor in two halves: loads that go out before a kernel's others do, and the factor, the same in every lane, of what they bring.
@@ -45,33 +66,35 @@ __device__ inline float largest_of_wave(float m) {
 template <bool GATED>
 class StoredFactor {
     static constexpr int kLoads = kMostLookers / 64;
-    float scale = 1.0f, bias = 0.0f, dy[kLoads] = {}, x[GATED ? kLoads : 1] = {};
+    float scale = 1.0f, bias = 0.0f, dy[kLoads] = {}, both[GATED ? kLoads : 1] = {};
 
 public:
     __device__ inline explicit StoredFactor(const GradientBounds& b) {
-        if (b.of_dy == 0) return;
+        if (b.lookers == 0) return;
         const int lane = threadIdx.x & 63;
         scale = b.parts[0];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) dy[i] = b.parts[2 + min(lane + 64 * i, b.of_dy - 1)];
+        for (int i = 0; i < kLoads; ++i) dy[i] = b.parts[2 + min(lane + 64 * i, b.lookers - 1)];
         if constexpr (GATED) {
             bias = b.parts[1];
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) x[i] = b.parts[2 + b.of_dy + min(lane + 64 * i, b.of_x - 1)];
+            for (int i = 0; i < kLoads; ++i) both[i] = b.parts[2 + b.lookers + min(lane + 64 * i, b.lookers - 1)];
         }
     }
-    __device__ inline float operator()(int K, int act) const {
-        float bound = dy[0], z = 1.2f;
+    __device__ inline float operator()(int act) const {
+        float most_dy = dy[0];
 #pragma unroll
-        for (int i = 1; i < kLoads; ++i) bound = fmaxf(bound, dy[i]);
+        for (int i = 1; i < kLoads; ++i) most_dy = fmaxf(most_dy, dy[i]);
+        most_dy = largest_of_wave(most_dy);
+        float bound = 1.2f * most_dy * scale;
         if constexpr (GATED) {
-            float xs = x[0];
+            float most = both[0];
 #pragma unroll
-            for (int i = 1; i < kLoads; ++i) xs = fmaxf(xs, x[i]);
-            z = 1.2f * (scale * (float(K) * largest_of_wave(xs)) + bias);
-            if (act == BNN_ACT_SIGMOID) z = fmaxf(z, 1.0f);
+            for (int i = 1; i < kLoads; ++i) most = fmaxf(most, both[i]);
+            bound = 1.2f * (scale * largest_of_wave(most) + bias * most_dy);
+            if (act == BNN_ACT_SIGMOID) bound = fmaxf(bound, most_dy);
+            bound *= scale;
         }
-        bound = largest_of_wave(bound) * z * scale;
         if (!(bound > 0.0f && bound < __builtin_inff())) return 1.0f;
         const int e = 14 - (int(__float_as_uint(bound) >> 23) - 127);
         return __uint_as_float(uint32_t(127 + min(max(e, -100), 100)) << 23);
@@ -84,34 +107,51 @@ __device__ inline void leave_units(float* units, int count, float factor) {
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < count; i += int64_t(gridDim.x) * blockDim.x) units[i] = 1.0f / factor;
 }
 
-// The largest finite magnitude of the groups of eight elements from `first` on, `step` apart, counted row by row.
-template <typename E>
-__device__ inline float largest_of_matrix(const E* p, int64_t ld, int64_t rows, int cols, uint32_t first, uint32_t step) {
-    const uint32_t per_row = uint32_t(cols + 7) / 8;
+// What a lane has of the magnitudes of a row that `lanes` neighbouring lanes (a power of two, 8 at least) take together: the largest, or the
+// sum, of the finite ones.  Four groups of eight elements are on their way at once; load() and take() apart let two rows' be.
+template <typename E, bool SUM>
+struct RowMagnitude {
+    const E* row;
+    int groups, lane, lanes;
+    E end;                     // an element past the last whole group
     float m = 0.0f;
-    int64_t row = first / per_row;
-    uint32_t c = first % per_row;
-    const uint32_t rows_on = step / per_row, on = step % per_row;
-    while (row < rows) {
-        typename Vec8<E>::type v[8] = {};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // The row's end from its last eight elements: some are looked at twice.
-            const int at = min(int(c * 8), max(cols - 8, 0));
-            if (row < rows) v[i] = load8<E>(p + row * ld + at, cols - at);
-            row += rows_on;
-            c += on;
-            if (c >= per_row) {
-                c -= per_row;
-                ++row;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_magnitude(float(v[i][e])));
+    typename Vec8<E>::type v[4];
+    __device__ inline RowMagnitude(const E* p, int cols, int l, int n) : row(p), groups(cols / 8), lane(l), lanes(n), end(E(0.0f)) {
+        if (8 * groups + l < cols) end = p[8 * groups + l];
     }
-    return m;
+    __device__ inline void load(int first) {           // groups from `first` on; those that are not there: the last one
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const typename Vec8<E>::any*>(row + 8 * int64_t(min(first + lane + i * lanes, groups - 1)));
+    }
+    __device__ inline void add(float magnitude) { m = SUM ? m + magnitude : fmaxf(m, magnitude); }
+    __device__ inline void take(int first) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float of = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) of = SUM ? of + __builtin_fabsf(float(v[i][e])) : fmaxf(of, __builtin_fabsf(float(v[i][e])));
+            if (!(of < __builtin_inff())) {             // an element is infinite or no number: without it
+                of = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) of = SUM ? of + finite_magnitude(float(v[i][e])) : fmaxf(of, finite_magnitude(float(v[i][e])));
+            }
+            add(first + lane + i * lanes < groups ? of : 0.0f);
+        }
+    }
+    __device__ inline float over_lanes() {
+        add(finite_magnitude(float(end)));
+        return over_group(m, lanes, [](float a, float b) { return SUM ? a + b : fmaxf(a, b); });
+    }
+};
+
+template <typename E>
+__device__ inline float largest_of_row(const E* p, int cols, int lane, int lanes) {
+    RowMagnitude<E, false> r(p, cols, lane, lanes);
+    for (int first = 0; first < r.groups; first += 4 * lanes) {
+        r.load(first);
+        r.take(first);
+    }
+    return r.over_lanes();
 }
 
 }  // namespace bnn

@@ -528,6 +528,27 @@ def test_float16_backward_keeps_small_gradients(M, N, K, dy_std, act, gated):
 
 
 @gpu
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+@pytest.mark.parametrize("M,F,K,loud", [(64, 256, 1024, 1000), (64, 256, 1024, 10000), (1500, 33, 300, 1000), (40, 300, 4, 1000)])
+def test_float16_backward_beside_loud_rows(M, F, K, loud, act):
+    """Some rows of x and others of dh have elements far above the rest: the other rows keep their digits, by the row's mean square."""
+    p = Product(M, 2 * F, K, torch.float16, seed=21)
+    p.scale = (torch.rand(2 * F, generator=torch.Generator().manual_seed(5)) + 0.5) / 64
+    p.scaled = p.scale.to(DEV)
+    dh = torch.randn(M, F, generator=torch.Generator().manual_seed(2)).mul_(1e-3)
+    p.x[:2, :40] = (p.x[:2, :40].float() * loud).clamp(-6e4, 6e4).half()
+    p.xd.copy_(p.x)
+    dh[2:4, :10] *= loud
+    dh = dh.half()
+    got = bnn.gated_bits_backward(dh.to(DEV), p.xd, p.wd, p.scaled, p.biased, ACTS[act])["dx"].cpu().double()
+    want, spread = backward_want(p, act, True, dh)
+    want, spread = want["dx"][0][4:], spread["dx"][4:]
+    err = (got[4:] - want).square().mean(1).sqrt()
+    bound = 3 * (spread.mean(1) + TINY[p.T] ** 2 / 3).sqrt() + 1e-6 * want.square().mean(1).sqrt()
+    assert (err <= bound).all(), (err / bound).max().item()
+
+
+@gpu
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("act", ["none", "gelu"])
 def test_float16_backward_of_large_gradients(act, gated):
