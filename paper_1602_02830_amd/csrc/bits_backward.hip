@@ -105,7 +105,7 @@ __device__ inline void look_for_bounds(const BoundArgs& a, int block) {
 }
 
 // What the products need and what does not wait for them, in one launch: workgroups that transpose, then those that look.  LOOK: there
-// are some, whose loads in flight take registers: 5 wavefronts a SIMD instead of 8.
+// are some, whose loads in flight take registers: 4 wavefronts a SIMD instead of 8.
 template <bool LOOK>
 __global__ __launch_bounds__(256) void prepare_kernel(const TurnArgs t, const BoundArgs b) {
     if (!LOOK || int(blockIdx.x) < t.blocks) transpose_weights(t);

@@ -10,7 +10,7 @@
 //   gated:   |ds| <= max over rows m of |dh_m| max(1.2 Z_m, 1 for a sigmoid) max|scale|,  Z_m = max|scale| sum_k |x_mk| + max|bias| >= |z_m|
 //
 // 2^e brings the bound to between 2^14 and 2^15, half of float16's largest and 2^28 above its smallest normal number.  The bound is loose, for
-// Gaussian operands of 4096 columns by 2^9; with outliers a thousand times as large in some rows of x and of dh, the other rows' ds are
+// Gaussian operands of 4096 columns by about 2^9; with outliers a thousand times as large in some rows of x and of dh, the other rows' ds are
 // normal numbers still (with max|x| K in the place of the row's sum they were not, and lost digits).  bfloat16 has float32's exponents and needs
 // none of it.  Powers of two change no digit of a normal number.  Looking costs a pass over dy, gated over x too, beside the transposition of
 // the weights: 500 x 784 -> 2 x 1531 43.2 us with it and 40.4 without, 3762 x 911 -> 2 x 256 68.8 and 63.0.

@@ -260,7 +260,6 @@ class BinaryConvNet:
         return self.scores
 
 
-
 def _writes(t: torch.Tensor):
     """torch's count of the writes to a tensor (inference tensors have none)."""
     return None if t.is_inference() else t._version
