@@ -1,0 +1,390 @@
+"""The feed-forward block with microscaled activations: rows in 8 or 4 bits, a scale for each 32 elements, +-1 weights.
+
+A block of 32 elements of a row shares a power of two, 2^e; its elements are codes of 8 bits (e4m3: 4 exponent and 3
+mantissa bits, up to 448) or of 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives).  e is the smallest exponent
+with which the block's largest magnitude does not round past the largest code; codes are the nearest ones, ties to the
+even one.  x^ are the values that codes and scales stand for.
+
+  quantise   x -> codes, scales, x^                                                       bnn.mx_quantize
+  norm       r = x + res_scale * gate * post(y), codes, scales and n^ of n = pre(r)        bnn.norm_residual_mx
+  linear     y = act(scale * (x^ w^T) + bias) + residual                                  bnn.linear_mx
+  gated      h = act(z_gate) * z_up, z = scale * (x^ w^T) + bias, w [2F][K]                bnn.gated_mx
+             with "out" the codes, scales and h^ of h, for the product that follows
+
+Where a computed value lies next to the border between two codes, the last bit of a 32-bit sum decides between them.  Cases that
+quantise what they have computed (norm, and gated with "out") therefore have results of 16 bits and codes of e4m3, whose neighbours
+are an eighth of the value apart at most (e2m1: up to half of it), and of their x^ there is no value in 64 bits to be equal to.
+
+``own`` says which form run() computes: elementary torch operations in 32 bits, or the package's entry points.  The weights are
+the same +-1 matrix and the activations the same x^ for both; each form keeps them the way a program that calls it
+would (weights in float32 and x^ in the activations' type for the plain form, packed bits and codes for the package).
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+EPS = 1e-5
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+BYTES = {"bf16": 2, "f16": 2, "f32": 4}
+CODE_BITS = {"e4m3": 8, "e2m1": 4}
+
+MAX_FLOPS = 2 * 8192 * 4096 * 16384        # the largest listed product (gated_8192x4096x8192)
+MAX_NORM_REALS = 16384 * 4096              # elements of the largest listed matrix of the norms
+MAX_REALS = 16384 * 8192                   # elements of the largest listed matrix elsewhere
+
+
+def listed():
+    return [
+        # A ragged batch of a program in 32 bits: rows of odd length whose last block is not whole.
+        {"name": "quantise_1000x2047_f32_e2m1", "op": "quantise", "format": "e2m1", "type": "f32", "M": 1000, "K": 2047},
+        # The hidden activations of long prompts.
+        {"name": "quantise_16384x8192_bf16_e4m3", "op": "quantise", "format": "e4m3", "type": "bf16", "M": 16384, "K": 8192},
+        # Between two blocks, a token at a time.
+        {"name": "norm_1x4096_bf16_e4m3", "op": "norm", "format": "e4m3", "type": "bf16", "M": 1, "D": 4096, "rows_per_gate": 1,
+         "x": True, "gate": True, "post": "rms", "pre": "rms"},
+        # A ragged prompt with rows of odd length, layer norms and a gate for each 100 rows.
+        {"name": "norm_333x2049_f16_e4m3", "op": "norm", "format": "e4m3", "type": "f16", "M": 333, "D": 2049, "rows_per_gate": 100,
+         "x": True, "gate": True, "post": "layer", "pre": "layer"},
+        # Between two blocks of a long batch.
+        {"name": "norm_16384x4096_bf16_e4m3", "op": "norm", "format": "e4m3", "type": "bf16", "M": 16384, "D": 4096,
+         "rows_per_gate": 16384, "x": True, "gate": False, "post": "rms", "pre": "rms"},
+        # The block's second product for a few sequences, a token each, added to the stream.
+        {"name": "linear_8x8192x4096_bf16_e2m1", "op": "linear", "format": "e2m1", "type": "bf16", "M": 8, "K": 8192, "N": 4096,
+         "act": "none", "scale": True, "bias": True, "residual": True},
+        # A layer of the framework's MLP on quantised inputs, results in its own 32 bits.
+        {"name": "linear_1000x784x4096_f32_e4m3", "op": "linear", "format": "e4m3", "type": "f32", "M": 1000, "K": 784, "N": 4096,
+         "act": "relu", "scale": True, "bias": True, "residual": False},
+        # The block's second product for long prompts.
+        {"name": "linear_8192x8192x4096_bf16_e4m3", "op": "linear", "format": "e4m3", "type": "bf16", "M": 8192, "K": 8192, "N": 4096,
+         "act": "none", "scale": True, "bias": False, "residual": True},
+        # One token through the first half of a served model's block, quantised for the second.
+        {"name": "gated_1x4096x8192_bf16_e4m3", "op": "gated", "format": "e4m3", "type": "bf16", "M": 1, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False, "out": True},
+        # A ragged prompt with sizes that fit no tile.
+        {"name": "gated_333x1000x2047_f16_e2m1", "op": "gated", "format": "e2m1", "type": "f16", "M": 333, "K": 1000, "F": 2047,
+         "act": "gelu_tanh", "scale": True, "bias": True, "out": False},
+        # Long prompts in 4 bits.
+        {"name": "gated_8192x4096x8192_bf16_e2m1", "op": "gated", "format": "e2m1", "type": "bf16", "M": 8192, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False, "out": False},
+        # The forward half of a training step in 8 bits.
+        {"name": "gated_4096x4096x8192_bf16_e4m3", "op": "gated", "format": "e4m3", "type": "bf16", "M": 4096, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False, "out": True},
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi, step):
+    """A size in [lo, hi], spread over its logarithm; half of the time a multiple of `step`."""
+    v = _log_int(rng, lo, hi)
+    return max(step, v // step * step) if rng.random() < 0.5 else v
+
+
+def draw(rng):
+    while True:
+        op = rng.choice(["quantise", "norm", "linear", "gated"])
+        case = {"op": op, "format": rng.choice(["e4m3", "e2m1"]), "type": rng.choice(["bf16", "bf16", "bf16", "f16", "f16", "f32"])}
+        if op == "quantise":
+            case.update(M=_log_int(rng, 1, 32768), K=_size(rng, 64, 16384, 64))
+            if case["M"] * case["K"] <= MAX_REALS:
+                return case
+            continue
+        if op == "norm":
+            M = _log_int(rng, 1, 32768)
+            if case["type"] == "f32":
+                continue
+            case.update(format="e4m3", M=M, D=_size(rng, 64, 8192, 64), rows_per_gate=rng.choice([1, M, _log_int(rng, 1, M)]),
+                        x=rng.random() < 0.8, gate=rng.random() < 0.6, post=rng.choice(["none", "rms", "layer"]),
+                        pre=rng.choice(["rms", "rms", "layer"]))
+            if case["M"] * case["D"] <= MAX_NORM_REALS:
+                return case
+            continue
+        M = _log_int(rng, 1, 16) if rng.random() < 0.3 else _log_int(rng, 16, 16384)
+        acts = ["silu", "gelu", "gelu_tanh", "sigmoid", "relu"]
+        case.update(M=M, K=_size(rng, 256, 8192, 128))
+        if op == "gated":
+            out = case["format"] == "e4m3" and case["type"] != "f32" and rng.random() < 0.6
+            case.update(F=_size(rng, 256, 8192, 128), act=rng.choice(acts), scale=True, bias=rng.random() < 0.4, out=out)
+            n = 2 * case["F"]
+        else:
+            n = _size(rng, 256, 8192, 128)
+            case.update(N=n, act=rng.choice(["none", "none"] + acts), bias=rng.random() < 0.5, residual=rng.random() < 0.5)
+            case["scale"] = case["act"] != "none" or rng.random() < 0.8
+        if work(case)["flops"] <= MAX_FLOPS and M * max(n, case["K"]) <= MAX_REALS:
+            return case
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------
+
+def _draws(case, seed):
+    """The values behind a case, in the types in which a program holds them; +-1 weights as float32, x before it is quantised."""
+    g = torch.Generator(device=DEV).manual_seed(1000003 * int(seed) + 11)
+    T = TYPES[case["type"]]
+    M = case["M"]
+
+    def normal(*shape, std=1.0, mean=0.0, dtype=torch.float32):
+        return torch.randn(shape, generator=g, device=DEV).mul_(std).add_(mean).to(dtype)
+
+    def loud(n):
+        """A few channels are much larger than the others."""
+        return 1 + 15 * (torch.rand(n, generator=g, device=DEV) < 0.01).float()
+
+    d = {}
+    if case["op"] == "norm":
+        D = case["D"]
+        d["y"] = (normal(M, D) * loud(D)).to(T)
+        d["x"] = normal(M, D, std=2.0, dtype=T) if case["x"] else None
+        d["gate"] = normal(-(-M // case["rows_per_gate"]), D, std=0.3, mean=1.0, dtype=T) if case["gate"] else None
+        d["res_scale"] = 0.5
+        for side in ("post", "pre"):
+            d[side + "_gamma"] = normal(D, std=0.2, mean=1.0) if case[side] != "none" else None
+            d[side + "_beta"] = normal(D, std=0.2) if case[side] == "layer" else None
+        return d
+    K = case["K"]
+    d["x"] = (normal(M, K) * loud(K)).to(T)
+    if case["op"] == "quantise":
+        return d
+    N = 2 * case["F"] if case["op"] == "gated" else case["N"]
+    d["w"] = torch.randint(0, 2, (N, K), generator=g, device=DEV).mul_(2).sub_(1).float()
+    d["scale"] = torch.rand(N, generator=g, device=DEV).add_(0.5).div_(math.sqrt(K)) if case["scale"] else None
+    d["bias"] = normal(N, std=0.2) if case["bias"] else None
+    if case["op"] == "linear":
+        d["residual"] = normal(M, N, std=2.0, dtype=T) if case["residual"] else None
+    return d
+
+
+def prepare(case, seed):
+    st = _draws(case, seed)
+    st.update(case=case, T=TYPES[case["type"]])
+    if own:
+        import paper_1602_02830_amd as bnn
+        st["bnn"], st["format"] = bnn, {"e4m3": bnn.MX_E4M3, "e2m1": bnn.MX_E2M1}[case["format"]]
+        st["act"] = {"none": bnn.ACT_NONE, "relu": bnn.ACT_RELU, "silu": bnn.ACT_SILU, "gelu": bnn.ACT_GELU,
+                     "gelu_tanh": bnn.ACT_GELU_TANH, "sigmoid": bnn.ACT_SIGMOID}[case.get("act", "none")]
+        if case["op"] == "quantise":
+            st["out_mx"] = bnn.mx_rows(case["M"], case["K"], st["format"], device=DEV, hat=st["T"])
+        elif case["op"] == "norm":
+            st["kinds"] = {"none": bnn.NORM_NONE, "rms": bnn.NORM_RMS, "layer": bnn.NORM_LAYER}
+            st["out_r"] = torch.empty_like(st["y"])
+            st["out_mx"] = bnn.mx_rows(case["M"], case["D"], st["format"], device=DEV, hat=st["T"])
+        else:
+            st["x"] = bnn.mx_quantize(st["x"], st["format"])
+            st["w_bits"] = bnn.pack_sign(st.pop("w"))
+            cols = case["F"] if case["op"] == "gated" else case["N"]
+            if case.get("out"):
+                st["out_mx"] = bnn.mx_rows(case["M"], cols, st["format"], device=DEV, hat=st["T"])
+            else:
+                st["out"] = torch.empty((case["M"], cols), dtype=st["T"], device=DEV)
+    elif case["op"] in ("linear", "gated"):
+        st["x"] = _plain_hat(st["x"].float(), case["format"]).to(st["T"])       # exact in each type
+    return st
+
+
+# ---- the operators -----------------------------------------------------------------------------------------
+
+def run(st):
+    case = st["case"]
+    if own:
+        return _own(st)
+    if case["op"] == "quantise":
+        return _plain_hat(st["x"].float(), case["format"]).to(st["T"])
+    return _plain_norm(st) if case["op"] == "norm" else _plain_product(st)
+
+
+def _own(st):
+    bnn, case = st["bnn"], st["case"]
+    if case["op"] == "quantise":
+        return bnn.mx_quantize(st["x"], st["format"], out=st["out_mx"]).hat
+    if case["op"] == "norm":
+        r, n = bnn.norm_residual_mx(st["y"], st["x"], st["gate"], st["res_scale"], st["kinds"][case["post"]], st["post_gamma"],
+                                    st["post_beta"], st["kinds"][case["pre"]], st["pre_gamma"], st["pre_beta"], EPS,
+                                    case["rows_per_gate"], format=st["format"], out=st["out_r"], out_mx=st["out_mx"])
+        return {"r": r, "n": n.hat}
+    if case["op"] == "linear":
+        return bnn.linear_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], st["residual"], out=st["out"])
+    if case["out"]:
+        return bnn.gated_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], out_mx=st["out_mx"]).hat
+    return bnn.gated_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], out=st["out"])
+
+
+# ---- plain forms: elementary operations in 32 bits, rounded once at the end ----------------------------------
+
+def _power(e):
+    """2^e of whole numbers, by its bits: exact, which torch's powers on the GPU are not."""
+    return ((e + 127) << 23).to(torch.int32).view(torch.float32)
+
+
+def _plain_hat(x, fmt):
+    """x^ of float32 rows."""
+    M, K = x.shape
+    largest, least, digits = (8, -6, 3) if fmt == "e4m3" else (2, 0, 1)         # exponents of the largest and least normal code
+    blocks = -(-K // 32)
+    v = torch.cat([x, x.new_zeros(M, 32 * blocks - K)], dim=1) if 32 * blocks > K else x
+    v = v.view(M, blocks, 32)
+    mantissa, exponent = torch.frexp(v.abs().amax(dim=2, keepdim=True))          # in [0.5, 1)
+    past = mantissa > 464 / 512 if fmt == "e4m3" else mantissa >= 7 / 8
+    e = torch.clamp(exponent - 1 - largest + past.to(exponent.dtype), min=-126)
+    v = v * _power(-e)
+    step = _power(torch.clamp(torch.frexp(v)[1] - 1, min=least) - digits)
+    v = torch.round(v / step) * step * _power(e)
+    return v.view(M, 32 * blocks)[:, :K]
+
+
+def _act(z, name):
+    if name == "none":
+        return z
+    if name == "relu":
+        return torch.clamp(z, min=0)
+    if name == "silu":
+        return z / (1 + torch.exp(-z))
+    if name == "sigmoid":
+        return 1 / (1 + torch.exp(-z))
+    if name == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z)))
+
+
+def _plain_product(st):
+    case, T = st["case"], st["T"]
+    z = st["x"].float() @ st["w"].t()
+    if st["scale"] is not None:
+        z = z * st["scale"]
+    if st["bias"] is not None:
+        z = z + st["bias"]
+    if case["op"] == "gated":
+        F = case["F"]
+        h = _act(z[:, :F], case["act"]) * z[:, F:]
+        return (_plain_hat(h, case["format"]) if case["out"] else h).to(T)
+    y = _act(z, case["act"])
+    if st["residual"] is not None:
+        y = y + st["residual"].float()
+    return y.to(T)
+
+
+def _plain_side(v, kind, gamma, beta):
+    if kind == "none":
+        return v
+    if kind == "layer":
+        v = v - v.mean(1, keepdim=True)
+    v = v * torch.rsqrt((v * v).mean(1, keepdim=True) + EPS) * gamma
+    return v if beta is None else v + beta
+
+
+def _plain_norm(st):
+    case, T = st["case"], st["T"]
+    r = _plain_side(st["y"].float(), case["post"], st["post_gamma"], st["post_beta"]) * st["res_scale"]
+    if st["gate"] is not None:
+        r = r * st["gate"].float().repeat_interleave(case["rows_per_gate"], 0)[:case["M"]]
+    if st["x"] is not None:
+        r = r + st["x"].float()
+    n = _plain_side(r, case["pre"], st["pre_gamma"], st["pre_beta"])
+    return {"r": r.to(T), "n": _plain_hat(n, case["format"]).to(T)}
+
+
+# ---- what an operator cannot do without ----------------------------------------------------------------------
+
+def _codes(case, rows, cols):
+    """Bytes of quantised rows: codes and scales."""
+    return rows * (cols * CODE_BITS[case["format"]] // 8 + -(-cols // 32))
+
+
+def work(case):
+    size = BYTES[case["type"]]
+    M = case["M"]
+    if case["op"] == "quantise":
+        return {"bytes": 2 * size * M * case["K"] + _codes(case, M, case["K"]), "flops": 4 * M * case["K"]}
+    if case["op"] == "norm":
+        D, G = case["D"], -(-case["M"] // case["rows_per_gate"])
+        sides = sum({"none": 0, "rms": 1, "layer": 2}[case[s]] for s in ("post", "pre"))
+        b = size * M * D * (3 + case["x"]) + _codes(case, M, D) + size * G * D * case["gate"] + 4 * D * sides
+        return {"bytes": b, "flops": 16 * M * D}
+    K, gated = case["K"], case["op"] == "gated"
+    N, cols = (2 * case["F"], case["F"]) if gated else (case["N"], case["N"])
+    b = _codes(case, M, K) + 4 * N * ((K + 31) // 32) + 4 * N * (case["scale"] + case["bias"])
+    b += size * M * cols * (1 + case.get("residual", False)) + (_codes(case, M, cols) if case.get("out") else 0)
+    return {"bytes": b, "flops": 2 * M * N * K}
+
+
+# ---- the same results from the definitions, in 64 bits -------------------------------------------------------
+
+#: The magnitudes that codes stand for, in the order of the codes, and the one that would follow the largest.
+_E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 8.0]
+_E4M3 = [i / 512 for i in range(8)] + [(8 + i) * 2.0 ** (e - 3) for e in range(-6, 9) for i in range(8)]      # the last one: 480
+
+
+def _exact_hat(v, fmt):
+    """The nearest codes, even ones between two, looked up in a table; of rows in 64 bits."""
+    table = torch.tensor(_E4M3 if fmt == "e4m3" else _E2M1, dtype=torch.float64, device=DEV)
+    border = (table[1:] + table[:-1]) / 2
+
+    def nearest(a):
+        below = torch.searchsorted(border, a)                       # borders below a
+        tie = border[torch.clamp(below, max=border.numel() - 1)] == a
+        return below + (tie & (below % 2 == 1)).long()
+
+    M, K = v.shape
+    out = torch.zeros_like(v)
+    rows = max(1, (1 << 24) // max(K, 1))
+    for first in range(0, M, rows):                                 # a part at a time: look-ups take memory
+        part = v[first:first + rows]
+        part = torch.nn.functional.pad(part, (0, -K % 32)).reshape(part.shape[0], -1, 32)
+        peak = part.abs().max(dim=2, keepdim=True).values
+        # The largest code is below 2^9 (2^3): one of two exponents.
+        low = torch.floor(torch.log2(torch.clamp(peak, min=2.0 ** -100))) - (8 if fmt == "e4m3" else 2)
+        unit = ((low.long() + 1023) << 52).view(torch.float64)      # 2^low
+        unit = torch.where(nearest(peak / unit) < table.numel() - 1, unit, 2 * unit)
+        got = torch.sign(part) * table[nearest((part / unit).abs())] * unit
+        out[first:first + rows] = got.reshape(got.shape[0], -1)[:, :K]
+    return out
+
+
+def _phi(z, name):
+    if name == "none":
+        return z
+    if name == "relu":
+        return torch.where(z > 0, z, torch.zeros_like(z))
+    if name == "gelu":
+        return z * 0.5 * torch.erfc(-z / math.sqrt(2))
+    if name == "gelu_tanh":
+        return z * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3))
+    s = torch.sigmoid(z)
+    return s if name == "sigmoid" else z * s
+
+
+def _exact_norm_of(v, kind, gamma, beta):
+    if kind == "none":
+        return v
+    centre = v.mean(dim=1, keepdim=True) if kind == "layer" else torch.zeros(v.shape[0], 1, dtype=torch.float64, device=DEV)
+    res = (v - centre) / torch.sqrt(((v - centre) ** 2).mean(dim=1, keepdim=True) + EPS) * gamma.double()
+    return res if beta is None else res + beta.double()
+
+
+def exact(case, seed):
+    if case["op"] == "gated" and case["out"]:
+        return None
+    d = _draws(case, seed)
+    if case["op"] == "quantise":
+        return _exact_hat(d["x"].double(), case["format"])
+    if case["op"] == "norm":
+        r = d["res_scale"] * _exact_norm_of(d["y"].double(), case["post"], d["post_gamma"], d["post_beta"])
+        if d["gate"] is not None:
+            r = r * d["gate"].double()[torch.arange(case["M"], device=DEV) // case["rows_per_gate"]]
+        if d["x"] is not None:
+            r = r + d["x"].double()
+        return {"r": r, "n": None}
+    z = torch.mm(_exact_hat(d["x"].double(), case["format"]), d["w"].double().t())
+    if d["scale"] is not None:
+        z.mul_(d["scale"].double())
+    if d["bias"] is not None:
+        z.add_(d["bias"].double())
+    if case["op"] == "gated":
+        return _phi(z[:, :case["F"]], case["act"]).mul(z[:, case["F"]:])
+    y = _phi(z, case["act"])
+    return y if d["residual"] is None else y + d["residual"].double()
