@@ -1,23 +1,24 @@
-"""The feed-forward block with microscaled activations: rows in 8 or 4 bits, a scale for each 32 elements, +-1 weights.
+"""The feed-forward block with quantised activations: rows of 8 or 4 bits with scales, +-1 weights.
 
-A block of 32 elements of a row shares a power of two, 2^e; its elements are codes of 8 bits (e4m3: 4 exponent and 3
-mantissa bits, up to 448) or of 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives).  e is the smallest exponent
-with which the block's largest magnitude does not round past the largest code; codes are the nearest ones, ties to the
-even one.  x^ are the values that codes and scales stand for.
+  i8    x^ = s q, q whole numbers from -127 to 127; a float32 scale s for each row, its largest magnitude over 127 (2^-126 at
+        least)
+  mx4   x^ = 2^e c, a power of two for each 32 elements of a row, c of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; e is the smallest
+        exponent with which the block's largest magnitude does not round past 6
 
-  quantise   x -> codes, scales, x^                                                       bnn.mx_quantize
-  norm       r = x + res_scale * gate * post(y), codes, scales and n^ of n = pre(r)        bnn.norm_residual_mx
-  linear     y = act(scale * (x^ w^T) + bias) + residual                                  bnn.linear_mx
-  gated      h = act(z_gate) * z_up, z = scale * (x^ w^T) + bias, w [2F][K]                bnn.gated_mx
-             with "out" the codes, scales and h^ of h, for the product that follows
+q and c are the nearest ones, ties to the even code.
 
-Where a computed value lies next to the border between two codes, the last bit of a 32-bit sum decides between them.  Cases that
-quantise what they have computed (norm, and gated with "out") therefore have results of 16 bits and codes of e4m3, whose neighbours
-are an eighth of the value apart at most (e2m1: up to half of it), and of their x^ there is no value in 64 bits to be equal to.
+  quantise   x -> codes, scales and x^                                                    bnn.quantize_rows
+  norm       r = x + res_scale * gate * post(y); codes, scales and n^ of n = pre(r)        bnn.norm_residual_q
+  linear     y = act(scale * (x^ w^T) + bias) + residual                                  bnn.linear_q_bits
+  gated      h = act(z_gate) * z_up, z = scale * (x^ w^T) + bias, w [2F][K]                bnn.gated_q_bits
+
+Where a computed value lies next to the border between two codes, the last bit of a 32-bit sum decides between them.  The norm's cases
+therefore have results of 16 bits and codes of 8, whose neighbours are close (those of mx4 are up to half of the value apart),
+and its n^ has no value in 64 bits to be equal to.  Rows quantised as they are stored are whole numbers of steps exactly.
 
 ``own`` says which form run() computes: elementary torch operations in 32 bits, or the package's entry points.  The weights are
 the same +-1 matrix and the activations the same x^ for both; each form keeps them the way a program that calls it
-would (weights in float32 and x^ in the activations' type for the plain form, packed bits and codes for the package).
+would (the plain form weights in float32, q and s, and x^ of mx4 in the activations' type; the package packed bits and codes).
 """
 from __future__ import annotations
 
@@ -31,7 +32,6 @@ DEV = "cuda:0"
 EPS = 1e-5
 TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 BYTES = {"bf16": 2, "f16": 2, "f32": 4}
-CODE_BITS = {"e4m3": 8, "e2m1": 4}
 
 MAX_FLOPS = 2 * 8192 * 4096 * 16384        # the largest listed product (gated_8192x4096x8192)
 MAX_NORM_REALS = 16384 * 4096              # elements of the largest listed matrix of the norms
@@ -41,39 +41,39 @@ MAX_REALS = 16384 * 8192                   # elements of the largest listed matr
 def listed():
     return [
         # A ragged batch of a program in 32 bits: rows of odd length whose last block is not whole.
-        {"name": "quantise_1000x2047_f32_e2m1", "op": "quantise", "format": "e2m1", "type": "f32", "M": 1000, "K": 2047},
+        {"name": "quantise_1000x2047_f32_mx4", "op": "quantise", "format": "mx4", "type": "f32", "M": 1000, "K": 2047},
         # The hidden activations of long prompts.
-        {"name": "quantise_16384x8192_bf16_e4m3", "op": "quantise", "format": "e4m3", "type": "bf16", "M": 16384, "K": 8192},
+        {"name": "quantise_16384x8192_bf16_i8", "op": "quantise", "format": "i8", "type": "bf16", "M": 16384, "K": 8192},
         # Between two blocks, a token at a time.
-        {"name": "norm_1x4096_bf16_e4m3", "op": "norm", "format": "e4m3", "type": "bf16", "M": 1, "D": 4096, "rows_per_gate": 1,
+        {"name": "norm_1x4096_bf16_i8", "op": "norm", "format": "i8", "type": "bf16", "M": 1, "D": 4096, "rows_per_gate": 1,
          "x": True, "gate": True, "post": "rms", "pre": "rms"},
         # A ragged prompt with rows of odd length, layer norms and a gate for each 100 rows.
-        {"name": "norm_333x2049_f16_e4m3", "op": "norm", "format": "e4m3", "type": "f16", "M": 333, "D": 2049, "rows_per_gate": 100,
+        {"name": "norm_333x2049_f16_i8", "op": "norm", "format": "i8", "type": "f16", "M": 333, "D": 2049, "rows_per_gate": 100,
          "x": True, "gate": True, "post": "layer", "pre": "layer"},
         # Between two blocks of a long batch.
-        {"name": "norm_16384x4096_bf16_e4m3", "op": "norm", "format": "e4m3", "type": "bf16", "M": 16384, "D": 4096,
+        {"name": "norm_16384x4096_bf16_i8", "op": "norm", "format": "i8", "type": "bf16", "M": 16384, "D": 4096,
          "rows_per_gate": 16384, "x": True, "gate": False, "post": "rms", "pre": "rms"},
         # The block's second product for a few sequences, a token each, added to the stream.
-        {"name": "linear_8x8192x4096_bf16_e2m1", "op": "linear", "format": "e2m1", "type": "bf16", "M": 8, "K": 8192, "N": 4096,
+        {"name": "linear_8x8192x4096_bf16_mx4", "op": "linear", "format": "mx4", "type": "bf16", "M": 8, "K": 8192, "N": 4096,
          "act": "none", "scale": True, "bias": True, "residual": True},
         # A layer of the framework's MLP on quantised inputs, results in its own 32 bits.
-        {"name": "linear_1000x784x4096_f32_e4m3", "op": "linear", "format": "e4m3", "type": "f32", "M": 1000, "K": 784, "N": 4096,
+        {"name": "linear_1000x784x4096_f32_i8", "op": "linear", "format": "i8", "type": "f32", "M": 1000, "K": 784, "N": 4096,
          "act": "relu", "scale": True, "bias": True, "residual": False},
         # The block's second product for long prompts.
-        {"name": "linear_8192x8192x4096_bf16_e4m3", "op": "linear", "format": "e4m3", "type": "bf16", "M": 8192, "K": 8192, "N": 4096,
+        {"name": "linear_8192x8192x4096_bf16_i8", "op": "linear", "format": "i8", "type": "bf16", "M": 8192, "K": 8192, "N": 4096,
          "act": "none", "scale": True, "bias": False, "residual": True},
-        # One token through the first half of a served model's block, quantised for the second.
-        {"name": "gated_1x4096x8192_bf16_e4m3", "op": "gated", "format": "e4m3", "type": "bf16", "M": 1, "K": 4096, "F": 8192,
-         "act": "silu", "scale": True, "bias": False, "out": True},
+        # One token through the first half of a served model's block.
+        {"name": "gated_1x4096x8192_bf16_i8", "op": "gated", "format": "i8", "type": "bf16", "M": 1, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False},
         # A ragged prompt with sizes that fit no tile.
-        {"name": "gated_333x1000x2047_f16_e2m1", "op": "gated", "format": "e2m1", "type": "f16", "M": 333, "K": 1000, "F": 2047,
-         "act": "gelu_tanh", "scale": True, "bias": True, "out": False},
+        {"name": "gated_333x1000x2047_f16_mx4", "op": "gated", "format": "mx4", "type": "f16", "M": 333, "K": 1000, "F": 2047,
+         "act": "gelu_tanh", "scale": True, "bias": True},
         # Long prompts in 4 bits.
-        {"name": "gated_8192x4096x8192_bf16_e2m1", "op": "gated", "format": "e2m1", "type": "bf16", "M": 8192, "K": 4096, "F": 8192,
-         "act": "silu", "scale": True, "bias": False, "out": False},
+        {"name": "gated_8192x4096x8192_bf16_mx4", "op": "gated", "format": "mx4", "type": "bf16", "M": 8192, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False},
         # The forward half of a training step in 8 bits.
-        {"name": "gated_4096x4096x8192_bf16_e4m3", "op": "gated", "format": "e4m3", "type": "bf16", "M": 4096, "K": 4096, "F": 8192,
-         "act": "silu", "scale": True, "bias": False, "out": True},
+        {"name": "gated_4096x4096x8192_bf16_i8", "op": "gated", "format": "i8", "type": "bf16", "M": 4096, "K": 4096, "F": 8192,
+         "act": "silu", "scale": True, "bias": False},
     ]
 
 
@@ -90,7 +90,7 @@ def _size(rng, lo, hi, step):
 def draw(rng):
     while True:
         op = rng.choice(["quantise", "norm", "linear", "gated"])
-        case = {"op": op, "format": rng.choice(["e4m3", "e2m1"]), "type": rng.choice(["bf16", "bf16", "bf16", "f16", "f16", "f32"])}
+        case = {"op": op, "format": rng.choice(["i8", "mx4"]), "type": rng.choice(["bf16", "bf16", "bf16", "f16", "f16", "f32"])}
         if op == "quantise":
             case.update(M=_log_int(rng, 1, 32768), K=_size(rng, 64, 16384, 64))
             if case["M"] * case["K"] <= MAX_REALS:
@@ -100,7 +100,7 @@ def draw(rng):
             M = _log_int(rng, 1, 32768)
             if case["type"] == "f32":
                 continue
-            case.update(format="e4m3", M=M, D=_size(rng, 64, 8192, 64), rows_per_gate=rng.choice([1, M, _log_int(rng, 1, M)]),
+            case.update(format="i8", M=M, D=_size(rng, 64, 8192, 64), rows_per_gate=rng.choice([1, M, _log_int(rng, 1, M)]),
                         x=rng.random() < 0.8, gate=rng.random() < 0.6, post=rng.choice(["none", "rms", "layer"]),
                         pre=rng.choice(["rms", "rms", "layer"]))
             if case["M"] * case["D"] <= MAX_NORM_REALS:
@@ -110,8 +110,7 @@ def draw(rng):
         acts = ["silu", "gelu", "gelu_tanh", "sigmoid", "relu"]
         case.update(M=M, K=_size(rng, 256, 8192, 128))
         if op == "gated":
-            out = case["format"] == "e4m3" and case["type"] != "f32" and rng.random() < 0.6
-            case.update(F=_size(rng, 256, 8192, 128), act=rng.choice(acts), scale=True, bias=rng.random() < 0.4, out=out)
+            case.update(F=_size(rng, 256, 8192, 128), act=rng.choice(acts), scale=True, bias=rng.random() < 0.4)
             n = 2 * case["F"]
         else:
             n = _size(rng, 256, 8192, 128)
@@ -165,25 +164,25 @@ def prepare(case, seed):
     st.update(case=case, T=TYPES[case["type"]])
     if own:
         import paper_1602_02830_amd as bnn
-        st["bnn"], st["format"] = bnn, {"e4m3": bnn.MX_E4M3, "e2m1": bnn.MX_E2M1}[case["format"]]
+        st["bnn"], st["format"] = bnn, {"i8": bnn.ROWS_I8, "mx4": bnn.ROWS_MX4}[case["format"]]
         st["act"] = {"none": bnn.ACT_NONE, "relu": bnn.ACT_RELU, "silu": bnn.ACT_SILU, "gelu": bnn.ACT_GELU,
                      "gelu_tanh": bnn.ACT_GELU_TANH, "sigmoid": bnn.ACT_SIGMOID}[case.get("act", "none")]
         if case["op"] == "quantise":
-            st["out_mx"] = bnn.mx_rows(case["M"], case["K"], st["format"], device=DEV, hat=st["T"])
+            st["out_q"] = bnn.quantized_rows(case["M"], case["K"], st["format"], device=DEV, hat=st["T"])
         elif case["op"] == "norm":
             st["kinds"] = {"none": bnn.NORM_NONE, "rms": bnn.NORM_RMS, "layer": bnn.NORM_LAYER}
             st["out_r"] = torch.empty_like(st["y"])
-            st["out_mx"] = bnn.mx_rows(case["M"], case["D"], st["format"], device=DEV, hat=st["T"])
+            st["out_q"] = bnn.quantized_rows(case["M"], case["D"], st["format"], device=DEV, hat=st["T"])
         else:
-            st["x"] = bnn.mx_quantize(st["x"], st["format"])
+            st["x"] = bnn.quantize_rows(st["x"], st["format"])
             st["w_bits"] = bnn.pack_sign(st.pop("w"))
-            cols = case["F"] if case["op"] == "gated" else case["N"]
-            if case.get("out"):
-                st["out_mx"] = bnn.mx_rows(case["M"], cols, st["format"], device=DEV, hat=st["T"])
-            else:
-                st["out"] = torch.empty((case["M"], cols), dtype=st["T"], device=DEV)
+            st["out"] = torch.empty((case["M"], case["F"] if case["op"] == "gated" else case["N"]), dtype=st["T"], device=DEV)
     elif case["op"] in ("linear", "gated"):
-        st["x"] = _plain_hat(st["x"].float(), case["format"]).to(st["T"])       # exact in each type
+        x = st.pop("x").float()
+        if case["format"] == "i8":
+            st["q"], st["s"] = _plain_i8(x)
+        else:
+            st["x"] = _plain_mx4(x).to(st["T"])       # exact in each type
     return st
 
 
@@ -201,17 +200,15 @@ def run(st):
 def _own(st):
     bnn, case = st["bnn"], st["case"]
     if case["op"] == "quantise":
-        return bnn.mx_quantize(st["x"], st["format"], out=st["out_mx"]).hat
+        return bnn.quantize_rows(st["x"], st["format"], out=st["out_q"]).hat
     if case["op"] == "norm":
-        r, n = bnn.norm_residual_mx(st["y"], st["x"], st["gate"], st["res_scale"], st["kinds"][case["post"]], st["post_gamma"],
-                                    st["post_beta"], st["kinds"][case["pre"]], st["pre_gamma"], st["pre_beta"], EPS,
-                                    case["rows_per_gate"], format=st["format"], out=st["out_r"], out_mx=st["out_mx"])
+        r, n = bnn.norm_residual_q(st["y"], st["x"], st["gate"], st["res_scale"], st["kinds"][case["post"]], st["post_gamma"],
+                                   st["post_beta"], st["kinds"][case["pre"]], st["pre_gamma"], st["pre_beta"], EPS,
+                                   case["rows_per_gate"], st["format"], out=st["out_r"], out_q=st["out_q"])
         return {"r": r, "n": n.hat}
     if case["op"] == "linear":
-        return bnn.linear_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], st["residual"], out=st["out"])
-    if case["out"]:
-        return bnn.gated_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], out_mx=st["out_mx"]).hat
-    return bnn.gated_mx(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], out=st["out"])
+        return bnn.linear_q_bits(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], st["residual"], out=st["out"])
+    return bnn.gated_q_bits(st["x"], st["w_bits"], st["scale"], st["bias"], st["act"], out=st["out"])
 
 
 # ---- plain forms: elementary operations in 32 bits, rounded once at the end ----------------------------------
@@ -221,20 +218,31 @@ def _power(e):
     return ((e + 127) << 23).to(torch.int32).view(torch.float32)
 
 
-def _plain_hat(x, fmt):
+def _plain_i8(x):
+    """q and s of float32 rows; the quotients in 64 bits, in which those next to a border fall on their own side of it."""
+    s = torch.clamp(x.abs().amax(dim=1, keepdim=True) / 127, min=2.0 ** -126)
+    return torch.round(x.double() / s.double()).to(torch.int8), s
+
+
+def _plain_mx4(x):
     """x^ of float32 rows."""
     M, K = x.shape
-    largest, least, digits = (8, -6, 3) if fmt == "e4m3" else (2, 0, 1)         # exponents of the largest and least normal code
     blocks = -(-K // 32)
     v = torch.cat([x, x.new_zeros(M, 32 * blocks - K)], dim=1) if 32 * blocks > K else x
     v = v.view(M, blocks, 32)
-    mantissa, exponent = torch.frexp(v.abs().amax(dim=2, keepdim=True))          # in [0.5, 1)
-    past = mantissa > 464 / 512 if fmt == "e4m3" else mantissa >= 7 / 8
-    e = torch.clamp(exponent - 1 - largest + past.to(exponent.dtype), min=-126)
+    mantissa, exponent = torch.frexp(v.abs().amax(dim=2, keepdim=True))          # mantissa in [0.5, 1)
+    e = torch.clamp(exponent - 3 + (mantissa >= 7 / 8).to(exponent.dtype), min=-126)
     v = v * _power(-e)
-    step = _power(torch.clamp(torch.frexp(v)[1] - 1, min=least) - digits)
+    step = _power(torch.clamp(torch.frexp(v)[1] - 1, min=0) - 1)                  # 0.5 below 2, 1 below 4, 2 from there on
     v = torch.round(v / step) * step * _power(e)
     return v.view(M, 32 * blocks)[:, :K]
+
+
+def _plain_hat(x, fmt):
+    if fmt == "mx4":
+        return _plain_mx4(x)
+    q, s = _plain_i8(x)
+    return q.float() * s
 
 
 def _act(z, name):
@@ -253,15 +261,14 @@ def _act(z, name):
 
 def _plain_product(st):
     case, T = st["case"], st["T"]
-    z = st["x"].float() @ st["w"].t()
+    z = (st["q"].float() @ st["w"].t()) * st["s"] if case["format"] == "i8" else st["x"].float() @ st["w"].t()
     if st["scale"] is not None:
         z = z * st["scale"]
     if st["bias"] is not None:
         z = z + st["bias"]
     if case["op"] == "gated":
         F = case["F"]
-        h = _act(z[:, :F], case["act"]) * z[:, F:]
-        return (_plain_hat(h, case["format"]) if case["out"] else h).to(T)
+        return (_act(z[:, :F], case["act"]) * z[:, F:]).to(T)
     y = _act(z, case["act"])
     if st["residual"] is not None:
         y = y + st["residual"].float()
@@ -292,7 +299,7 @@ def _plain_norm(st):
 
 def _codes(case, rows, cols):
     """Bytes of quantised rows: codes and scales."""
-    return rows * (cols * CODE_BITS[case["format"]] // 8 + -(-cols // 32))
+    return rows * (cols + 4) if case["format"] == "i8" else rows * (cols // 2 + -(-cols // 32))
 
 
 def work(case):
@@ -308,20 +315,28 @@ def work(case):
     K, gated = case["K"], case["op"] == "gated"
     N, cols = (2 * case["F"], case["F"]) if gated else (case["N"], case["N"])
     b = _codes(case, M, K) + 4 * N * ((K + 31) // 32) + 4 * N * (case["scale"] + case["bias"])
-    b += size * M * cols * (1 + case.get("residual", False)) + (_codes(case, M, cols) if case.get("out") else 0)
+    b += size * M * cols * (1 + case.get("residual", False))
     return {"bytes": b, "flops": 2 * M * N * K}
 
 
 # ---- the same results from the definitions, in 64 bits -------------------------------------------------------
 
-#: The magnitudes that codes stand for, in the order of the codes, and the one that would follow the largest.
-_E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 8.0]
-_E4M3 = [i / 512 for i in range(8)] + [(8 + i) * 2.0 ** (e - 3) for e in range(-6, 9) for i in range(8)]      # the last one: 480
+def _exact_i8(v):
+    """s is a number of 32 bits by definition; q the nearest whole number to v / s."""
+    s = torch.clamp((v.abs().max(dim=1, keepdim=True).values / 127).float().double(), min=2.0 ** -126)
+    q = torch.floor(v / s)
+    rest = v / s - q
+    up = (rest > 0.5) | ((rest == 0.5) & (torch.remainder(q, 2) == 1))
+    return (q + up.double()) * s
 
 
-def _exact_hat(v, fmt):
-    """The nearest codes, even ones between two, looked up in a table; of rows in 64 bits."""
-    table = torch.tensor(_E4M3 if fmt == "e4m3" else _E2M1, dtype=torch.float64, device=DEV)
+#: The magnitudes that codes of 4 bits stand for, in the order of the codes, and the one that would follow the largest.
+_MX4 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 8.0]
+
+
+def _exact_mx4(v):
+    """The nearest codes, even ones between two, looked up in a table."""
+    table = torch.tensor(_MX4, dtype=torch.float64, device=DEV)
     border = (table[1:] + table[:-1]) / 2
 
     def nearest(a):
@@ -329,19 +344,22 @@ def _exact_hat(v, fmt):
         tie = border[torch.clamp(below, max=border.numel() - 1)] == a
         return below + (tie & (below % 2 == 1)).long()
 
-    M, K = v.shape
-    out = torch.zeros_like(v)
-    rows = max(1, (1 << 24) // max(K, 1))
-    for first in range(0, M, rows):                                 # a part at a time: look-ups take memory
-        part = v[first:first + rows]
-        part = torch.nn.functional.pad(part, (0, -K % 32)).reshape(part.shape[0], -1, 32)
-        peak = part.abs().max(dim=2, keepdim=True).values
-        # The largest code is below 2^9 (2^3): one of two exponents.
-        low = torch.floor(torch.log2(torch.clamp(peak, min=2.0 ** -100))) - (8 if fmt == "e4m3" else 2)
-        unit = ((low.long() + 1023) << 52).view(torch.float64)      # 2^low
-        unit = torch.where(nearest(peak / unit) < table.numel() - 1, unit, 2 * unit)
-        got = torch.sign(part) * table[nearest((part / unit).abs())] * unit
-        out[first:first + rows] = got.reshape(got.shape[0], -1)[:, :K]
+    part = torch.nn.functional.pad(v, (0, -v.shape[1] % 32)).reshape(v.shape[0], -1, 32)
+    peak = part.abs().max(dim=2, keepdim=True).values
+    # The largest code is below 2^3: one of two exponents.
+    low = torch.floor(torch.log2(torch.clamp(peak, min=2.0 ** -100))) - 2
+    unit = ((low.long() + 1023) << 52).view(torch.float64)           # 2^low
+    unit = torch.where(nearest(peak / unit) < table.numel() - 1, unit, 2 * unit)
+    got = torch.sign(part) * table[nearest((part / unit).abs())] * unit
+    return got.reshape(got.shape[0], -1)[:, :v.shape[1]]
+
+
+def _exact_hat(v, fmt):
+    """x^ of rows in 64 bits, a part of them at a time: look-ups take memory."""
+    out = torch.empty_like(v)
+    rows = max(1, (1 << 24) // max(v.shape[1], 1))
+    for first in range(0, v.shape[0], rows):
+        out[first:first + rows] = (_exact_i8 if fmt == "i8" else _exact_mx4)(v[first:first + rows])
     return out
 
 
@@ -367,8 +385,6 @@ def _exact_norm_of(v, kind, gamma, beta):
 
 
 def exact(case, seed):
-    if case["op"] == "gated" and case["out"]:
-        return None
     d = _draws(case, seed)
     if case["op"] == "quantise":
         return _exact_hat(d["x"].double(), case["format"])
