@@ -451,6 +451,56 @@ int bnn_norm_residual_backward(int type, const void *dr, int64_t ld_dr, const vo
                                float *dpost_beta, float *dpre_gamma, float *dpre_beta, int64_t M, int64_t D,
                                void *workspace, int64_t workspace_bytes, void *stream);
 
+/* ---- quantised activations, packed weights -----------------------------------------------------------------------
+ *
+ * Rows of activations as codes of 8 or 4 bits with scales.  x^ is what they stand for:
+ *   BNN_ROWS_I8   x^ = s q,   q a whole number in [-127, 127], s a float32 for each row: its largest magnitude / 127, and 2^-126 at
+ *                 least.  A row with an infinity or a NaN has the scale NaN and codes of 0.
+ *   BNN_ROWS_MX4  x^ = 2^e c, c one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (the 4-bit floating point codes e2m1), e for each 32
+ *                 elements of a row the smallest exponent with which the largest magnitude of them does not round past 6, and -126
+ *                 at least; held as the byte e + 127, 255 for a block with an infinity or a NaN, whose codes mean nothing.
+ * q and c are the nearest ones to x / s and x / 2^e, of two as near the even code.
+ *   codes   [M][ld_c] bytes, 16-byte aligned, ld_c a multiple of 16 and at least 32 (I8) or 16 (MX4) times ceil(K / 32): whole
+ *           blocks of 32 elements, those past K zero.  Byte 4 i + j of an I8 block is element 8 j + i, nibble 8 i + j of an MX4 block
+ *           (the lower half of a byte first) is element 4 j + i.
+ *   scales  I8: float [M].  MX4: bytes [M][ld_s], ld_s a multiple of 4 and at least ceil(K / 32).  4-byte aligned.
+ * Leading dimensions of reals as above.
+ */
+typedef enum bnn_rows { BNN_ROWS_I8 = 0, BNN_ROWS_MX4 = 1 } bnn_rows;
+
+/*
+ * bnn_quantize_rows: x [M][ld_x] of `type` to codes and scales, and x^ rounded to `type` in hat [M][ld_h], which may be NULL or x
+ *   itself (same address and leading dimension).  x^ of MX4 is a number of each type, but for float16's range.
+ * bnn_dequantize_rows: x^ of codes and scales, rounded to `type`.
+ */
+int bnn_quantize_rows(int rows, int type, const void *x, int64_t ld_x, uint8_t *codes, int64_t ld_c, void *scales, int64_t ld_s,
+                      void *hat, int64_t ld_h, int64_t M, int64_t K, void *stream);
+int bnn_dequantize_rows(int rows, int type, const uint8_t *codes, int64_t ld_c, const void *scales, int64_t ld_s, void *x,
+                        int64_t ld_x, int64_t M, int64_t K, void *stream);
+
+/*
+ * bnn_norm_residual with n quantised: codes and scales of n (of r, if pre is BNN_NORM_NONE), taken of the unrounded values; hat [M][ld_h]
+ * of `type` (or NULL) gets n^.  r may be NULL, or x itself.
+ */
+int bnn_norm_residual_q(int type, const void *y, int64_t ld_y, const void *x, int64_t ld_x, const void *gate, int64_t ld_gate,
+                        int64_t rows_per_gate, float res_scale, int post, const float *post_gamma, const float *post_beta, int pre,
+                        const float *pre_gamma, const float *pre_beta, float eps, void *r, int64_t ld_r, int rows, uint8_t *codes,
+                        int64_t ld_c, void *scales, int64_t ld_s, void *hat, int64_t ld_h, int64_t M, int64_t D, void *stream);
+
+/*
+ * bnn_linear_bits and bnn_gated_bits on quantised rows x^ of K elements; residual, y and h of `type`.  The sums of I8 rows are
+ * exact (whole numbers, before the scales), those of MX4 rows float32.  K up to 2^18 for I8, else BNN_ERR_UNSUPPORTED: sums are held
+ * in 32 bits.
+ * The gated product may give its result quantised, for the product that reads it: with out_codes [M][ld_oc] and out_scales
+ * [M][ld_os], MX4 rows of F elements taken of the unrounded h, and h (or NULL) gets h^.  Without: NULL.
+ */
+int bnn_linear_q_bits(int rows, const uint8_t *codes, int64_t ld_c, const void *scales, int64_t ld_s, const uint32_t *w, int64_t ld_w,
+                      const float *scale, const float *bias, int act, int type, const void *residual, int64_t ld_r, void *y,
+                      int64_t ld_y, int64_t M, int64_t N, int64_t K, void *stream);
+int bnn_gated_q_bits(int rows, const uint8_t *codes, int64_t ld_c, const void *scales, int64_t ld_s, const uint32_t *w, int64_t ld_w,
+                     const float *scale, const float *bias, int act, int type, void *h, int64_t ld_h, uint8_t *out_codes,
+                     int64_t ld_oc, uint8_t *out_scales, int64_t ld_os, int64_t M, int64_t F, int64_t K, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,7 @@ POOL_APART, POOL_IN_CONV, POOL_WINDOWS = range(3)
 
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_SIGMOID = range(6)
 NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+ROWS_I8, ROWS_MX4 = range(2)                                             # bnn_rows
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}         # bnn_type
 
 _i64 = ctypes.c_int64
@@ -78,6 +79,14 @@ _SIGNATURES = {
     "bnn_norm_residual_backward": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _f32, _int,
                                           _ptr, _ptr, _int, _ptr, _f32, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _ptr,
                                           _ptr, _i64, _i64, _ptr, _i64, _ptr]),
+    "bnn_quantize_rows": (_int, [_int, _int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _i64, _ptr]),
+    "bnn_dequantize_rows": (_int, [_int, _int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _i64, _ptr]),
+    "bnn_norm_residual_q": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _f32, _int, _ptr, _ptr, _int, _ptr, _ptr, _f32,
+                                   _ptr, _i64, _int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _i64, _i64, _ptr]),
+    "bnn_linear_q_bits": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _int, _ptr, _i64, _ptr, _i64, _i64, _i64,
+                                 _i64, _ptr]),
+    "bnn_gated_q_bits": (_int, [_int, _ptr, _i64, _ptr, _i64, _ptr, _i64, _ptr, _ptr, _int, _int, _ptr, _i64, _ptr, _i64, _ptr, _i64,
+                                _i64, _i64, _i64, _ptr]),
 }
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -939,3 +948,330 @@ def norm_residual_backward(dr: torch.Tensor | None, dn: torch.Tensor | None, y: 
                                           *(None if got["d" + k] is None else got["d" + k].data_ptr() for k in vectors), M, D,
                                           ws.data_ptr(), ws.numel(), _stream(y)))
     return got
+
+
+# ---- quantised activations, packed weights ----------------------------------------------------------------------
+
+class QuantizedRows:
+    """Rows of K activations as codes with scales (bnn_rows): ``kind`` ROWS_I8 or ROWS_MX4, ``codes`` uint8 [M][bytes], ``scales``
+    float32 [M] (I8) or uint8 [M][bytes] (MX4), and ``hat``, the values x^ that they stand for in a real type, or None.  hat is
+    what torch differentiates: its gradient is that of the values that were quantised (straight through)."""
+    __slots__ = ("kind", "K", "codes", "scales", "hat")
+
+    def __init__(self, kind: int, K: int, codes: torch.Tensor, scales: torch.Tensor, hat: torch.Tensor | None = None):
+        self.kind, self.K, self.codes, self.scales, self.hat = kind, K, codes, scales, hat
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.K
+
+
+def _blocks(K: int) -> int:
+    return (K + 31) // 32
+
+
+def quantized_rows(M: int, K: int, kind: int = ROWS_I8, device="cuda", hat: torch.dtype | None = None) -> QuantizedRows:
+    """Rows to be written: memory for M x K codes and their scales, and for x^ in the type `hat`."""
+    if kind not in (ROWS_I8, ROWS_MX4):
+        raise ValueError("kind must be ROWS_I8 or ROWS_MX4")
+    if M < 0 or K < 0:
+        raise ValueError("sizes must not be negative")
+    codes = torch.empty((M, _blocks(K) * (32 if kind == ROWS_I8 else 16)), dtype=torch.uint8, device=device)
+    scales = torch.empty(M, dtype=torch.float32, device=device) if kind == ROWS_I8 else \
+        torch.empty((M, (_blocks(K) + 3) // 4 * 4), dtype=torch.uint8, device=device)
+    return QuantizedRows(kind, K, codes, scales, None if hat is None else torch.empty((M, K), dtype=hat, device=device))
+
+
+def _rows_at(q: QuantizedRows, M: int, K: int, device, name: str):
+    """Addresses and leading dimensions of codes and scales of M x K elements on `device`."""
+    if not isinstance(q, QuantizedRows):
+        raise ValueError(f"{name} must be QuantizedRows")
+    if q.kind not in (ROWS_I8, ROWS_MX4):
+        raise ValueError(f"{name}: kind must be ROWS_I8 or ROWS_MX4")
+    c, s = q.codes, q.scales
+    _dev(c, torch.uint8, f"{name}: codes")
+    if q.K != K or c.shape[0] != M or c.shape[1] < _blocks(K) * (32 if q.kind == ROWS_I8 else 16):
+        raise ValueError(f"{name} must have codes of {M} rows of {K} elements")
+    if c.device != device or s.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if q.kind == ROWS_I8:
+        if s.dtype != torch.float32 or tuple(s.shape) != (M,) or not s.is_contiguous():
+            raise ValueError(f"{name}: scales must be a contiguous float32 vector of {M} elements")
+        return c.data_ptr(), _ld(c), s.data_ptr(), 0
+    _dev(s, torch.uint8, f"{name}: scales")
+    if s.shape[0] != M or s.shape[1] < (_blocks(K) + 3) // 4 * 4:
+        raise ValueError(f"{name}: scales must be {M} rows of a byte for each 32 elements, whole groups of four")
+    return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
+
+
+def _count_rows(q: QuantizedRows | None):
+    if q is not None:
+        for t in (q.codes, q.scales, q.hat):
+            _count_write(t)
+
+
+class _QuantizeRows(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, kind):
+        q = quantize_rows(x, kind, hat=True)
+        ctx.mark_non_differentiable(q.codes, q.scales)
+        return q.codes, q.scales, q.hat
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, _, __, dhat):
+        return dhat, None
+
+
+def quantize_rows(x: torch.Tensor, kind: int = ROWS_I8, hat: bool = False, out: QuantizedRows | None = None) -> QuantizedRows:
+    """bnn_quantize_rows: real rows [M][K] as codes with scales; `hat`: x^ too.  Without `out`, of rows that require a gradient, x^ is
+    always made, and torch differentiates it as if it were x."""
+    if out is not None and _calls is not None:
+        st = _calls.quantize_rows(x, out.kind, out.K, out.codes, out.scales, out.hat)
+        if st == 0 or _took("bnn_quantize_rows", st):
+            return out
+    if out is None and _recorded(x):
+        return QuantizedRows(kind, x.shape[1], *_QuantizeRows.apply(x, kind))
+    lib = load_library()
+    _real(x, "x")
+    M, K = x.shape
+    given = out
+    if out is None:
+        out = quantized_rows(M, K, kind, x.device, x.dtype if hat else None)
+    at = _rows_at(out, M, K, x.device, "out")
+    if out.hat is not None:
+        _sized(out.hat, M, K, "out: hat", x)
+    _check("bnn_quantize_rows", lib.bnn_quantize_rows(out.kind, _TYPES[x.dtype], *_at(x), *at, *_at(out.hat), M, K, _stream(x)))
+    _count_rows(given)
+    return out
+
+
+def dequantize_rows(q: QuantizedRows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """bnn_dequantize_rows: x^ [M][K]."""
+    lib = load_library()
+    M, K = q.shape
+    at = _rows_at(q, M, K, q.codes.device, "q")
+    given = out
+    if out is None:
+        _real_type(dtype)
+        out = torch.empty((M, K), dtype=dtype, device=q.codes.device)
+    _real(out, "out")
+    if out.device != q.codes.device or tuple(out.shape) != (M, K):
+        raise ValueError(f"out must be [{M}][{K}] on {q.codes.device}")
+    _check("bnn_dequantize_rows", lib.bnn_dequantize_rows(q.kind, _TYPES[out.dtype], *at, *_at(out), M, K, _stream(out)))
+    _count_write(given)
+    return out
+
+
+class _NormResidualQ(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, kind):
+        r, q = norm_residual_q(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, kind,
+                               hat=True)
+        ctx.save_for_backward(y, r if pre != NORM_NONE else None, gate, post_gamma, post_beta, pre_gamma, pre_beta)
+        ctx.kinds = res_scale, post, pre, eps, rows_per_gate
+        ctx.mark_non_differentiable(q.codes, q.scales)
+        ctx.set_materialize_grads(False)
+        return r, q.codes, q.scales, q.hat
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dr, _, __, dhat):
+        if ctx.kinds[2] == NORM_NONE:          # the codes are r's
+            dr, dhat = dhat if dr is None else dr if dhat is None else dr + dhat, None
+        return *_NormResidual.backward(ctx, dr, dhat), None
+
+
+def norm_residual_q(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Tensor | None = None, res_scale: float = 1.0,
+                    post: int = NORM_NONE, post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None,
+                    pre: int = NORM_NONE, pre_gamma: torch.Tensor | None = None, pre_beta: torch.Tensor | None = None,
+                    eps: float = 1e-5, rows_per_gate: int = 1, kind: int = ROWS_I8, out: torch.Tensor | None = None,
+                    out_q: QuantizedRows | None = None, need_r: bool = True, hat: bool = False):
+    """bnn_norm_residual_q: norm_residual whose n (r, without a `pre` norm) comes as codes with scales: (r, QuantizedRows), with x^ where
+    `hat` or out_q has it.  Without `out` and `out_q`, of tensors that require a gradient, n^ is always made, and torch differentiates
+    it as if it were n."""
+    if out is not None and out_q is not None and _calls is not None:
+        st = _calls.norm_residual_q(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
+                                    out, out_q.kind, out_q.K, out_q.codes, out_q.scales, out_q.hat)
+        if st == 0 or _took("bnn_norm_residual_q", st):
+            return out, out_q
+    if out is None and out_q is None and _recorded(y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta):
+        r, *q = _NormResidualQ.apply(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, kind)
+        return (r if need_r else None), QuantizedRows(kind, y.shape[1], *q)
+    lib = load_library()
+    _real(y, "y")
+    M, D = y.shape
+    if x is not None:
+        _sized(x, M, D, "x", y)
+    if gate is not None:
+        if rows_per_gate < 1:
+            raise ValueError("rows_per_gate must be positive")
+        _sized(gate, -(-M // rows_per_gate), D, "gate", y)
+    given = out, out_q
+    if out is None and need_r:
+        out = torch.empty((M, D), dtype=y.dtype, device=y.device)
+    if out is not None:
+        _sized(out, M, D, "out", y)
+    if out_q is None:
+        out_q = quantized_rows(M, D, kind, y.device, y.dtype if hat else None)
+    at = _rows_at(out_q, M, D, y.device, "out_q")
+    if out_q.hat is not None:
+        _sized(out_q.hat, M, D, "out_q: hat", y)
+    _check("bnn_norm_residual_q",
+           lib.bnn_norm_residual_q(_TYPES[y.dtype], *_at(y), *_at(x), *_at(gate), rows_per_gate, res_scale, post,
+                                   _vector(post_gamma, D, "post_gamma", y), _vector(post_beta, D, "post_beta", y), pre,
+                                   _vector(pre_gamma, D, "pre_gamma", y), _vector(pre_beta, D, "pre_beta", y), eps,
+                                   *_at(out), out_q.kind, *at, *_at(out_q.hat), M, D, _stream(y)))
+    _count_write(given[0])
+    _count_rows(given[1])
+    return out, out_q
+
+
+class _LinearQBits(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hat, scale, bias, residual, q, w_bits, act, dtype):
+        ctx.save_for_backward(hat, q.codes, q.scales, w_bits, scale, bias)
+        ctx.kinds = q.kind, q.K, act, dtype
+        return linear_q_bits(q, w_bits, scale, bias, act, residual, dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return *_q_gradients(ctx, linear_bits_backward, dy), dy if ctx.needs_input_grad[3] else None, None, None, None, None
+
+
+class _GatedQBits(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hat, scale, bias, q, w_bits, act, dtype, out_kind):
+        ctx.save_for_backward(hat, q.codes, q.scales, w_bits, scale, bias)
+        ctx.kinds = q.kind, q.K, act, dtype
+        if out_kind is None:
+            return gated_q_bits(q, w_bits, scale, bias, act, dtype)
+        h = gated_q_bits(q, w_bits, scale, bias, act, dtype, out_kind=out_kind, hat=True)
+        ctx.mark_non_differentiable(h.codes, h.scales)
+        return h.hat, h.codes, h.scales
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, *_):
+        return *_q_gradients(ctx, gated_bits_backward, dh), None, None, None, None, None
+
+
+def _q_gradients(ctx, call, dy):
+    """Of x^, scale and bias: those of the product at the values that the codes stand for."""
+    need_x, need_scale, need_bias = ctx.needs_input_grad[:3]
+    if not (need_x or need_scale or need_bias):
+        return None, None, None
+    hat, codes, scales, w_bits, scale, bias = ctx.saved_tensors
+    kind, K, act, dtype = ctx.kinds
+    if hat is None:
+        hat = dequantize_rows(QuantizedRows(kind, K, codes, scales), dtype)
+    got = call(dy.contiguous(), hat, w_bits, scale, bias, act, need_dx=need_x, need_dw=False)
+    return got["dx"], got["dscale"] if need_scale else None, got["dbias"] if need_bias else None
+
+
+def _q_weights(q: QuantizedRows, w_bits: torch.Tensor, dtype: torch.dtype):
+    """Addresses of the rows, and a tensor that stands for the result's type and device."""
+    if not isinstance(q, QuantizedRows):
+        raise ValueError("x must be QuantizedRows")
+    _real_type(dtype)
+    at = _rows_at(q, q.codes.shape[0], q.K, q.codes.device, "x")
+    _dev(w_bits, torch.int32, "w_bits")
+    if w_bits.device != q.codes.device:
+        raise ValueError(f"w_bits must be on {q.codes.device}")
+    if w_bits.shape[1] < words_per_row(q.K):
+        raise ValueError("packed weights have fewer words per row than x has columns")
+    return at, torch.empty((0, 0), dtype=dtype, device=q.codes.device)
+
+
+def _differentiable_hat(q: QuantizedRows, dtype: torch.dtype):
+    """x^ where torch has a gradient of it to give."""
+    if q.hat is None or not q.hat.requires_grad:
+        return None
+    if q.hat.dtype != dtype:
+        raise ValueError(f"a result that torch differentiates must be of the type of x^, {q.hat.dtype}")
+    return q.hat
+
+
+def linear_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                  act: int = ACT_NONE, residual: torch.Tensor | None = None, dtype: torch.dtype | None = None,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """bnn_linear_q_bits: quantised rows x^ [M][K], packed weights [N][ceil(K/32)] -> act(scale * (x^ w^T) + bias) + residual [M][N], of
+    the type of `out`, `residual`, `dtype` or x^, bfloat16 if there is none.  `out` may be `residual`.  Without `out`, torch
+    differentiates the result with respect to x^, scale, bias and residual."""
+    if out is not None and _calls is not None and isinstance(x, QuantizedRows):
+        st = _calls.linear_q_bits(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, residual, out)
+        if st == 0 or _took("bnn_linear_q_bits", st):
+            return out
+    dtype = _result_type(x, out, residual, dtype)
+    if out is None and _recorded(x.hat, scale, bias, residual):
+        return _LinearQBits.apply(_differentiable_hat(x, dtype), scale, bias, residual, x, w_bits, act, dtype)
+    lib = load_library()
+    at, like = _q_weights(x, w_bits, dtype)
+    (M, K), N = x.shape, w_bits.shape[0]
+    if residual is not None:
+        _sized(residual, M, N, "residual", like)
+    given = out
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=like.device)
+    _sized(out, M, N, "out", like)
+    _check("bnn_linear_q_bits",
+           lib.bnn_linear_q_bits(x.kind, *at, *_at(w_bits), _vector(scale, N, "scale", like), _vector(bias, N, "bias", like), act,
+                                 _TYPES[dtype], *_at(residual), *_at(out), M, N, K, _stream(out)))
+    _count_write(given)
+    return out
+
+
+def _result_type(x, out, residual, dtype):
+    if not isinstance(x, QuantizedRows):
+        raise ValueError("x must be QuantizedRows")
+    for t in (out, residual):
+        if t is not None:
+            return t.dtype
+    return dtype if dtype is not None else x.hat.dtype if x.hat is not None else torch.bfloat16
+
+
+def gated_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                 act: int = ACT_SILU, dtype: torch.dtype | None = None, out: torch.Tensor | None = None, out_kind: int | None = None,
+                 out_q: QuantizedRows | None = None, hat: bool = False):
+    """bnn_gated_q_bits: quantised rows x^ [M][K], packed weights [2F][ceil(K/32)] (the gate's rows first) -> act(z_gate) * z_up [M][F]
+    with z = scale * (x^ w^T) + bias.  With out_kind ROWS_MX4, or rows out_q of that kind, the result is QuantizedRows for the product
+    that reads it (of ROWS_I8 a row's scale needs the whole row: quantize_rows makes them).  Types and differentiation as of
+    linear_q_bits; of a quantised result torch differentiates h^ as if it were h."""
+    if _calls is not None and (out is not None) != (out_q is not None) and out_kind is None and isinstance(x, QuantizedRows):
+        st = _calls.gated_q_bits(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out) if out_q is None else \
+            _calls.gated_q_bits_rows(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out_q.kind, out_q.K, out_q.codes,
+                                     out_q.scales, out_q.hat)
+        if st == 0 or _took("bnn_gated_q_bits", st):
+            return out if out_q is None else out_q
+    if out is not None and (out_q is not None or out_kind is not None):
+        raise ValueError("the result is either real (out) or quantised (out_kind, out_q)")
+    if out_q is not None:
+        out_kind = out_q.kind
+    if out_kind is not None and out_kind != ROWS_MX4:
+        raise ValueError("a quantised result is of ROWS_MX4: quantize_rows makes the rows of ROWS_I8")
+    dtype = _result_type(x, out if out_q is None else out_q.hat, None, dtype)
+    if out is None and out_q is None and _recorded(x.hat, scale, bias):
+        got = _GatedQBits.apply(_differentiable_hat(x, dtype), scale, bias, x, w_bits, act, dtype, out_kind)
+        return got if out_kind is None else QuantizedRows(out_kind, _halves(w_bits), *got[1:], got[0])
+    lib = load_library()
+    at, like = _q_weights(x, w_bits, dtype)
+    (M, K), F = x.shape, _halves(w_bits)
+    given = out, out_q
+    if out_kind is not None:
+        if out_q is None:
+            out_q = quantized_rows(M, F, out_kind, like.device, dtype if hat else None)
+        at_out = _rows_at(out_q, M, F, like.device, "out_q")
+        out = out_q.hat
+    else:
+        at_out = None, 0, None, 0
+        if out is None:
+            out = torch.empty((M, F), dtype=dtype, device=like.device)
+    if out is not None:
+        _sized(out, M, F, "out", like)
+    _check("bnn_gated_q_bits",
+           lib.bnn_gated_q_bits(x.kind, *at, *_at(w_bits), _vector(scale, 2 * F, "scale", like), _vector(bias, 2 * F, "bias", like), act,
+                                _TYPES[dtype], *_at(out), *at_out, M, F, K, _stream(like)))
+    _count_write(given[0])
+    _count_rows(given[1])
+    return out if out_kind is None else out_q

@@ -18,143 +18,13 @@
 // elements do not fit the registers: 324 - 596 bytes a lane go to scratch memory (4000 x 16000 bfloat16: 555 us, 1.4 TB/s), forwards
 // 28 - 316 (118 us).
 #include "join_sums.h"
+#include "row_layout.h"
 
 namespace bnn {
 
 namespace {
 
-constexpr int64_t kMaxNormRow = 16384;       // elements of the longest row that a workgroup holds in registers
 constexpr int kNormWaves = 16;               // wavefronts of a compute unit that walk over rows forwards
-
-__device__ inline float sum_of_wave(float v) {
-    v = sum_of_32(v);
-    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
-}
-
-// Sums of a and of b over the workgroup of up to WAVES wavefronts, the same in every thread.  Two buffers in turn: a thread writes
-// one again only after the barrier of the sum between, by which everyone has read it.
-template <int WAVES>
-struct Sums {
-    float2* lds;             // [2][WAVES]; zero where there is no such wavefront
-    int turn = 0;
-    __device__ inline explicit Sums(float2* p) : lds(p) {
-        if constexpr (WAVES > 1) {
-            if (threadIdx.x < 2 * WAVES) lds[threadIdx.x] = make_float2(0.0f, 0.0f);
-            __syncthreads();
-        }
-    }
-    __device__ inline float2 operator()(float a, float b) {
-        a = sum_of_wave(a);
-        b = sum_of_wave(b);
-        if constexpr (WAVES > 1) {
-            float2* const p = lds + turn * WAVES;
-            turn ^= 1;
-            if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = make_float2(a, b);
-            __syncthreads();
-            a = b = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                a += p[w].x;
-                b += p[w].y;
-            }
-        }
-        return make_float2(a, b);
-    }
-};
-
-// A row's layout over a workgroup: CH groups of G elements a thread, in a workgroup of no more wavefronts than the row needs (WAVES
-// at most).  Group i of a thread begins with column first_col(i).
-template <int W, int GROUP, int GROUPS, bool IS_SHORT>
-struct Layout {
-    static constexpr int WAVES = W, G = GROUP, CH = GROUPS;
-    static constexpr bool SHORT = IS_SHORT;      // rows of fewer than G elements
-    static constexpr bool FULL = W == 1 || (W == 16);
-    static inline int threads(int64_t D) { return FULL ? 64 * W : 64 * int(ceil_div(D, 64 * G * CH)); }
-    __device__ static inline int first_col(int i) { return (i * (FULL ? 64 * W : int(blockDim.x)) + int(threadIdx.x)) * G; }
-};
-
-template <typename L>
-using Values = float[L::CH][L::G];
-
-template <typename L, typename F>
-__device__ inline void each(F&& f) {
-#pragma unroll
-    for (int i = 0; i < L::CH; ++i)
-#pragma unroll
-        for (int e = 0; e < L::G; ++e) f(i, e);
-}
-
-// A row's part of this thread, as it lies in memory.  Loads ask no questions, so that the compiler knows how many are on their way:
-// what lies past the row's end is loaded from its last group (SHORT: an element at a time), and put right by `widened`.
-template <typename E, typename L>
-struct Row {
-    typename Group<E, L::G>::type v[L::CH];
-    __device__ inline void load(const void* matrix, int64_t m, int64_t ld, int D) {
-        const E* const row = static_cast<const E*>(matrix) + m * ld;
-#pragma unroll
-        for (int i = 0; i < L::CH; ++i) {
-            const int c = L::first_col(i);
-            if constexpr (L::SHORT) v[i] = load_group<E, L::G>(row + c, D - c);
-            else v[i] = *reinterpret_cast<const typename Group<E, L::G>::any*>(row + min(c, D - L::G));
-        }
-    }
-    // As floats, zero past the row's end.
-    __device__ inline void widened(int D, Values<L>& to) const {
-#pragma unroll
-        for (int i = 0; i < L::CH; ++i) {
-            const int c = L::first_col(i);
-            typename Group<E, L::G>::type q = v[i];
-            // The wavefront's last group lies past the row's end: some of them have to be moved.
-            if (!L::SHORT && __builtin_amdgcn_readfirstlane(c) + 64 * L::G > D) q = row_end<E, L::G>(q, D - c);
-#pragma unroll
-            for (int e = 0; e < L::G; ++e) to[i][e] = float(q[e]);
-        }
-    }
-};
-
-template <typename L>
-__device__ inline void load_vector(const float* p, int D, float otherwise, Values<L>& v) {
-    if (!p) return each<L>([&](int i, int e) { v[i][e] = otherwise; });
-    Row<float, L> row;
-    row.load(p, 0, 0, D);
-    row.widened(D, v);
-}
-
-template <typename E, typename L>
-__device__ inline void store_row(E* row, int D, const Values<L>& v) {
-#pragma unroll
-    for (int i = 0; i < L::CH; ++i) {
-        const int c = L::first_col(i);
-        if (c < D) store_group<E, L::G>(row + c, v[i], D - c);
-    }
-}
-
-template <typename L>
-__device__ inline float sum_of(const Values<L>& v) {
-    float s = 0.0f;
-    each<L>([&](int i, int e) { s += v[i][e]; });
-    return s;
-}
-
-template <typename L>
-__device__ inline float sum_of_squares(const Values<L>& v) {
-    float s = 0.0f;
-    each<L>([&](int i, int e) { s = fmaf(v[i][e], v[i][e], s); });
-    return s;
-}
-
-// Elements past the row's end are, and stay, zero.
-template <typename L>
-__device__ inline void trim(Values<L>& v, int D) {
-#pragma unroll
-    for (int i = 0; i < L::CH; ++i) {
-        const int c = L::first_col(i);
-        if (__builtin_amdgcn_readfirstlane(c) + 64 * L::G <= D) continue;      // for a whole wavefront
-#pragma unroll
-        for (int e = 0; e < L::G; ++e) v[i][e] = c + e < D ? v[i][e] : 0.0f;
-    }
-}
 
 template <typename L>
 __device__ inline void take_off(float mean, Values<L>& v, int D) {
@@ -204,11 +74,20 @@ struct NormArgs {
     int post, pre, M, D;
 };
 
+// With codes of n (bnn_rows) in the place of n: calls without them have no more arguments than they had.
+struct NormRowsArgs : NormArgs {
+    QuantOut out;
+};
+
+constexpr int kReals = -1;                   // in the place of a bnn_rows: n as it is
+
 // BETAS: a norm has one.
-template <typename E, typename L, bool BETAS>
-__global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const NormArgs a) {
+template <typename E, typename L, bool BETAS, int ROWS = kReals>
+__global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const typename std::conditional<ROWS == kReals, NormArgs, NormRowsArgs>::type a) {
     __shared__ float2 sums_s[2 * L::WAVES];
     Sums<L::WAVES> sums(sums_s);
+    __shared__ uint32_t largest_s[ROWS == BNN_ROWS_I8 ? 2 * L::WAVES : 1];
+    Largest<ROWS == BNN_ROWS_I8 ? L::WAVES : 1> largest(largest_s);
     const int D = a.D;
     Values<L> post_g, pre_g, post_b, pre_b;
     Row<E, L> y, x, gate;
@@ -251,8 +130,10 @@ __global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const Norm
             normalise<L>(a.pre, v, D, a.eps, sums);
             each<L>([&](int i, int e) { v[i][e] *= pre_g[i][e]; });
             if constexpr (BETAS) each<L>([&](int i, int e) { v[i][e] += pre_b[i][e]; });
-            store_row<E, L>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
+            if constexpr (ROWS == kReals) store_row<E, L>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
         }
+        if constexpr (ROWS == BNN_ROWS_I8) store_row_i8<E, L>(a.out, m, D, v, largest);
+        if constexpr (ROWS == BNN_ROWS_MX4) store_row_mx4<E, L>(a.out, m, D, v);
     }
 }
 
@@ -448,22 +329,11 @@ __global__ __launch_bounds__(64 * L::WAVES) __attribute__((amdgpu_waves_per_eu((
     }
 }
 
-// Calls f(layout) for rows of D elements.
-template <typename F>
-inline void with_row(int64_t D, F&& f) {
-    if (D < 8) f(Layout<1, 8, 1, true>{});
-    else if (D <= 512) f(Layout<1, 8, 1, false>{});
-    else if (D <= 1024) f(Layout<1, 8, 2, false>{});
-    else if (D <= 4096) f(Layout<4, 8, 2, false>{});
-    else if (D <= 8192) f(Layout<8, 8, 2, false>{});
-    else f(Layout<16, 8, 2, false>{});
-}
-
 bool norm_kind(int kind) { return kind == BNN_NORM_NONE || kind == BNN_NORM_RMS || kind == BNN_NORM_LAYER; }
 
 int check_norm_sizes(int64_t M, int64_t D, int64_t rows_per_gate) {
     if (M < 0 || D < 0 || rows_per_gate < 1 || M > kMaxDim || D > kMaxDim || rows_per_gate > kMaxDim) return BNN_ERR_INVALID_ARG;
-    return D > kMaxNormRow ? BNN_ERR_UNSUPPORTED : BNN_OK;
+    return D > kMaxRowHeld ? BNN_ERR_UNSUPPORTED : BNN_OK;
 }
 
 // A matrix of the call: there or not wanted, with rows of D.
@@ -471,6 +341,44 @@ struct Operand2 {
     const void* p;
     int64_t ld;
 };
+
+// What both entry points check; a.n: n, or the place of n^.
+int check_norm(int type, const NormArgs& a, int64_t M, int64_t D) {
+    const int64_t size = type_bytes(type);
+    if (size == 0 || !norm_kind(a.post) || !norm_kind(a.pre)) return BNN_ERR_INVALID_ARG;
+    const int st = check_norm_sizes(M, D, a.rows_per_gate);
+    if (st != BNN_OK) return st;
+    if ((a.post != BNN_NORM_LAYER && a.post_beta) || (a.post == BNN_NORM_NONE && a.post_gamma) || (a.pre != BNN_NORM_LAYER && a.pre_beta) ||
+        (a.pre == BNN_NORM_NONE && a.pre_gamma))
+        return BNN_ERR_INVALID_ARG;
+    for (const Operand2& o : {Operand2{a.y, a.ld_y}, Operand2{a.x, a.ld_x}, Operand2{a.gate, a.ld_gate}, Operand2{a.r, a.ld_r}, Operand2{a.n, a.ld_n}}) {
+        if (o.p && (o.ld < D || o.ld > kMaxDim)) return BNN_ERR_INVALID_ARG;
+        if (!aligned_to(o.p, size)) return BNN_ERR_ALIGNMENT;
+    }
+    for (const float* p : {a.post_gamma, a.post_beta, a.pre_gamma, a.pre_beta})
+        if (!aligned_to(p, 4)) return BNN_ERR_ALIGNMENT;
+    return BNN_OK;
+}
+
+template <int ROWS, typename A>
+int launch_norm(int type, A a, int64_t M, int64_t D, void* stream) {
+    a.M = int(M);
+    a.D = int(D);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool betas = a.post_beta || a.pre_beta;
+    with_type(type, [&](auto e) {
+        with_row(D, [&](auto layout) {
+            using L = decltype(layout);
+            // As many workgroups as are on the chip together, each walking over rows.
+            const int threads = L::threads(D);
+            const int64_t together = 256 * (64 * kNormWaves / threads);
+            const dim3 grid(uint32_t(M < together ? M : together)), block(uint32_t(threads), 1, 1);
+            if (betas) norm_residual_kernel<decltype(e), L, true, ROWS><<<grid, block, 0, s>>>(a);
+            else norm_residual_kernel<decltype(e), L, false, ROWS><<<grid, block, 0, s>>>(a);
+        });
+    });
+    return check_launch();
+}
 
 }  // namespace
 }  // namespace bnn
@@ -480,37 +388,29 @@ extern "C" int bnn_norm_residual(int type, const void* y, int64_t ld_y, const vo
                                  const float* post_beta, int pre, const float* pre_gamma, const float* pre_beta, float eps, void* r,
                                  int64_t ld_r, void* n, int64_t ld_n, int64_t M, int64_t D, void* stream) {
     using namespace bnn;
-    const int64_t size = type_bytes(type);
-    if (size == 0 || !norm_kind(post) || !norm_kind(pre)) return BNN_ERR_INVALID_ARG;
-    const int st = check_norm_sizes(M, D, rows_per_gate);
-    if (st != BNN_OK) return st;
-    if ((post != BNN_NORM_LAYER && post_beta) || (post == BNN_NORM_NONE && post_gamma) || (pre != BNN_NORM_LAYER && pre_beta) ||
-        (pre == BNN_NORM_NONE && pre_gamma))
-        return BNN_ERR_INVALID_ARG;
-    for (const Operand2& o : {Operand2{y, ld_y}, Operand2{x, ld_x}, Operand2{gate, ld_gate}, Operand2{r, ld_r}, Operand2{n, ld_n}}) {
-        if (o.p && (o.ld < D || o.ld > kMaxDim)) return BNN_ERR_INVALID_ARG;
-        if (!aligned_to(o.p, size)) return BNN_ERR_ALIGNMENT;
-    }
-    for (const float* p : {post_gamma, post_beta, pre_gamma, pre_beta})
-        if (!aligned_to(p, 4)) return BNN_ERR_ALIGNMENT;
-    if (M == 0 || D == 0) return BNN_OK;
+    const NormArgs a{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, r, n, ld_y, ld_x, ld_gate, ld_r, ld_n, rows_per_gate,
+                     res_scale, eps, post, pre, 0, 0};
+    const int st = check_norm(type, a, M, D);
+    if (st != BNN_OK || M == 0 || D == 0) return st;
     if (!y || (n != nullptr) != (pre != BNN_NORM_NONE) || (!r && !n)) return BNN_ERR_INVALID_ARG;
-    NormArgs a{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, r, n, ld_y, ld_x, ld_gate, ld_r, ld_n, rows_per_gate,
-               res_scale, eps, post, pre, int(M), int(D)};
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool betas = post_beta || pre_beta;
-    with_type(type, [&](auto e) {
-        with_row(D, [&](auto layout) {
-            using L = decltype(layout);
-            // As many workgroups as are on the chip together, each walking over rows.
-            const int threads = L::threads(D);
-            const int64_t together = 256 * (64 * kNormWaves / threads);
-            const dim3 grid(uint32_t(M < together ? M : together)), block(uint32_t(threads), 1, 1);
-            if (betas) norm_residual_kernel<decltype(e), L, true><<<grid, block, 0, s>>>(a);
-            else norm_residual_kernel<decltype(e), L, false><<<grid, block, 0, s>>>(a);
-        });
-    });
-    return check_launch();
+    return launch_norm<kReals>(type, a, M, D, stream);
+}
+
+extern "C" int bnn_norm_residual_q(int type, const void* y, int64_t ld_y, const void* x, int64_t ld_x, const void* gate,
+                                   int64_t ld_gate, int64_t rows_per_gate, float res_scale, int post, const float* post_gamma,
+                                   const float* post_beta, int pre, const float* pre_gamma, const float* pre_beta, float eps, void* r,
+                                   int64_t ld_r, int rows, uint8_t* codes, int64_t ld_c, void* scales, int64_t ld_s, void* hat,
+                                   int64_t ld_h, int64_t M, int64_t D, void* stream) {
+    using namespace bnn;
+    NormRowsArgs a{};
+    static_cast<NormArgs&>(a) = NormArgs{y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta, r, hat, ld_y, ld_x, ld_gate, ld_r, ld_h, rows_per_gate,
+                                         res_scale, eps, post, pre, 0, 0};
+    int st = check_norm(type, a, M, D);
+    if (st == BNN_OK) st = check_rows(rows, codes, ld_c, scales, ld_s, M, D);
+    if (st != BNN_OK || M == 0 || D == 0) return st;
+    if (!y) return BNN_ERR_INVALID_ARG;
+    a.out = QuantOut{codes, scales, hat, ld_c, ld_s, ld_h};
+    return rows == BNN_ROWS_I8 ? launch_norm<BNN_ROWS_I8>(type, a, M, D, stream) : launch_norm<BNN_ROWS_MX4>(type, a, M, D, stream);
 }
 
 extern "C" int64_t bnn_norm_residual_backward_workspace(int64_t M, int64_t D, int64_t rows_per_gate) {

@@ -67,6 +67,14 @@ struct EntryPoints {
                                   const void*, int64_t, int64_t, float, int, const float*, const float*, int, const float*, float,
                                   void*, int64_t, void*, int64_t, void*, int64_t, float*, float*, float*, float*, int64_t, int64_t,
                                   void*, int64_t, void*);
+    int (*quantize_rows)(int, int, const void*, int64_t, uint8_t*, int64_t, void*, int64_t, void*, int64_t, int64_t, int64_t, void*);
+    int (*norm_residual_q)(int, const void*, int64_t, const void*, int64_t, const void*, int64_t, int64_t, float, int, const float*,
+                           const float*, int, const float*, const float*, float, void*, int64_t, int, uint8_t*, int64_t, void*, int64_t,
+                           void*, int64_t, int64_t, int64_t, void*);
+    int (*linear_q_bits)(int, const uint8_t*, int64_t, const void*, int64_t, Words, int64_t, const float*, const float*, int, int,
+                         const void*, int64_t, void*, int64_t, int64_t, int64_t, int64_t, void*);
+    int (*gated_q_bits)(int, const uint8_t*, int64_t, const void*, int64_t, Words, int64_t, const float*, const float*, int, int, void*,
+                        int64_t, uint8_t*, int64_t, uint8_t*, int64_t, int64_t, int64_t, int64_t, void*);
 };
 
 EntryPoints entry{};
@@ -514,6 +522,143 @@ PyObject* norm_residual(PyObject* const* a) {
     });
 }
 
+// Quantised rows: (kind, K, codes, scales).
+struct Rows {
+    int kind = 0;
+    int64_t K = 0, ld_s = 0;
+    Matrix codes, scales_mx;
+    void* scales = nullptr;
+    const at::Tensor* scales_t = nullptr;
+    bool read(PyObject* const* a) {
+        if (!small_integer(a[0], kind) || kind < 0 || kind > 1 || !integer(a[1], K) || K < 0 || K > INT64_MAX / 2 ||
+            !codes.read(a[2], at::kByte) || codes.cols < words(K) * (kind == 0 ? 32 : 16))
+            return false;
+        if (kind == 0) {
+            scales_t = plain(a[3], at::kFloat);
+            if (!scales_t || scales_t->dim() != 1 || scales_t->size(0) != codes.rows || !scales_t->is_contiguous()) return false;
+            scales = scales_t->data_ptr();
+        } else {
+            if (!scales_mx.read(a[3], at::kByte) || scales_mx.rows != codes.rows || scales_mx.cols < (words(K) + 3) / 4 * 4) return false;
+            scales_t = scales_mx.t;
+            scales = scales_mx.data;
+            ld_s = scales_mx.ld;
+        }
+        return scales_t->get_device() == codes.t->get_device();
+    }
+    bool of(const at::Tensor& t, int64_t m, int64_t k) const { return codes.rows == m && K == k && codes.t->get_device() == t.get_device(); }
+    void count_written() const {
+        count_write(codes);
+        if (!scales_t->is_inference()) scales_t->unsafeGetTensorImpl()->bump_version();
+    }
+};
+
+// (x, kind, K, codes, scales, hat)
+PyObject* quantize_rows(PyObject* const* a) {
+    Matrix x, hat;
+    Rows q;
+    if (!read_real(a[0], x, nullptr, 0, 0) || !q.read(a + 1) || !q.of(*x.t, x.rows, x.cols) ||
+        (a[5] != Py_None && !read_real(a[5], hat, x.t, x.rows, x.cols)))
+        return long_way();
+    q.count_written();
+    count_write(hat);
+    return launch(*x.t, [&](void* s) {
+        return entry.quantize_rows(q.kind, real_type(x.t->scalar_type()), x.data, x.ld, q.codes.as<uint8_t>(), q.codes.ld, q.scales,
+                                   q.ld_s, hat.data, hat.ld, x.rows, x.cols, s);
+    });
+}
+
+// (y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, out, kind, K, codes, scales, hat)
+PyObject* norm_residual_q(PyObject* const* a) {
+    Matrix y, x, gate, out, hat;
+    Rows q;
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+    float res_scale, eps;
+    int post, pre;
+    int64_t rows_per_gate;
+    if (!read_real(a[0], y, nullptr, 0, 0) || !real_number(a[3], res_scale) || !small_integer(a[4], post) ||
+        !small_integer(a[7], pre) || !real_number(a[10], eps) || !integer(a[11], rows_per_gate) || rows_per_gate < 1)
+        return long_way();
+    const int64_t M = y.rows, D = y.cols;
+    if ((a[1] != Py_None && !read_real(a[1], x, y.t, M, D)) ||
+        (a[2] != Py_None && !read_real(a[2], gate, y.t, M / rows_per_gate + (M % rows_per_gate != 0), D)) ||
+        !read_vector(a[5], D, *y.t, post_gamma) || !read_vector(a[6], D, *y.t, post_beta) || !read_vector(a[8], D, *y.t, pre_gamma) ||
+        !read_vector(a[9], D, *y.t, pre_beta) || !read_real(a[12], out, y.t, M, D) || !q.read(a + 13) || !q.of(*y.t, M, D) ||
+        (a[17] != Py_None && !read_real(a[17], hat, y.t, M, D)))
+        return long_way();
+    count_write(out);
+    q.count_written();
+    count_write(hat);
+    return launch(*out.t, [&](void* s) {
+        return entry.norm_residual_q(real_type(y.t->scalar_type()), y.data, y.ld, x.data, x.ld, gate.data, gate.ld, rows_per_gate,
+                                     res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, out.data, out.ld, q.kind,
+                                     q.codes.as<uint8_t>(), q.codes.ld, q.scales, q.ld_s, hat.data, hat.ld, M, D, s);
+    });
+}
+
+// Quantised rows, packed weights, their scale and bias.
+struct QWeighted {
+    Rows x;
+    Matrix w;
+    const float *scale = nullptr, *bias = nullptr;
+    bool read(PyObject* const* a) {
+        return x.read(a) && w.read(a[4], at::kInt) && w.t->get_device() == x.codes.t->get_device() && w.cols >= words(x.K) &&
+               read_vector(a[5], w.rows, *w.t, scale) && read_vector(a[6], w.rows, *w.t, bias);
+    }
+    // A result of `cols` columns.
+    bool read_out(PyObject* o, Matrix& out, int64_t cols) const {
+        return read_real(o, out, nullptr, 0, 0) && out.t->get_device() == w.t->get_device() && out.rows == x.codes.rows && out.cols == cols;
+    }
+};
+
+// (kind, K, codes, scales, w_bits, scale, bias, act, residual, out)
+PyObject* linear_q_bits(PyObject* const* a) {
+    QWeighted p;
+    Matrix residual, out;
+    int act;
+    if (!p.read(a) || !small_integer(a[7], act) || !p.read_out(a[9], out, p.w.rows) ||
+        (a[8] != Py_None && !read_real(a[8], residual, out.t, out.rows, out.cols)))
+        return long_way();
+    count_write(out);
+    return launch(*out.t, [&](void* s) {
+        return entry.linear_q_bits(p.x.kind, p.x.codes.as<uint8_t>(), p.x.codes.ld, p.x.scales, p.x.ld_s, p.w.as<uint32_t>(), p.w.ld,
+                                   p.scale, p.bias, act, real_type(out.t->scalar_type()), residual.data, residual.ld, out.data, out.ld,
+                                   out.rows, out.cols, p.x.K, s);
+    });
+}
+
+// (kind, K, codes, scales, w_bits, scale, bias, act, out)
+PyObject* gated_q_bits(PyObject* const* a) {
+    QWeighted p;
+    Matrix out;
+    int act;
+    if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[7], act) || !p.read_out(a[8], out, p.w.rows / 2)) return long_way();
+    count_write(out);
+    return launch(*out.t, [&](void* s) {
+        return entry.gated_q_bits(p.x.kind, p.x.codes.as<uint8_t>(), p.x.codes.ld, p.x.scales, p.x.ld_s, p.w.as<uint32_t>(), p.w.ld,
+                                  p.scale, p.bias, act, real_type(out.t->scalar_type()), out.data, out.ld, nullptr, 0, nullptr, 0,
+                                  out.rows, out.cols, p.x.K, s);
+    });
+}
+
+// (kind, K, codes, scales, w_bits, scale, bias, act, kind, F, codes, scales and hat of the result)
+PyObject* gated_q_bits_rows(PyObject* const* a) {
+    QWeighted p;
+    Rows q;
+    Matrix hat;
+    int act;
+    if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[7], act) || !q.read(a + 8) || q.kind != 1 ||
+        !q.of(*p.w.t, p.x.codes.rows, p.w.rows / 2) || (a[12] != Py_None && !p.read_out(a[12], hat, p.w.rows / 2)))
+        return long_way();
+    q.count_written();
+    count_write(hat);
+    return launch(*p.w.t, [&](void* s) {
+        return entry.gated_q_bits(p.x.kind, p.x.codes.as<uint8_t>(), p.x.codes.ld, p.x.scales, p.x.ld_s, p.w.as<uint32_t>(), p.w.ld,
+                                  p.scale, p.bias, act, hat.t ? real_type(hat.t->scalar_type()) : 0, hat.data, hat.ld,
+                                  q.codes.as<uint8_t>(), q.codes.ld, static_cast<uint8_t*>(q.scales), q.ld_s, q.codes.rows, q.K,
+                                  p.x.K, s);
+    });
+}
+
 // Backward passes: what they return is allocated here, and comes as (status, tensors or None ...).
 
 bool truth(PyObject* o, bool& v) {
@@ -687,6 +832,10 @@ PyObject* bind(PyObject*, PyObject* args) {
     set(e.gated_bits_backward, "bnn_gated_bits_backward");
     set(e.norm_residual_backward_workspace, "bnn_norm_residual_backward_workspace");
     set(e.norm_residual_backward, "bnn_norm_residual_backward");
+    set(e.quantize_rows, "bnn_quantize_rows");
+    set(e.norm_residual_q, "bnn_norm_residual_q");
+    set(e.linear_q_bits, "bnn_linear_q_bits");
+    set(e.gated_q_bits, "bnn_gated_q_bits");
     if (!ok || !PyCallable_Check(stream)) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point or the stream function is missing");
         return nullptr;
@@ -725,6 +874,11 @@ PyMethodDef methods[] = {
     fast<linear_bits_backward, 9>("linear_bits_backward"),
     fast<gated_bits_backward, 9>("gated_bits_backward"),
     fast<norm_residual_backward, 16>("norm_residual_backward"),
+    fast<quantize_rows, 6>("quantize_rows"),
+    fast<norm_residual_q, 18>("norm_residual_q"),
+    fast<linear_q_bits, 10>("linear_q_bits"),
+    fast<gated_q_bits, 9>("gated_q_bits"),
+    fast<gated_q_bits_rows, 13>("gated_q_bits_rows"),
     {nullptr, nullptr, 0, nullptr},
 };
 

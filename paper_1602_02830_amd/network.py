@@ -260,8 +260,10 @@ class BinaryConvNet:
         return self.scores
 
 
-def _writes(t: torch.Tensor):
-    """torch's count of the writes to a tensor (inference tensors have none)."""
+def _writes(t):
+    """torch's count of the writes to a tensor (inference tensors have none), or to those of quantised rows."""
+    if isinstance(t, B.QuantizedRows):
+        return _writes(t.codes), _writes(t.scales)
     return None if t.is_inference() else t._version
 
 
@@ -280,12 +282,19 @@ class BinaryFeedForward:
     next_gamma; that of first_norm() is differentiated by first_norm_backward().  torch's own differentiation does not see the block: of
     the real weights it would know the scales alone.
 
+    With rows = ROWS_I8 or ROWS_MX4 the products read quantised activations: first_norm() and forward() give n and n' as
+    QuantizedRows, and take n so; the quantisation of h is the gated product's own where that can be (MX4).  backward() gives the
+    gradients at the values that the codes stand for, straight through the quantisation; it keeps codes, not the values.
+
     w_in: float32 device weights [2F][D], the gate's rows first; w_out: [D][F]; gammas: float32 [D] or None (1);
     gate: [1][D] in the stream's type, shared by all rows, or None.
     """
 
     def __init__(self, w_in, w_out, act: int = B.ACT_SILU, pre_gamma=None, post_gamma=None, next_gamma=None, gate=None,
-                 res_scale: float = 1.0, eps: float = 1e-5):
+                 res_scale: float = 1.0, eps: float = 1e-5, rows: int | None = None):
+        if rows not in (None, B.ROWS_I8, B.ROWS_MX4):
+            raise ValueError("rows must be None, ROWS_I8 or ROWS_MX4")
+        self.rows = rows
         self.D, self.F, self.act = int(w_out.shape[0]), int(w_out.shape[1]), act
         if tuple(w_in.shape) != (2 * self.F, self.D):
             raise ValueError("w_in must be [2F][D] where w_out is [D][F]")
@@ -301,8 +310,11 @@ class BinaryFeedForward:
         self.w_in, self.w_out = B.pack_sign(w_in), B.pack_sign(w_out)
         self.scale_in, self.scale_out = w_in.abs().mean(1), w_out.abs().mean(1)
 
-    def first_norm(self, x: torch.Tensor) -> torch.Tensor:
+    def first_norm(self, x: torch.Tensor):
         """pre(x): what the first block of a stack reads beside the stream."""
+        if self.rows is not None:
+            n = B.quantized_rows(x.shape[0], x.shape[1], self.rows, x.device)
+            return B.norm_residual_q(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, out_q=n, need_r=False)[1]
         n = x.new_empty(x.shape)
         return B.norm_residual(x, pre=B.NORM_RMS, pre_gamma=self.pre_gamma, eps=self.eps, out_n=n, need_r=False)[1]
 
@@ -317,8 +329,10 @@ class BinaryFeedForward:
         """The gate's row for the rows of y: none for none."""
         return self.gate if y.shape[0] else None
 
-    def forward(self, x: torch.Tensor, n: torch.Tensor, keep: bool = False):
+    def forward(self, x: torch.Tensor, n, keep: bool = False):
         """Stream x and its norm n, [M][D] -> (r, n').  keep: what backward() reads is kept."""
+        if self.rows is not None:
+            return self._forward_q(x, n, keep)
         M = x.shape[0]
         h, y, r, after = (x.new_empty((M, cols)) for cols in (self.F, self.D, self.D, self.D))       # calls with `out` are not recorded
         B.gated_bits(n, self.w_in, self.scale_in, None, self.act, out=h)
@@ -326,6 +340,22 @@ class BinaryFeedForward:
         B.norm_residual(y, x, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma, None,
                         self.eps, max(M, 1), out=r, out_n=after)
         # n and r are the caller's, who may write over them before backward() (r in place is the next sum's documented place).
+        self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
+        return r, after
+
+    def _forward_q(self, x, n, keep):
+        if not isinstance(n, B.QuantizedRows) or n.kind != self.rows:
+            raise ValueError("n must be QuantizedRows of the block's kind, as first_norm() and forward() give them")
+        M = x.shape[0]
+        y, r = x.new_empty((M, self.D)), x.new_empty((M, self.D))
+        h, after = (B.quantized_rows(M, cols, self.rows, x.device) for cols in (self.F, self.D))
+        if self.rows == B.ROWS_MX4:
+            B.gated_q_bits(n, self.w_in, self.scale_in, None, self.act, out_q=h)
+        else:
+            B.quantize_rows(B.gated_q_bits(n, self.w_in, self.scale_in, None, self.act, out=x.new_empty((M, self.F))), out=h)
+        B.linear_q_bits(h, self.w_out, self.scale_out, out=y)
+        B.norm_residual_q(y, x, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS, self.next_gamma, None,
+                          self.eps, max(M, 1), out=r, out_q=after)
         self._kept = (n, h, y, r, _writes(n), _writes(r)) if keep else None
         return r, after
 
@@ -338,6 +368,8 @@ class BinaryFeedForward:
             raise RuntimeError("backward() needs the input n and the result r of forward(keep=True) as they were: one was written over")
         got = B.norm_residual_backward(dr, dn_after, y, r, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
                                        self.next_gamma, None, self.eps, max(y.shape[0], 1))
+        if self.rows is not None:              # the values that the codes stand for
+            n, h = B.dequantize_rows(n, y.dtype), B.dequantize_rows(h, y.dtype)
         dgate = torch.zeros_like(self.gate) if self.gate is not None and y.shape[0] == 0 else got["dgate"]
         out = B.linear_bits_backward(got["dy"], h, self.w_out, self.scale_out)
         gated = B.gated_bits_backward(out["dx"], n, self.w_in, self.scale_in, None, self.act)
