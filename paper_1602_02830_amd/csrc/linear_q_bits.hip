@@ -1,5 +1,5 @@
 // Products of quantised rows with packed weights and their epilogues in one launch: bnn_linear_q_bits and bnn_gated_q_bits.
-#include "q_bits.h"
+#include "q_tiles.h"
 
 namespace bnn {
 
@@ -7,6 +7,7 @@ namespace {
 
 template <int ROWS, int EPI>
 int forward(const QProductArgs& a, hipStream_t s) {
+    if (a.M > 64 && a.K > 0) return launch_q_tile<ROWS, EPI, 2, 4, 4, 2>(a, s);
     // Codes of the result are made of 32 columns at a time.
     if (a.out.codes) return launch_q_small<ROWS, EPI, 2>(a, s);
     return launch_q_small<ROWS, EPI, 1>(a, s);
