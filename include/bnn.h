@@ -463,7 +463,8 @@ int bnn_norm_residual_backward(int type, const void *dr, int64_t ld_dr, const vo
  *   codes   [M][ld_c] bytes, 16-byte aligned, ld_c a multiple of 16 and at least 32 (I8) or 16 (MX4) times ceil(K / 32): whole
  *           blocks of 32 elements, those past K zero.  Byte 4 i + j of an I8 block is element 8 j + i, nibble 8 i + j of an MX4 block
  *           (the lower half of a byte first) is element 4 j + i.
- *   scales  I8: float [M].  MX4: bytes [M][ld_s], ld_s a multiple of 4 and at least ceil(K / 32).  4-byte aligned.
+ *   scales  I8: float [M].  MX4: bytes [M][ld_s], 16-byte aligned, ld_s a multiple of 16 and at least ceil(K / 32); what the bytes past
+ *           ceil(K / 32) hold means nothing.
  * Leading dimensions of reals as above.
  */
 typedef enum bnn_rows { BNN_ROWS_I8 = 0, BNN_ROWS_MX4 = 1 } bnn_rows;

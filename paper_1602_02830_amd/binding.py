@@ -978,7 +978,7 @@ def quantized_rows(M: int, K: int, kind: int = ROWS_I8, device="cuda", hat: torc
         raise ValueError("sizes must not be negative")
     codes = torch.empty((M, _blocks(K) * (32 if kind == ROWS_I8 else 16)), dtype=torch.uint8, device=device)
     scales = torch.empty(M, dtype=torch.float32, device=device) if kind == ROWS_I8 else \
-        torch.empty((M, (_blocks(K) + 3) // 4 * 4), dtype=torch.uint8, device=device)
+        torch.empty((M, (_blocks(K) + 15) // 16 * 16), dtype=torch.uint8, device=device)
     return QuantizedRows(kind, K, codes, scales, None if hat is None else torch.empty((M, K), dtype=hat, device=device))
 
 
@@ -999,8 +999,8 @@ def _rows_at(q: QuantizedRows, M: int, K: int, device, name: str):
             raise ValueError(f"{name}: scales must be a contiguous float32 vector of {M} elements")
         return c.data_ptr(), _ld(c), s.data_ptr(), 0
     _dev(s, torch.uint8, f"{name}: scales")
-    if s.shape[0] != M or s.shape[1] < (_blocks(K) + 3) // 4 * 4:
-        raise ValueError(f"{name}: scales must be {M} rows of a byte for each 32 elements, whole groups of four")
+    if s.shape[0] != M or s.shape[1] < (_blocks(K) + 15) // 16 * 16:
+        raise ValueError(f"{name}: scales must be {M} rows of a byte for each 32 elements, whole groups of 16")
     return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
 
 

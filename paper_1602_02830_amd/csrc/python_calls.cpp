@@ -538,7 +538,7 @@ struct Rows {
             if (!scales_t || scales_t->dim() != 1 || scales_t->size(0) != codes.rows || !scales_t->is_contiguous()) return false;
             scales = scales_t->data_ptr();
         } else {
-            if (!scales_mx.read(a[3], at::kByte) || scales_mx.rows != codes.rows || scales_mx.cols < (words(K) + 3) / 4 * 4) return false;
+            if (!scales_mx.read(a[3], at::kByte) || scales_mx.rows != codes.rows || scales_mx.cols < (words(K) + 15) / 16 * 16) return false;
             scales_t = scales_mx.t;
             scales = scales_mx.data;
             ld_s = scales_mx.ld;

@@ -92,9 +92,8 @@ __device__ inline v4f_t mfma_mx4(v4i_t w, v4i_t x, v4f_t c, uint32_t scales) {
 
 // The epilogue of W = 8 or 4 consecutive columns from n on of row m, from their sums (gated: of both halves): what is stored, in
 // float32.
-template <int EPI, int W>
-__device__ inline void results(const QProductArgs& a, const float (&s)[kQHalves<EPI>][W], const float* const (&scale)[kQHalves<EPI>],
-                               const float* const (&bias)[kQHalves<EPI>], float (&v)[W]) {
+template <int EPI, int W, typename V>
+__device__ inline void results(const QProductArgs& a, const float (&s)[kQHalves<EPI>][W], const V& scale, const V& bias, float (&v)[W]) {
     float z[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) z[i] = fmaf(s[0][i], scale[0][i], bias[0][i]);
@@ -106,8 +105,10 @@ __device__ inline void results(const QProductArgs& a, const float (&s)[kQHalves<
     }
 }
 
-// `valid` of the columns exist.
-template <typename E, int EPI, int W>
+// `valid` of the columns exist.  PAST: stores go past the cache, which a large result does not fit (as are those of q_tiles.h:
+// 4096 x 4096 -> 4096 of 8 bits 62 us against 65, 1000 x 784 -> 4096 in float32 12.0 against 13.7; BinaryFeedForward.forward, which reads them
+// next, takes as long either way).
+template <typename E, int EPI, int W, bool PAST>
 __device__ inline void store_results(const QProductArgs& a, int m, int n, float (&v)[W], int64_t valid) {
     if constexpr (EPI == kQLinear) {
         if (a.residual) {
@@ -117,20 +118,27 @@ __device__ inline void store_results(const QProductArgs& a, int m, int n, float 
             for (int i = 0; i < W; ++i) v[i] += r[i];
         }
     }
-    store_group<E, W>(static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n, v, valid);
+    E* const y = static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n;
+    if (PAST && valid >= W) {
+        typename Group<E, W>::type o;
+#pragma unroll
+        for (int i = 0; i < W; ++i) o[i] = E(v[i]);
+        __builtin_nontemporal_store(o, reinterpret_cast<typename Group<E, W>::any*>(y));
+    } else {
+        store_group<E, W>(y, v, valid);
+    }
 }
 
 // All lanes of a quad that has a block of 32 columns come here together (W = 8).
-template <int EPI, int W>
-__device__ inline void finish_q(const QProductArgs& a, int m, int n, const float (&s)[kQHalves<EPI>][W], const float* const (&scale)[kQHalves<EPI>],
-                                const float* const (&bias)[kQHalves<EPI>]) {
+template <int EPI, int W, bool PAST = false, typename V>
+__device__ inline void finish_q(const QProductArgs& a, int m, int n, const float (&s)[kQHalves<EPI>][W], const V& scale, const V& bias) {
     if (m >= a.M) return;
     const int64_t valid = int64_t(a.N) - n;
     float v[W];
     if constexpr (EPI == kQGated && W == 8) {
         if (a.out.codes) {
             if ((n & ~31) >= a.N) return;
-            results<EPI, W>(a, s, scale, bias, v);
+            results<EPI, W, V>(a, s, scale, bias, v);
 #pragma unroll
             for (int i = 0; i < W; ++i) v[i] = i < valid ? v[i] : 0.0f;
             switch (a.type) {
@@ -141,11 +149,11 @@ __device__ inline void finish_q(const QProductArgs& a, int m, int n, const float
         }
     }
     if (valid <= 0) return;
-    results<EPI, W>(a, s, scale, bias, v);
+    results<EPI, W, V>(a, s, scale, bias, v);
     switch (a.type) {
-        case BNN_BF16: return store_results<bf16_t, EPI, W>(a, m, n, v, valid);
-        case BNN_F16: return store_results<f16_t, EPI, W>(a, m, n, v, valid);
-        default: return store_results<float, EPI, W>(a, m, n, v, valid);
+        case BNN_BF16: return store_results<bf16_t, EPI, W, PAST>(a, m, n, v, valid);
+        case BNN_F16: return store_results<f16_t, EPI, W, PAST>(a, m, n, v, valid);
+        default: return store_results<float, EPI, W, PAST>(a, m, n, v, valid);
     }
 }
 
@@ -261,13 +269,34 @@ __global__ __launch_bounds__(512) void q_small_kernel(const QProductArgs a) {
 }
 
 template <int ROWS, int EPI, int FN>
-int launch_q_small(const QProductArgs& a, hipStream_t s) {
-    const int64_t blocks = ceil_div(a.N, 16 * FN), tiles_m = ceil_div(a.M, kQRows), runs = ceil_div(a.K, kQRunK);
+int launch_q_small(QProductArgs a, hipStream_t s) {
+    const int64_t blocks = ceil_div(a.N, 16 * FN), runs = ceil_div(a.K, kQRunK);
     const int waves = int(runs >= 8 ? 8 : runs < 1 ? 1 : runs);
-    if (blocks * tiles_m > max_blocks(64 * waves) || tiles_m > 65535) return BNN_ERR_UNSUPPORTED;
     const size_t lds = size_t(waves) * FN * kQHalves<EPI> * 1024;
-    q_small_kernel<ROWS, EPI, FN><<<dim3(uint32_t(blocks), uint32_t(tiles_m)), dim3(64 * waves), lds, s>>>(a);
-    return check_launch();
+    // As many rows at a time as a grid has places for.
+    const int64_t most = max_blocks(64 * waves) / blocks < 65535 ? max_blocks(64 * waves) / blocks : 65535, M = a.M;
+    const int64_t size = type_bytes(a.type);
+    if (most < 1) return BNN_ERR_UNSUPPORTED;
+    for (int64_t first = 0; first < M; first += most * kQRows) {
+        QProductArgs part = a;
+        part.M = int(M - first < most * kQRows ? M - first : most * kQRows);
+        if (first > 0) {
+            auto move = [&](auto& p, int64_t bytes) {
+                if (p) p = reinterpret_cast<std::decay_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + uintptr_t(first * bytes));
+            };
+            move(part.codes, a.ld_c);
+            move(part.scales, ROWS == BNN_ROWS_I8 ? 4 : a.ld_s);
+            move(part.residual, a.ld_r * size);
+            move(part.y, a.ld_y * size);
+            move(part.out.codes, a.out.ld_c);
+            move(part.out.scales, a.out.ld_s);
+            move(part.out.hat, a.out.ld_h * size);
+        }
+        q_small_kernel<ROWS, EPI, FN><<<dim3(uint32_t(blocks), uint32_t(ceil_div(part.M, kQRows))), dim3(64 * waves), lds, s>>>(part);
+        const int st = check_launch();
+        if (st != BNN_OK) return st;
+    }
+    return BNN_OK;
 }
 
 }  // namespace bnn

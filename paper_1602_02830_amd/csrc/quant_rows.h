@@ -208,11 +208,11 @@ inline int check_rows(int rows, const uint8_t* codes, int64_t ld_c, const void* 
     if (!rows_kind(rows)) return BNN_ERR_INVALID_ARG;
     const bool mx4 = rows == BNN_ROWS_MX4;
     if (M > 0 && ((K > 0 && !codes) || ((K > 0 || !mx4) && !scales))) return BNN_ERR_INVALID_ARG;
-    if (!aligned_to(codes, 16) || !aligned_to(scales, 4)) return BNN_ERR_ALIGNMENT;
+    if (!aligned_to(codes, 16) || !aligned_to(scales, mx4 ? 16 : 4)) return BNN_ERR_ALIGNMENT;
     if (K == 0) return BNN_OK;
     const int64_t blocks = (K + 31) / 32;
     if (ld_c < blocks * block_bytes(rows) || ld_c > kMaxDim || (mx4 && (ld_s < blocks || ld_s > kMaxDim))) return BNN_ERR_INVALID_ARG;
-    if (ld_c % 16 != 0 || (mx4 && ld_s % 4 != 0)) return BNN_ERR_ALIGNMENT;
+    if (ld_c % 16 != 0 || (mx4 && ld_s % 16 != 0)) return BNN_ERR_ALIGNMENT;
     return BNN_OK;
 }
 

@@ -200,8 +200,8 @@ def test_quantise_places(kind):
         scales = torch.full((M + 2,), 123.0, device=DEV)
         inner = scales[1:-1]
     else:
-        scales = torch.full((M + 2, 20), 0xA5, dtype=torch.uint8, device=DEV)
-        inner = scales[1:-1, :12]
+        scales = torch.full((M + 2, 32), 0xA5, dtype=torch.uint8, device=DEV)
+        inner = scales[1:-1, :16]
     real = torch.full((M + 2, K + 9), 7.0, dtype=torch.float16, device=DEV)
     real[1:-1, 1:K + 1] = x.to(DEV)
     place = real[1:-1, 1:K + 1]
@@ -306,7 +306,7 @@ class QProduct:
             self.q.codes = codes[:, :self.q.codes.shape[1]]
             if self.kind == bnn.ROWS_MX4:
                 wide = self.q.scales.shape[1]
-                scales = torch.full((M, wide + 4 * gap), 0xFF, dtype=torch.uint8, device=DEV)
+                scales = torch.full((M, wide + 16 * gap), 0xFF, dtype=torch.uint8, device=DEV)
                 scales[:, :(K + 31) // 32] = self.q.scales[:, :(K + 31) // 32]         # the bytes past K's blocks: NaN, not to be read as scales
                 self.q.scales = scales[:, :wide]
         self.x = hat_of(self.q)
@@ -352,7 +352,7 @@ def result(p, act, gated=False, residual=None):
 
 
 PRODUCTS = [(1, 1, 1), (1, 64, 32), (3, 17, 40), (16, 48, 512), (2, 33, 513), (5, 100, 1030), (17, 96, 4096), (8, 40, 8200), (33, 130, 700), (70, 257, 333), (130, 520, 1024),
-            (300, 300, 96)]
+            (300, 300, 96), (257, 300, 128), (100, 260, 256), (70, 70, 384), (65, 96, 512), (300, 136, 640), (90, 520, 1152), (513, 200, 896), (66, 64, 4224), (130, 70, 97), (80, 130, 130), (68, 40, 2050), (129, 300, 3333), (66, 33, 545)]
 
 
 @gpu
@@ -422,6 +422,24 @@ def test_products_of_nan_rows(kind):
     assert bad[[3, 19]].all() and int(torch.isnan(y).any(1).sum()) == 2
     h = bnn.gated_q_bits(q, w, out_kind=bnn.ROWS_MX4, hat=True)
     assert torch.isnan(h.hat).any(1).nonzero().flatten().tolist() == [3, 19]
+
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_more_rows_than_a_grid_has_places(kind):
+    """Small tiles of more than 65535 times 16 rows: of no elements, and of one block, where the sums are exact."""
+    M = 65535 * 16 + 37
+    q = bnn.quantize_rows(torch.empty(M, 0, device=DEV), KINDS[kind])
+    bias = torch.randn(20, device=DEV)
+    y = bnn.linear_q_bits(q, torch.empty(20, 0, dtype=torch.int32, device=DEV), None, bias, dtype=torch.float32)
+    assert torch.equal(y, bias.expand(M, 20))
+    x = torch.randint(-7, 8, (M, 32), device=DEV).float()
+    x[:, 0] = 127 if kind == "i8" else 6                   # steps of 1; halves are not asked for
+    w = bnn.pack_sign(torch.randn(9, 32, device=DEV))
+    q = bnn.quantize_rows(x, KINDS[kind], hat=True)
+    assert torch.equal(bnn.linear_q_bits(q, w, dtype=torch.float32), bnn.linear_bits(q.hat, w))
+    h = bnn.gated_q_bits(q, w[:8], dtype=torch.float32)
+    assert torch.equal(h[-100:], bnn.gated_q_bits(bnn.quantize_rows(x[-100:], KINDS[kind]), w[:8], dtype=torch.float32))
 
 
 @gpu
@@ -521,13 +539,13 @@ def test_refusals(monkeypatch):
     lib = bnn.load_library()
     at = 1 << 20                      # never read
 
-    def quantise(rows=0, type=0, x=at, ld_x=64, codes=at, ld_c=64, scales=at, ld_s=4, hat=0, ld_h=64, M=2, K=64):
+    def quantise(rows=0, type=0, x=at, ld_x=64, codes=at, ld_c=64, scales=at, ld_s=16, hat=0, ld_h=64, M=2, K=64):
         return lib.bnn_quantize_rows(rows, type, x, ld_x, codes, ld_c, scales, ld_s, hat, ld_h, M, K, 0)
 
     for bad in (dict(rows=2), dict(rows=-1), dict(type=3), dict(M=-1), dict(K=-1), dict(ld_x=63), dict(ld_c=48), dict(rows=1, ld_c=16), dict(rows=1, ld_s=0, K=33),
                 dict(x=0), dict(codes=0), dict(scales=0), dict(hat=at, ld_h=63), dict(K=1 << 31)):
         assert quantise(**bad) == 1, bad
-    for bad in (dict(x=at + 1), dict(codes=at + 8), dict(ld_c=72), dict(scales=at + 2), dict(rows=1, ld_s=6), dict(hat=at + 1), dict(type=2, hat=at + 2)):
+    for bad in (dict(x=at + 1), dict(codes=at + 8), dict(ld_c=72), dict(scales=at + 2), dict(rows=1, ld_s=24), dict(rows=1, scales=at + 8, ld_s=16), dict(hat=at + 1), dict(type=2, hat=at + 2)):
         assert quantise(**bad) == 2, bad
     assert quantise(M=0) == 0
 
@@ -558,8 +576,8 @@ def test_refusals(monkeypatch):
     assert linear(K=big + 1, ld_c=2 * big, ld_w=big) == 3
     assert linear(M=0) == 0 and linear(N=0) == 0
 
-    def gated(rows=1, h=at, ld_h=8, oc=0, ld_oc=16, os=0, ld_os=4, F=8, M=2, K=64):
-        return lib.bnn_gated_q_bits(rows, at, 64, at, 4, at, 2, None, None, 2, 0, h, ld_h, oc, ld_oc, os, ld_os, M, F, K, 0)
+    def gated(rows=1, h=at, ld_h=8, oc=0, ld_oc=16, os=0, ld_os=16, F=8, M=2, K=64):
+        return lib.bnn_gated_q_bits(rows, at, 64, at, 16, at, 2, None, None, 2, 0, h, ld_h, oc, ld_oc, os, ld_os, M, F, K, 0)
 
     for bad in (dict(h=0), dict(ld_h=7), dict(oc=at), dict(os=at), dict(oc=at, os=at, ld_oc=0), dict(oc=at, os=at, ld_os=0), dict(F=-1), dict(F=1 << 30)):
         assert gated(**bad) == 1, bad
