@@ -1048,6 +1048,12 @@ def quantize_rows(x: torch.Tensor, kind: int = ROWS_I8, hat: bool = False, out: 
 
 def dequantize_rows(q: QuantizedRows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """bnn_dequantize_rows: x^ [M][K]."""
+    if not isinstance(q, QuantizedRows):
+        raise ValueError("q must be QuantizedRows")
+    if out is not None and _calls is not None:
+        st = _calls.dequantize_rows(q.kind, q.K, q.codes, q.scales, out)
+        if st == 0 or _took("bnn_dequantize_rows", st):
+            return out
     lib = load_library()
     M, K = q.shape
     at = _rows_at(q, M, K, q.codes.device, "q")

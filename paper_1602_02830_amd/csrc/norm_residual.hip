@@ -81,6 +81,12 @@ struct NormRowsArgs : NormArgs {
 
 constexpr int kReals = -1;                   // in the place of a bnn_rows: n as it is
 
+// Wavefronts of a compute unit that walk over rows and give codes: as many as are there together, so that no workgroup begins
+// when others end (16384 x 4096 bfloat16, root-mean-square norms, with 16: 138 us with codes of 8 bits and n^, 121 with those of 4; with
+// 12 125 and 116, 4.8 TB/s, and 100 and 88 without n^).  A third sum over the workgroup for the scale is what 8 bits cost more; in registers for
+// 16 wavefronts (128 of them) the kernels spill 60 bytes and take 143 and 137 us.
+constexpr int kNormRowsWaves = 12;
+
 // BETAS: a norm has one.
 template <typename E, typename L, bool BETAS, int ROWS = kReals>
 __global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const typename std::conditional<ROWS == kReals, NormArgs, NormRowsArgs>::type a) {
@@ -371,7 +377,8 @@ int launch_norm(int type, A a, int64_t M, int64_t D, void* stream) {
             using L = decltype(layout);
             // As many workgroups as are on the chip together, each walking over rows.
             const int threads = L::threads(D);
-            const int64_t together = 256 * (64 * kNormWaves / threads);
+            constexpr int WAVES = ROWS == kReals ? kNormWaves : kNormRowsWaves;
+            const int64_t together = 256 * (64 * WAVES / threads > 0 ? 64 * WAVES / threads : 1);
             const dim3 grid(uint32_t(M < together ? M : together)), block(uint32_t(threads), 1, 1);
             if (betas) norm_residual_kernel<decltype(e), L, true, ROWS><<<grid, block, 0, s>>>(a);
             else norm_residual_kernel<decltype(e), L, false, ROWS><<<grid, block, 0, s>>>(a);

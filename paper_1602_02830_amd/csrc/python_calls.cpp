@@ -68,6 +68,7 @@ struct EntryPoints {
                                   void*, int64_t, void*, int64_t, void*, int64_t, float*, float*, float*, float*, int64_t, int64_t,
                                   void*, int64_t, void*);
     int (*quantize_rows)(int, int, const void*, int64_t, uint8_t*, int64_t, void*, int64_t, void*, int64_t, int64_t, int64_t, void*);
+    int (*dequantize_rows)(int, int, const uint8_t*, int64_t, const void*, int64_t, void*, int64_t, int64_t, int64_t, void*);
     int (*norm_residual_q)(int, const void*, int64_t, const void*, int64_t, const void*, int64_t, int64_t, float, int, const float*,
                            const float*, int, const float*, const float*, float, void*, int64_t, int, uint8_t*, int64_t, void*, int64_t,
                            void*, int64_t, int64_t, int64_t, void*);
@@ -567,6 +568,18 @@ PyObject* quantize_rows(PyObject* const* a) {
     });
 }
 
+// (kind, K, codes, scales, out)
+PyObject* dequantize_rows(PyObject* const* a) {
+    Matrix out;
+    Rows q;
+    if (!q.read(a) || !read_real(a[4], out, nullptr, 0, 0) || !q.of(*out.t, out.rows, out.cols)) return long_way();
+    count_write(out);
+    return launch(*out.t, [&](void* s) {
+        return entry.dequantize_rows(q.kind, real_type(out.t->scalar_type()), q.codes.as<uint8_t>(), q.codes.ld, q.scales, q.ld_s,
+                                     out.data, out.ld, out.rows, out.cols, s);
+    });
+}
+
 // (y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, out, kind, K, codes, scales, hat)
 PyObject* norm_residual_q(PyObject* const* a) {
     Matrix y, x, gate, out, hat;
@@ -833,6 +846,7 @@ PyObject* bind(PyObject*, PyObject* args) {
     set(e.norm_residual_backward_workspace, "bnn_norm_residual_backward_workspace");
     set(e.norm_residual_backward, "bnn_norm_residual_backward");
     set(e.quantize_rows, "bnn_quantize_rows");
+    set(e.dequantize_rows, "bnn_dequantize_rows");
     set(e.norm_residual_q, "bnn_norm_residual_q");
     set(e.linear_q_bits, "bnn_linear_q_bits");
     set(e.gated_q_bits, "bnn_gated_q_bits");
@@ -875,6 +889,7 @@ PyMethodDef methods[] = {
     fast<gated_bits_backward, 9>("gated_bits_backward"),
     fast<norm_residual_backward, 16>("norm_residual_backward"),
     fast<quantize_rows, 6>("quantize_rows"),
+    fast<dequantize_rows, 5>("dequantize_rows"),
     fast<norm_residual_q, 18>("norm_residual_q"),
     fast<linear_q_bits, 10>("linear_q_bits"),
     fast<gated_q_bits, 9>("gated_q_bits"),

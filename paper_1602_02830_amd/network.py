@@ -369,7 +369,7 @@ class BinaryFeedForward:
         got = B.norm_residual_backward(dr, dn_after, y, r, self._gate_of(y), self.res_scale, B.NORM_RMS, self.post_gamma, None, B.NORM_RMS,
                                        self.next_gamma, None, self.eps, max(y.shape[0], 1))
         if self.rows is not None:              # the values that the codes stand for
-            n, h = B.dequantize_rows(n, y.dtype), B.dequantize_rows(h, y.dtype)
+            n, h = (B.dequantize_rows(q, out=y.new_empty(q.shape)) for q in (n, h))
         dgate = torch.zeros_like(self.gate) if self.gate is not None and y.shape[0] == 0 else got["dgate"]
         out = B.linear_bits_backward(got["dy"], h, self.w_out, self.scale_out)
         gated = B.gated_bits_backward(out["dx"], n, self.w_in, self.scale_in, None, self.act)

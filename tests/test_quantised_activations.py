@@ -473,7 +473,8 @@ def test_wrappers_and_native_calls_agree(kind, monkeypatch):
         y = bnn.linear_q_bits(q, p.wd, p.scaled, p.biased, out=torch.empty(9, 64, dtype=torch.float16, device=DEV))
         h = bnn.gated_q_bits(n, p.wd, p.scaled, p.biased, out=torch.empty(9, 32, device=DEV))
         hq = bnn.gated_q_bits(n, p.wd, p.scaled, p.biased, out_q=bnn.quantized_rows(9, 32, bnn.ROWS_MX4, DEV, torch.float32))
-        return [q.codes, q.hat, r, n.codes, n.hat, y, h, hq.codes, hq.hat]
+        back = bnn.dequantize_rows(n, out=torch.empty(9, 130, device=DEV))
+        return [q.codes, q.hat, r, n.codes, n.hat, y, h, hq.codes, hq.hat, back]
 
     bnn.load_library()
     native = calls()
@@ -605,6 +606,7 @@ def test_refusals_of_the_wrappers():
     refuses(lambda: bnn.dequantize_rows(q, torch.float64))
     refuses(lambda: bnn.dequantize_rows(q, out=torch.empty(4, 63, device=DEV)))
     refuses(lambda: bnn.dequantize_rows(R(bnn.ROWS_I8, 64, q.codes, q.scales)))
+    refuses(lambda: bnn.dequantize_rows(x))
     refuses(lambda: bnn.linear_q_bits(x, w))
     refuses(lambda: bnn.linear_q_bits(x, w, out=torch.empty(4, 8, device=DEV)))
     refuses(lambda: bnn.linear_q_bits(q, w[:, :1]))
