@@ -1247,7 +1247,7 @@ def gated_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | N
     if _calls is not None and (out is not None) != (out_q is not None) and out_kind is None and isinstance(x, QuantizedRows):
         st = _calls.gated_q_bits(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out) if out_q is None else \
             _calls.gated_q_bits_rows(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out_q.kind, out_q.K, out_q.codes,
-                                     out_q.scales, out_q.hat)
+                                     out_q.scales, out_q.hat, _TYPES.get(_result_type(x, out_q.hat, None, dtype), -1))
         if st == 0 or _took("bnn_gated_q_bits", st):
             return out if out_q is None else out_q
     if out is not None and (out_q is not None or out_kind is not None):

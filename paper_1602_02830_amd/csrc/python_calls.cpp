@@ -653,20 +653,21 @@ PyObject* gated_q_bits(PyObject* const* a) {
     });
 }
 
-// (kind, K, codes, scales, w_bits, scale, bias, act, kind, F, codes, scales and hat of the result)
+// (kind, K, codes, scales, w_bits, scale, bias, act, kind, F, codes, scales and hat of the result, its bnn_type)
 PyObject* gated_q_bits_rows(PyObject* const* a) {
     QWeighted p;
     Rows q;
     Matrix hat;
-    int act;
-    if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[7], act) || !q.read(a + 8) || q.kind != 1 ||
-        !q.of(*p.w.t, p.x.codes.rows, p.w.rows / 2) || (a[12] != Py_None && !p.read_out(a[12], hat, p.w.rows / 2)))
+    int act, type;
+    if (!p.read(a) || p.w.rows % 2 != 0 || !small_integer(a[7], act) || !small_integer(a[13], type) || type < 0 || !q.read(a + 8) || q.kind != 1 ||
+        !q.of(*p.w.t, p.x.codes.rows, p.w.rows / 2) ||
+        (a[12] != Py_None && (!p.read_out(a[12], hat, p.w.rows / 2) || real_type(hat.t->scalar_type()) != type)))
         return long_way();
     q.count_written();
     count_write(hat);
     return launch(*p.w.t, [&](void* s) {
         return entry.gated_q_bits(p.x.kind, p.x.codes.as<uint8_t>(), p.x.codes.ld, p.x.scales, p.x.ld_s, p.w.as<uint32_t>(), p.w.ld,
-                                  p.scale, p.bias, act, hat.t ? real_type(hat.t->scalar_type()) : 0, hat.data, hat.ld,
+                                  p.scale, p.bias, act, type, hat.data, hat.ld,
                                   q.codes.as<uint8_t>(), q.codes.ld, static_cast<uint8_t*>(q.scales), q.ld_s, q.codes.rows, q.K,
                                   p.x.K, s);
     });
@@ -893,7 +894,7 @@ PyMethodDef methods[] = {
     fast<norm_residual_q, 18>("norm_residual_q"),
     fast<linear_q_bits, 10>("linear_q_bits"),
     fast<gated_q_bits, 9>("gated_q_bits"),
-    fast<gated_q_bits_rows, 13>("gated_q_bits_rows"),
+    fast<gated_q_bits_rows, 14>("gated_q_bits_rows"),
     {nullptr, nullptr, 0, nullptr},
 };
 

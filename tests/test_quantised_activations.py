@@ -626,6 +626,28 @@ def test_refusals_of_the_wrappers():
     refuses(lambda: bnn.norm_residual_q(x, x[:3], pre=bnn.NORM_RMS))
 
 
+def test_the_type_of_a_quantised_result_reaches_the_library(monkeypatch):
+    """Activations are as accurate as the result's type asks: that of h^, else `dtype`, else of x^, else bfloat16; by the native call
+    path as by the other."""
+    got = []
+
+    class Calls:
+        @staticmethod
+        def gated_q_bits_rows(*a):
+            got.append(a[-1])
+            return 0
+
+    monkeypatch.setattr(binding, "_calls", Calls)
+    types = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+    w = torch.zeros(8, 2, dtype=torch.int32)
+    for x_type in (None, torch.float16):
+        for dtype in (None, torch.float32):
+            for hat in (None, torch.bfloat16):
+                x, out = bnn.quantized_rows(4, 64, bnn.ROWS_I8, "cpu", x_type), bnn.quantized_rows(4, 4, bnn.ROWS_MX4, "cpu", hat)
+                assert bnn.gated_q_bits(x, w, dtype=dtype, out_q=out) is out
+                assert got.pop() == types[hat or dtype or x_type or torch.bfloat16]
+
+
 # ---- differentiation ---------------------------------------------------------------------------------------------------
 
 @gpu
