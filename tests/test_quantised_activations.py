@@ -626,6 +626,19 @@ def test_refusals_of_the_wrappers():
     refuses(lambda: bnn.norm_residual_q(x, x[:3], pre=bnn.NORM_RMS))
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_what_is_no_rows_is_refused(native, monkeypatch):
+    """As any other argument: by a ValueError, before the GPU or a native call sees it."""
+    if not native:
+        monkeypatch.setattr(binding, "_calls", None)
+    x, w, q = torch.zeros(4, 64), torch.zeros(8, 2, dtype=torch.int32), bnn.quantized_rows(4, 64, bnn.ROWS_MX4, "cpu")
+    for bad in (lambda: bnn.quantize_rows(x, out=x), lambda: bnn.quantize_rows(torch.zeros(4, requires_grad=True)),
+                lambda: bnn.norm_residual_q(x, out_q=x), lambda: bnn.norm_residual_q(x, out=x, out_q=x), lambda: bnn.gated_q_bits(q, w, out_q=x),
+                lambda: bnn.gated_q_bits(q, w, out_kind=bnn.ROWS_I8, out_q=q)):
+        with pytest.raises(ValueError):
+            bad()
+
+
 def test_the_type_of_a_quantised_result_reaches_the_library(monkeypatch):
     """Activations are as accurate as the result's type asks: that of h^, else `dtype`, else of x^, else bfloat16; by the native call
     path as by the other."""
