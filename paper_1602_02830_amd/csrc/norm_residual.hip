@@ -414,7 +414,8 @@ extern "C" int bnn_norm_residual_q(int type, const void* y, int64_t ld_y, const 
                                          res_scale, eps, post, pre, 0, 0};
     int st = check_norm(type, a, M, D);
     if (st == BNN_OK) st = check_rows(rows, codes, ld_c, scales, ld_s, M, D);
-    if (st != BNN_OK || M == 0 || D == 0) return st;
+    if (st != BNN_OK || M == 0) return st;
+    if (D == 0) return bnn_quantize_rows(rows, type, nullptr, 0, codes, ld_c, scales, ld_s, nullptr, 0, M, 0, stream);      // scales of rows of nothing
     if (!y) return BNN_ERR_INVALID_ARG;
     a.out = QuantOut{codes, scales, hat, ld_c, ld_s, ld_h};
     return rows == BNN_ROWS_I8 ? launch_norm<BNN_ROWS_I8>(type, a, M, D, stream) : launch_norm<BNN_ROWS_MX4>(type, a, M, D, stream);

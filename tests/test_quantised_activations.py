@@ -410,6 +410,18 @@ def test_products_of_nothing(kind):
 
 
 @gpu
+def test_scales_of_rows_of_nothing():
+    """The least one, from quantisation and from the norm alike; MX4 rows of nothing have no block."""
+    x = torch.empty(5, 0, device=DEV)
+    for give in (lambda q: bnn.quantize_rows(x, out=q), lambda q: bnn.norm_residual_q(x, pre=bnn.NORM_RMS, out_q=q, need_r=False)):
+        q = bnn.quantized_rows(5, 0, bnn.ROWS_I8, DEV)
+        q.scales.fill_(NAN)
+        give(q)
+        assert torch.equal(q.scales.cpu(), torch.full((5,), 2.0 ** -126))
+    assert bnn.norm_residual_q(x, pre=bnn.NORM_RMS, kind=bnn.ROWS_MX4, need_r=False)[1].shape == (5, 0)
+
+
+@gpu
 @pytest.mark.parametrize("kind", list(KINDS))
 def test_products_of_nan_rows(kind):
     """A row (8 bits) or block (4 bits) that stands for NaN makes its own row of the result NaN, no other."""
