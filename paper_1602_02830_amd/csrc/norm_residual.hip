@@ -81,11 +81,16 @@ struct NormRowsArgs : NormArgs {
 
 constexpr int kReals = -1;                   // in the place of a bnn_rows: n as it is
 
-// Wavefronts of a compute unit that walk over rows and give codes: as many as are there together, so that no workgroup begins
-// when others end (16384 x 4096 bfloat16, root-mean-square norms, with 16: 138 us with codes of 8 bits and n^, 121 with those of 4; with
-// 12 125 and 116, 4.8 TB/s, and 100 and 88 without n^).  A third sum over the workgroup for the scale is what 8 bits cost more; in registers for
-// 16 wavefronts (128 of them) the kernels spill 60 bytes and take 143 and 137 us.
-constexpr int kNormRowsWaves = 12;
+// Wavefronts of a compute unit that walk over rows and give codes: as many as are there together, so that no workgroup begins when others
+// end.  16384 x 4096 bfloat16, root-mean-square norms, with codes of 8 bits and n^, on the same matrices again and again: 100 us,
+// 6.0 TB/s (on others each time 123, 4.9 TB/s), with 16 wavefronts 116, with 8 116; of 4 bits 93, without n^
+// 89 and 76.  Rows of one group a lane take fewer registers: 100000 x 300 with 16 85, with 12 93.  A third sum over the
+// workgroup for the scale is what 8 bits cost more; in registers for 16 wavefronts (128 of them) the kernels spill 60 bytes (143 for then 125 us).
+//
+// r, codes and n^ are stored past the cache: 100 us are 125 otherwise, for 1000 rows 9.0 are 11.2.  Not in float32 with n^, whose lanes have two
+// pieces of 16 bytes side by side, so that no store fills a line: 16384 x 4096 235 us instead of 169, without n^ 116 instead of 121.
+template <typename L>
+constexpr int kNormRowsWaves = L::CH == 1 ? 16 : 12;
 
 // BETAS: a norm has one.
 template <typename E, typename L, bool BETAS, int ROWS = kReals>
@@ -131,15 +136,21 @@ __global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const type
             v[i][e] = a.x ? xv[i][e] + t : t;
         });
         trim<L>(v, D);           // 0 * inf of a scale that is none must not reach the sums from columns that are not there
-        if (a.r) store_row<E, L>(static_cast<E*>(a.r) + m * a.ld_r, D, v);
+        if (a.r) {
+            E* const r = static_cast<E*>(a.r) + m * a.ld_r;
+            bool past = ROWS != kReals;
+            if constexpr (ROWS != kReals && is_f32<E>) past = !a.out.hat;
+            if (past) store_row<E, L, ROWS != kReals>(r, D, v);
+            else store_row<E, L>(r, D, v);
+        }
         if (a.pre != BNN_NORM_NONE) {
             normalise<L>(a.pre, v, D, a.eps, sums);
             each<L>([&](int i, int e) { v[i][e] *= pre_g[i][e]; });
             if constexpr (BETAS) each<L>([&](int i, int e) { v[i][e] += pre_b[i][e]; });
             if constexpr (ROWS == kReals) store_row<E, L>(static_cast<E*>(a.n) + m * a.ld_n, D, v);
         }
-        if constexpr (ROWS == BNN_ROWS_I8) store_row_i8<E, L>(a.out, m, D, v, largest);
-        if constexpr (ROWS == BNN_ROWS_MX4) store_row_mx4<E, L>(a.out, m, D, v);
+        if constexpr (ROWS == BNN_ROWS_I8) store_row_i8<E, L, !is_f32<E>>(a.out, m, D, v, largest);
+        if constexpr (ROWS == BNN_ROWS_MX4) store_row_mx4<E, L, !is_f32<E>>(a.out, m, D, v);
     }
 }
 
@@ -377,7 +388,7 @@ int launch_norm(int type, A a, int64_t M, int64_t D, void* stream) {
             using L = decltype(layout);
             // As many workgroups as are on the chip together, each walking over rows.
             const int threads = L::threads(D);
-            constexpr int WAVES = ROWS == kReals ? kNormWaves : kNormRowsWaves;
+            constexpr int WAVES = ROWS == kReals ? kNormWaves : kNormRowsWaves<L>;
             const int64_t together = 256 * (64 * WAVES / threads > 0 ? 64 * WAVES / threads : 1);
             const dim3 grid(uint32_t(M < together ? M : together)), block(uint32_t(threads), 1, 1);
             if (betas) norm_residual_kernel<decltype(e), L, true, ROWS><<<grid, block, 0, s>>>(a);

@@ -118,15 +118,7 @@ __device__ inline void store_results(const QProductArgs& a, int m, int n, float 
             for (int i = 0; i < W; ++i) v[i] += r[i];
         }
     }
-    E* const y = static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n;
-    if (PAST && valid >= W) {
-        typename Group<E, W>::type o;
-#pragma unroll
-        for (int i = 0; i < W; ++i) o[i] = E(v[i]);
-        __builtin_nontemporal_store(o, reinterpret_cast<typename Group<E, W>::any*>(y));
-    } else {
-        store_group<E, W>(y, v, valid);
-    }
+    store_group<E, W, PAST>(static_cast<E*>(a.y) + int64_t(m) * a.ld_y + n, v, valid);
 }
 
 // All lanes of a quad that has a block of 32 columns come here together (W = 8).

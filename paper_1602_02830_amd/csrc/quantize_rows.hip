@@ -14,8 +14,9 @@ struct QuantiseArgs {
     FastDiv by_row;          // 4 bits: by the groups of eight elements of a row
 };
 
-// Wavefronts of a compute unit that walk over rows: 16384 x 4096 bfloat16 46 us without x^ (with 16 wavefronts 53, with 28 51), 65 with it
-// (68 and 74), 16384 x 8192 from memory 94 and 131.
+// Wavefronts of a compute unit that walk over rows: 16384 x 4096 bfloat16 45 us without x^ (4.5 TB/s; with 16 wavefronts 52, with 32 47), 56 with
+// it (6.0 TB/s; 58 and 61), on the same matrix again and again; 16384 x 8192 with it, on another each time, 124 (5.4 TB/s).  4-bit codes, whose
+// rows need no second look, 24 and 43.
 constexpr int kQuantiseWaves = 24;
 
 // A row in the registers of its workgroup: its largest magnitude, then its codes.  Workgroups walk over rows, the next row's loads

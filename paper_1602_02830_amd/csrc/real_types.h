@@ -80,13 +80,16 @@ __device__ inline typename Group<E, G>::type row_end(typename Group<E, G>::type 
     return left > 0 ? v : typename Group<E, G>::type{};
 }
 
-template <typename E, int G>
+// PAST: whole groups go past the cache.
+template <typename E, int G, bool PAST = false>
 __device__ inline void store_group(E* p, const float (&v)[G], int64_t valid) {
+    typedef typename Group<E, G>::any any;
     typename Group<E, G>::type o;
 #pragma unroll
     for (int i = 0; i < G; ++i) o[i] = E(v[i]);
     if (valid >= G) {
-        *reinterpret_cast<typename Group<E, G>::any*>(p) = o;
+        if constexpr (PAST) __builtin_nontemporal_store(o, reinterpret_cast<any*>(p));
+        else *reinterpret_cast<any*>(p) = o;
     } else {
 #pragma unroll
         for (int i = 0; i < G - 1; ++i)

@@ -128,20 +128,28 @@ struct Row {
     }
 };
 
+// Zero past the row's end: the unit checks the bound (333 x 2049 float16 with layer norms 9.0 us instead of 9.4 with row_end for vectors too).
 template <typename L>
 __device__ inline void load_vector(const float* p, int D, float otherwise, Values<L>& v) {
     if (!p) return each<L>([&](int i, int e) { v[i][e] = otherwise; });
-    Row<float, L> row;
-    row.load(p, 0, 0, D);
-    row.widened(D, v);
+    constexpr int kWords = 0x00027000;               // data format: 32 bits
+    const auto vector = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, D * 4, kWords);
+#pragma unroll
+    for (int i = 0; i < L::CH; ++i)
+#pragma unroll
+        for (int q = 0; q < L::G / 4; ++q) {
+            const auto words = __builtin_amdgcn_raw_buffer_load_b128(vector, (L::first_col(i) + 4 * q) * 4, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][4 * q + e] = __uint_as_float(words[e]);
+        }
 }
 
-template <typename E, typename L>
+template <typename E, typename L, bool PAST = false>
 __device__ inline void store_row(E* row, int D, const Values<L>& v) {
 #pragma unroll
     for (int i = 0; i < L::CH; ++i) {
         const int c = L::first_col(i);
-        if (c < D) store_group<E, L::G>(row + c, v[i], D - c);
+        if (c < D) store_group<E, L::G, PAST>(row + c, v[i], D - c);
     }
 }
 
@@ -172,7 +180,7 @@ __device__ inline void trim(Values<L>& v, int D) {
 }
 
 // Codes, scale and x^ of a row whose elements past its end are zero.
-template <typename E, typename L>
+template <typename E, typename L, bool PAST = true>
 __device__ inline void store_row_i8(const QuantOut& o, int64_t m, int D, const Values<L>& v, Largest<L::WAVES>& largest) {
     uint32_t most = 0;
 #pragma unroll
@@ -182,16 +190,16 @@ __device__ inline void store_row_i8(const QuantOut& o, int64_t m, int D, const V
 #pragma unroll
     for (int i = 0; i < L::CH; ++i) {
         const int c = L::first_col(i);
-        if ((c & ~31) < D) quantise_i8<E>(o, m, c, v[i], s, D);
+        if ((c & ~31) < D) quantise_i8<E, PAST>(o, m, c, v[i], s, D);
     }
 }
 
-template <typename E, typename L>
+template <typename E, typename L, bool PAST = true>
 __device__ inline void store_row_mx4(const QuantOut& o, int64_t m, int D, const Values<L>& v) {
 #pragma unroll
     for (int i = 0; i < L::CH; ++i) {
         const int c = L::first_col(i);
-        if ((c & ~31) < D) quantise_mx4<E>(o, m, c, v[i], D);
+        if ((c & ~31) < D) quantise_mx4<E, PAST>(o, m, c, v[i], D);
     }
 }
 
