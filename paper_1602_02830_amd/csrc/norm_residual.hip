@@ -14,7 +14,7 @@
 // gradient of each norm.  A workgroup walks a strip of rows and keeps the sums over rows (of the gammas, betas and the gate) in
 // registers, the gammas and the beta in LDS; strips' sums are joined by a second launch in a fixed order.  16384 x 4096 bfloat16:
 // 176 us, 4.6 TB/s; 10000 x 2049 float32 with layer norms, a gate and all their gradients 179 us, 2.8 TB/s: five sums over rows instead of
-// two, for which 256 registers are 36 bytes a lane too few, in three wavefronts of whose 3072 places a third are empty.  Rows past 8192
+// two, for which 256 registers are 36 bytes a lane too few, in three wavefronts of whose places a third are empty.  Rows past 8192
 // elements do not fit the registers: 324 - 596 bytes a lane go to scratch memory (4000 x 16000 bfloat16: 555 us, 1.4 TB/s), forwards
 // 28 - 316 (118 us).
 #include "join_sums.h"

@@ -807,3 +807,65 @@ def test_block_is_near_the_real_one(kind):
     size = n.abs().sum(1, keepdim=True) * real.scale_in.max()
     # |z| <= size; either z is off by (D + 12) 2^-24 size, its activation by 1.2 times that and 32 2^-24 (1 + size), h by both times size.
     assert ((a - b).abs() <= 64 * D * F32 * (1 + size) ** 2).all()
+
+
+def block_of(kind, D, F):
+    g = torch.Generator(device=DEV).manual_seed(21)
+    return bnn.BinaryFeedForward(torch.randn(2 * F, D, device=DEV, generator=g), torch.randn(D, F, device=DEV, generator=g), rows=KINDS[kind],
+                                 post_gamma=torch.rand(D, device=DEV, generator=g) + 0.5, next_gamma=torch.rand(D, device=DEV, generator=g) + 0.5)
+
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_a_captured_training_step(kind):
+    """Forwards and backwards in one graph, replayed with new inputs and eager work between: bit for bit the eager step."""
+    M, D, F = 150, 96, 200
+    block = block_of(kind, D, F)
+    g = torch.Generator(device=DEV).manual_seed(22)
+    x, dr, dn = (torch.randn(M, D, device=DEV, generator=g).bfloat16() for _ in range(3))
+
+    def step():
+        r, after = block.forward(x, block.first_norm(x), keep=True)
+        dx, dn_before = block.backward(dr, dn)
+        scales = after.scales if kind == "i8" else after.scales[:, :D // 32]         # bytes past them mean nothing
+        return [r, after.codes, scales, dx, dn_before, *(block.grads[k] for k in ("w_in", "w_out", "scale_in", "scale_out", "next_gamma"))]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for _ in range(4):
+        x.copy_(torch.randn(M, D, device=DEV, generator=g).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        have = [t.clone() for t in captured]
+        want = step()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(have, want)):
+            assert torch.equal(a, b), i
+
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_two_streams_at_once(kind):
+    """Calls on two streams share nothing: rows, products and norms of each come out as they do alone."""
+    M, D, F = 700, 512, 1000
+    block = block_of(kind, D, F)
+    g = torch.Generator(device=DEV).manual_seed(23)
+    xs = [torch.randn(M, D, device=DEV, generator=g).bfloat16() for _ in range(2)]
+    alone = [block.forward(x, block.first_norm(x)) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = []
+    for _ in range(5):
+        for s, x in zip(streams, xs):
+            with torch.cuda.stream(s):
+                got.append(block.forward(x, block.first_norm(x)))
+    torch.cuda.synchronize()
+    for i, (r, after) in enumerate(got):
+        assert torch.equal(r, alone[i % 2][0]) and torch.equal(after.codes, alone[i % 2][1].codes), i
