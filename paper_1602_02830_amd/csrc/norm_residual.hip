@@ -106,11 +106,13 @@ __global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const type
     y.load(a.y, m, a.ld_y, D);
     if (a.x) x.load(a.x, m, a.ld_x, D);
     if (a.gate) gate.load(a.gate, gate_row, a.ld_gate, D);
-    load_vector<L>(a.post_gamma, D, 1.0f, post_g);
-    load_vector<L>(a.pre_gamma, D, 1.0f, pre_g);
+    // 4000 x 16000 bfloat16 with betas 188 us as rows, 226 otherwise.
+    constexpr bool AS_ROW = BETAS && L::WAVES == 16;
+    load_vector<L, AS_ROW>(a.post_gamma, D, 1.0f, post_g);
+    load_vector<L, AS_ROW>(a.pre_gamma, D, 1.0f, pre_g);
     if constexpr (BETAS) {
-        load_vector<L>(a.post_beta, D, 0.0f, post_b);
-        load_vector<L>(a.pre_beta, D, 0.0f, pre_b);
+        load_vector<L, AS_ROW>(a.post_beta, D, 0.0f, post_b);
+        load_vector<L, AS_ROW>(a.pre_beta, D, 0.0f, pre_b);
     }
     for (; m < a.M; m += gridDim.x) {
         Values<L> v, xv, g;

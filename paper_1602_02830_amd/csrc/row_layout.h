@@ -129,9 +129,15 @@ struct Row {
 };
 
 // Zero past the row's end: the unit checks the bound (333 x 2049 float16 with layer norms 9.0 us instead of 9.4 with row_end for vectors too).
-template <typename L>
+// AS_ROW: as a row instead, for a kernel that has too few registers either way and keeps fewer in scratch memory so.
+template <typename L, bool AS_ROW = false>
 __device__ inline void load_vector(const float* p, int D, float otherwise, Values<L>& v) {
     if (!p) return each<L>([&](int i, int e) { v[i][e] = otherwise; });
+    if constexpr (AS_ROW) {
+        Row<float, L> row;
+        row.load(p, 0, 0, D);
+        return row.widened(D, v);
+    }
     constexpr int kWords = 0x00027000;               // data format: 32 bits
     const auto vector = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, D * 4, kWords);
 #pragma unroll
