@@ -350,7 +350,7 @@ class BinaryFeedForward:
         y, r = x.new_empty((M, self.D)), x.new_empty((M, self.D))
         h, after = (B.quantized_rows(M, cols, self.rows, x.device) for cols in (self.F, self.D))
         if self.rows == B.ROWS_MX4:
-            B.gated_q_bits(n, self.w_in, self.scale_in, None, self.act, out_q=h)
+            B.gated_q_bits(n, self.w_in, self.scale_in, None, self.act, x.dtype, out_q=h)
         else:
             B.quantize_rows(B.gated_q_bits(n, self.w_in, self.scale_in, None, self.act, out=x.new_empty((M, self.F))), out=h)
         B.linear_q_bits(h, self.w_out, self.scale_out, out=y)

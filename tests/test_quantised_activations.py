@@ -673,6 +673,33 @@ def test_the_type_of_a_quantised_result_reaches_the_library(monkeypatch):
                 assert got.pop() == types[hat or dtype or x_type or torch.bfloat16]
 
 
+@pytest.mark.parametrize("T", list(TYPES))
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_the_type_of_the_blocks_stream_reaches_the_library(kind, T, monkeypatch):
+    """The block's activations are as accurate as its stream: its gated product gets the stream's type, whether its result is quantised
+    there (4 bits) or written out (8)."""
+    got = []
+
+    class Calls:
+        @staticmethod
+        def gated_q_bits_rows(*a):
+            got.append(a[-1])
+            return 0
+
+        @staticmethod
+        def gated_q_bits(*a):
+            got.append(binding._TYPES[a[-1].dtype])
+            return 0
+
+    for name in ("quantize_rows", "linear_q_bits", "norm_residual_q"):
+        setattr(Calls, name, staticmethod(lambda *a: 0))
+    monkeypatch.setattr(binding, "_calls", Calls)
+    monkeypatch.setattr(binding, "pack_sign", lambda w: torch.zeros(w.shape[0], (w.shape[1] + 31) // 32, dtype=torch.int32))
+    block = bnn.BinaryFeedForward(torch.randn(2 * 40, 64), torch.randn(64, 40), rows=KINDS[kind])
+    block.forward(torch.zeros(3, 64, dtype=TYPES[T]), bnn.quantized_rows(3, 64, KINDS[kind], "cpu"))
+    assert got == [binding._TYPES[TYPES[T]]]
+
+
 # ---- differentiation ---------------------------------------------------------------------------------------------------
 
 @gpu
@@ -789,6 +816,21 @@ def test_block(M, kind, T):
         block.forward(x, x)
     with pytest.raises(ValueError):
         bnn.BinaryFeedForward(w_in, w_out, rows=7)
+
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_a_float32_block_of_many_values(kind):
+    """600 000 hidden values, some of them next to a border between two codes: the block's are those of a float32 gated product."""
+    M, D, F = 300, 256, 2000
+    block = block_of(kind, D, F)
+    x = torch.randn(M, D, device=DEV, generator=torch.Generator(device=DEV).manual_seed(6))
+    n = block.first_norm(x)
+    r, after = block.forward(x, n)
+    h = bnn.gated_q_bits(n, block.w_in, block.scale_in, dtype=torch.float32, out_kind=bnn.ROWS_MX4 if kind == "mx4" else None)
+    y = bnn.linear_q_bits(h if kind == "mx4" else bnn.quantize_rows(h, KINDS[kind]), block.w_out, block.scale_out, dtype=torch.float32)
+    want_r, want = bnn.norm_residual_q(y, x, post=bnn.NORM_RMS, post_gamma=block.post_gamma, pre=bnn.NORM_RMS, pre_gamma=block.next_gamma, kind=KINDS[kind])
+    assert torch.equal(r, want_r) and torch.equal(after.codes, want.codes)
 
 
 @gpu
