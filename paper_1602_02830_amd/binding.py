@@ -1004,9 +1004,12 @@ def _rows_at(q: QuantizedRows, M: int, K: int, device, name: str):
     return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
 
 
-def _given_rows(q, name: str):
+def _given_rows(q, name: str, kind: int | None = None):
+    """Rows that a caller gives for the result, of the kind beside them if there is one."""
     if q is not None and not isinstance(q, QuantizedRows):
         raise ValueError(f"{name} must be QuantizedRows")
+    if q is not None and kind not in (None, q.kind):
+        raise ValueError(f"{name} is not of the kind asked for")
 
 
 def _count_rows(q: QuantizedRows | None):
@@ -1028,14 +1031,16 @@ class _QuantizeRows(torch.autograd.Function):
         return dhat, None
 
 
-def quantize_rows(x: torch.Tensor, kind: int = ROWS_I8, hat: bool = False, out: QuantizedRows | None = None) -> QuantizedRows:
-    """bnn_quantize_rows: real rows [M][K] as codes with scales; `hat`: x^ too.  Without `out`, of rows that require a gradient, x^ is
-    always made, and torch differentiates it as if it were x."""
-    _given_rows(out, "out")
+def quantize_rows(x: torch.Tensor, kind: int | None = None, hat: bool = False, out: QuantizedRows | None = None) -> QuantizedRows:
+    """bnn_quantize_rows: real rows [M][K] as codes with scales, of the kind of `out`, else of `kind`, ROWS_I8 if there is neither;
+    `hat`: x^ too.  Without `out`, of rows that require a gradient, x^ is always made, and torch differentiates it as if it were x."""
+    _given_rows(out, "out", kind)
     if out is not None and _calls is not None:
         st = _calls.quantize_rows(x, out.kind, out.K, out.codes, out.scales, out.hat)
         if st == 0 or _took("bnn_quantize_rows", st):
             return out
+    if out is None and kind is None:
+        kind = ROWS_I8
     if out is None and _recorded(x):
         q = _QuantizeRows.apply(x, kind)
         return QuantizedRows(kind, x.shape[1], *q)
@@ -1098,17 +1103,19 @@ class _NormResidualQ(torch.autograd.Function):
 def norm_residual_q(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.Tensor | None = None, res_scale: float = 1.0,
                     post: int = NORM_NONE, post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None,
                     pre: int = NORM_NONE, pre_gamma: torch.Tensor | None = None, pre_beta: torch.Tensor | None = None,
-                    eps: float = 1e-5, rows_per_gate: int = 1, kind: int = ROWS_I8, out: torch.Tensor | None = None,
+                    eps: float = 1e-5, rows_per_gate: int = 1, kind: int | None = None, out: torch.Tensor | None = None,
                     out_q: QuantizedRows | None = None, need_r: bool = True, hat: bool = False):
-    """bnn_norm_residual_q: norm_residual whose n (r, without a `pre` norm) comes as codes with scales: (r, QuantizedRows), with x^ where
-    `hat` or out_q has it.  Without `out` and `out_q`, of tensors that require a gradient, n^ is always made, and torch differentiates
-    it as if it were n."""
-    _given_rows(out_q, "out_q")
+    """bnn_norm_residual_q: norm_residual whose n (r, without a `pre` norm) comes as codes with scales: (r, QuantizedRows), of the kind
+    of out_q, else of `kind`, ROWS_I8 if there is neither, with x^ where `hat` or out_q has it.  Without `out` and `out_q`, of tensors
+    that require a gradient, n^ is always made, and torch differentiates it as if it were n."""
+    _given_rows(out_q, "out_q", kind)
     if out is not None and out_q is not None and _calls is not None:
         st = _calls.norm_residual_q(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
                                     out, out_q.kind, out_q.K, out_q.codes, out_q.scales, out_q.hat)
         if st == 0 or _took("bnn_norm_residual_q", st):
             return out, out_q
+    if out_q is None and kind is None:
+        kind = ROWS_I8
     if out is None and out_q is None and _recorded(y, x, gate, post_gamma, post_beta, pre_gamma, pre_beta):
         r, *q = _NormResidualQ.apply(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate, kind)
         return (r if need_r else None), QuantizedRows(kind, y.shape[1], *q)
@@ -1252,7 +1259,7 @@ def gated_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | N
     with z = scale * (x^ w^T) + bias.  With out_kind ROWS_MX4, or rows out_q of that kind, the result is QuantizedRows for the product
     that reads it (of ROWS_I8 a row's scale needs the whole row: quantize_rows makes them).  Types and differentiation as of
     linear_q_bits; of a quantised result torch differentiates h^ as if it were h."""
-    _given_rows(out_q, "out_q")
+    _given_rows(out_q, "out_q", out_kind)
     if _calls is not None and (out is not None) != (out_q is not None) and out_kind is None and isinstance(x, QuantizedRows):
         st = _calls.gated_q_bits(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out) if out_q is None else \
             _calls.gated_q_bits_rows(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out_q.kind, out_q.K, out_q.codes,
@@ -1262,8 +1269,6 @@ def gated_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | N
     if out is not None and (out_q is not None or out_kind is not None):
         raise ValueError("the result is either real (out) or quantised (out_kind, out_q)")
     if out_q is not None:
-        if out_kind not in (None, out_q.kind):
-            raise ValueError("out_q is not of the kind out_kind")
         out_kind = out_q.kind
     if out_kind is not None and out_kind != ROWS_MX4:
         raise ValueError("a quantised result is of ROWS_MX4: quantize_rows makes the rows of ROWS_I8")

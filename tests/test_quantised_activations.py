@@ -651,6 +651,26 @@ def test_what_is_no_rows_is_refused(native, monkeypatch):
             bad()
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_another_kind_than_that_of_given_rows_is_refused(native, monkeypatch):
+    """Before anything is written.  Rows that are given without a kind beside them keep theirs."""
+    class Calls:
+        quantize_rows = norm_residual_q = staticmethod(lambda *a: 0)
+
+    monkeypatch.setattr(binding, "_calls", Calls if native else None)
+    x = torch.zeros(4, 64)
+    for kind, other in ((bnn.ROWS_I8, bnn.ROWS_MX4), (bnn.ROWS_MX4, bnn.ROWS_I8)):
+        q = bnn.quantized_rows(4, 64, kind, "cpu")
+        for bad in (lambda: bnn.quantize_rows(x, other, out=q), lambda: bnn.norm_residual_q(x, kind=other, out=x, out_q=q),
+                    lambda: bnn.norm_residual_q(x, kind=other, out_q=q)):
+            with pytest.raises(ValueError, match="kind"):
+                bad()
+        if native:
+            for fine in (None, kind):
+                assert bnn.quantize_rows(x, fine, out=q) is q and bnn.norm_residual_q(x, kind=fine, out=x, out_q=q)[1] is q
+            assert bnn.quantize_rows(x, out=q) is q and bnn.norm_residual_q(x, out=x, out_q=q)[1] is q
+
+
 def test_the_type_of_a_quantised_result_reaches_the_library(monkeypatch):
     """Activations are as accurate as the result's type asks: that of h^, else `dtype`, else of x^, else bfloat16; by the native call
     path as by the other."""
