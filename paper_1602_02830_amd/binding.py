@@ -1004,12 +1004,14 @@ def _rows_at(q: QuantizedRows, M: int, K: int, device, name: str):
     return c.data_ptr(), _ld(c), s.data_ptr(), _ld(s)
 
 
-def _given_rows(q, name: str, kind: int | None = None):
-    """Rows that a caller gives for the result, of the kind beside them if there is one."""
+def _given_rows(q, name: str, kind: int | None, hat: bool):
+    """Rows that a caller gives for the result: of the kind beside them if there is one, with a place for x^ if that is asked for."""
     if q is not None and not isinstance(q, QuantizedRows):
         raise ValueError(f"{name} must be QuantizedRows")
     if q is not None and kind not in (None, q.kind):
         raise ValueError(f"{name} is not of the kind asked for")
+    if q is not None and hat and q.hat is None:
+        raise ValueError(f"{name} has no hat to write x^ to")
 
 
 def _count_rows(q: QuantizedRows | None):
@@ -1034,7 +1036,7 @@ class _QuantizeRows(torch.autograd.Function):
 def quantize_rows(x: torch.Tensor, kind: int | None = None, hat: bool = False, out: QuantizedRows | None = None) -> QuantizedRows:
     """bnn_quantize_rows: real rows [M][K] as codes with scales, of the kind of `out`, else of `kind`, ROWS_I8 if there is neither;
     `hat`: x^ too.  Without `out`, of rows that require a gradient, x^ is always made, and torch differentiates it as if it were x."""
-    _given_rows(out, "out", kind)
+    _given_rows(out, "out", kind, hat)
     if out is not None and _calls is not None:
         st = _calls.quantize_rows(x, out.kind, out.K, out.codes, out.scales, out.hat)
         if st == 0 or _took("bnn_quantize_rows", st):
@@ -1108,7 +1110,7 @@ def norm_residual_q(y: torch.Tensor, x: torch.Tensor | None = None, gate: torch.
     """bnn_norm_residual_q: norm_residual whose n (r, without a `pre` norm) comes as codes with scales: (r, QuantizedRows), of the kind
     of out_q, else of `kind`, ROWS_I8 if there is neither, with x^ where `hat` or out_q has it.  Without `out` and `out_q`, of tensors
     that require a gradient, n^ is always made, and torch differentiates it as if it were n."""
-    _given_rows(out_q, "out_q", kind)
+    _given_rows(out_q, "out_q", kind, hat)
     if out is not None and out_q is not None and _calls is not None:
         st = _calls.norm_residual_q(y, x, gate, res_scale, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, eps, rows_per_gate,
                                     out, out_q.kind, out_q.K, out_q.codes, out_q.scales, out_q.hat)
@@ -1259,7 +1261,7 @@ def gated_q_bits(x: QuantizedRows, w_bits: torch.Tensor, scale: torch.Tensor | N
     with z = scale * (x^ w^T) + bias.  With out_kind ROWS_MX4, or rows out_q of that kind, the result is QuantizedRows for the product
     that reads it (of ROWS_I8 a row's scale needs the whole row: quantize_rows makes them).  Types and differentiation as of
     linear_q_bits; of a quantised result torch differentiates h^ as if it were h."""
-    _given_rows(out_q, "out_q", out_kind)
+    _given_rows(out_q, "out_q", out_kind, hat)
     if _calls is not None and (out is not None) != (out_q is not None) and out_kind is None and isinstance(x, QuantizedRows):
         st = _calls.gated_q_bits(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out) if out_q is None else \
             _calls.gated_q_bits_rows(x.kind, x.K, x.codes, x.scales, w_bits, scale, bias, act, out_q.kind, out_q.K, out_q.codes,

@@ -671,6 +671,27 @@ def test_another_kind_than_that_of_given_rows_is_refused(native, monkeypatch):
             assert bnn.quantize_rows(x, out=q) is q and bnn.norm_residual_q(x, out=x, out_q=q)[1] is q
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_given_rows_without_a_place_for_the_values_asked_for_are_refused(native, monkeypatch):
+    """hat=True with rows that have no hat: by a ValueError, before anything is written."""
+    class Calls:
+        quantize_rows = norm_residual_q = gated_q_bits_rows = staticmethod(lambda *a: 0)
+
+    monkeypatch.setattr(binding, "_calls", Calls if native else None)
+    x, w = torch.zeros(4, 64), torch.zeros(128, 2, dtype=torch.int32)
+    n = bnn.quantized_rows(4, 64, bnn.ROWS_I8, "cpu")
+    calls = {"quantise": lambda q, hat: bnn.quantize_rows(x, hat=hat, out=q), "norm": lambda q, hat: bnn.norm_residual_q(x, out=x, out_q=q, hat=hat)[1],
+             "norm alone": lambda q, hat: bnn.norm_residual_q(x, out_q=q, need_r=False, hat=hat)[1],
+             "gated": lambda q, hat: bnn.gated_q_bits(n, w, out_q=q, hat=hat),
+             "gated, kind": lambda q, hat: bnn.gated_q_bits(n, w, out_kind=q.kind, out_q=q, hat=hat)}
+    for name, call in calls.items():
+        without, with_hat = (bnn.quantized_rows(4, 64, bnn.ROWS_MX4, "cpu", T) for T in (None, torch.float32))
+        with pytest.raises(ValueError, match="hat"):
+            call(without, True)
+        if native and name in ("quantise", "norm", "gated"):
+            assert call(without, False) is without and call(with_hat, True) is with_hat and call(with_hat, False) is with_hat
+
+
 def test_the_type_of_a_quantised_result_reaches_the_library(monkeypatch):
     """Activations are as accurate as the result's type asks: that of h^, else `dtype`, else of x^, else bfloat16; by the native call
     path as by the other."""
