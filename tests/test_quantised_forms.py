@@ -1,4 +1,5 @@
-"""The kernels behind products of quantised rows, each against the definition in 64 bits at sizes that it is taken for.
+"""The kernels behind products of quantised rows, each against the definition in 64 bits at sizes that it is taken for; and norms and
+quantisation of more rows than workgroups.
 
 FORMS names the kernel of each shape.  A host test asks the library which one it launches (nothing runs), so that a change of the rule that
 chooses them cannot leave one of them without a test; the GPU tests compare the same shapes.  Rows and channels fit no tile; K ends
@@ -13,9 +14,10 @@ import pytest
 import torch
 
 import paper_1602_02830_amd as bnn
-from test_launch_limits import A, B, C, CHILD, LIB, OUT, RUNTIME
-from test_quantised_activations import INF, KINDS, MX4, NAN, placed, result
-from test_real_activations import ACTS, DEV, F32, rounded
+from test_launch_limits import A, B, C, CHILD, LIB, OUT, RUNTIME, launches_of  # noqa: F401
+from test_quantised_activations import INF, KINDS, MX4, NAN, check_codes, placed, result
+from test_quantised_activations import test_norm as norm_against_its_definition
+from test_real_activations import ACTS, DEV, F32, NORMS, ROUND, TINY, TYPES, rounded
 
 gpu = pytest.mark.gpu
 
@@ -258,3 +260,113 @@ def test_nan_rows_of_each_form(kind, form, M, N, K):
     assert there.any(1).nonzero().flatten().tolist() == bad and there.all(1).nonzero().flatten().tolist() == bad
     h = bnn.gated_q_bits(q, w, out_kind=bnn.ROWS_MX4, hat=True)
     assert torch.isnan(h.hat).any(1).nonzero().flatten().tolist() == bad and torch.isnan(h.hat).all(1).nonzero().flatten().tolist() == bad
+
+
+# ---- rows that are walked over ------------------------------------------------------------------------------------------
+# Workgroups of the norms and of the quantisation to 8 bits take one row after another; from the third on they use every buffer again.
+
+#: (M, D) of rows in 1, 1, 1, 3, 4, 5, 8, 16 and 16 wavefronts: three rows a workgroup and more.
+WALKED = [(13000, 5), (13000, 300), (13000, 777), (4200, 2049), (3300, 4096), (2600, 5000), (1700, 8192), (600, 9001), (600, 16384)]
+#: And of rows that are read twice.
+LONG = (1100, 16385)
+PART = 200                                   # rows of which no workgroup has a second one
+
+
+def quantise_call(kind, type_, M, K):
+    blocks = (K + 31) // 32
+    return "bnn_quantize_rows", (KINDS[kind], type_, A, K, B, blocks * 32, C, (blocks + 15) // 16 * 16, 0, 0, M, K, 0)
+
+
+def norm_call(kind, type_, M, D, beta):
+    """Without its two floats, which travel in registers of their own."""
+    blocks = (D + 31) // 32
+    return "bnn_norm_residual_q", (type_, A, D, 0, 0, 0, 0, 1, 2, 0, beta, 2, 0, beta, 0, 0, KINDS[kind], B, blocks * 32, C, (blocks + 15) // 16 * 16, 0, 0, M, D, 0)
+
+
+def test_workgroups_take_rows_one_after_another(launches_of):  # noqa: F811
+    for type_ in range(3):
+        for M, D in [*WALKED, LONG]:
+            calls = [quantise_call("i8", type_, M, D)]
+            if (M, D) != LONG:
+                calls += [norm_call(kind, type_, M, D, beta) for kind in KINDS for beta in (0, OUT)]
+            for (st, log), (name, _) in zip(launches_of(*calls), calls):
+                assert st == 0 and len(log) == 1 and PART <= log[0][0] and 2 * log[0][0] < M, (name, M, D, log)
+
+
+def part_of(q, a, b):
+    return bnn.QuantizedRows(q.kind, q.K, q.codes[a:b], q.scales[a:b], None if q.hat is None else q.hat[a:b])
+
+
+def same_rows(q, own, what):
+    blocks = (q.K + 31) // 32
+    assert torch.equal(q.codes, own.codes) and torch.equal(q.hat, own.hat), what
+    assert torch.equal(q.scales, own.scales) if q.kind == bnn.ROWS_I8 else torch.equal(q.scales[:, :blocks], own.scales[:, :blocks]), what
+
+
+def rows_of_many_sizes(M, D, T, seed):
+    """Rows whose magnitudes differ: what is left of another row shows."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(M, D, device=DEV, generator=g) * torch.exp2(torch.randint(-6, 7, (M, 1), device=DEV, generator=g).float())
+    x[5 % M] = 0
+    return x.to(T)
+
+
+@gpu
+@pytest.mark.parametrize("T", list(TYPES))
+@pytest.mark.parametrize("M,D", [*WALKED, LONG])
+def test_quantise_more_rows_than_workgroups(M, D, T):
+    """Each row is what it is by itself, bit for bit; the first, some and the last against the definition, with x^ in the rows' own
+    place too."""
+    x = rows_of_many_sizes(M, D, TYPES[T], 1)
+    q = bnn.quantize_rows(x, bnn.ROWS_I8, hat=True)
+    for a in range(0, M, PART):
+        same_rows(part_of(q, a, a + PART), bnn.quantize_rows(x[a:a + PART], bnn.ROWS_I8, hat=True), a)
+    for a in (0, M // 2 + 3, M - 16):
+        check_codes(part_of(q, a, a + 16), x[a:a + 16].cpu())
+    place = bnn.QuantizedRows(bnn.ROWS_I8, D, torch.empty_like(q.codes), torch.empty_like(q.scales), x)
+    same_rows(bnn.quantize_rows(x, out=place), q, "in place")
+
+
+@gpu
+@pytest.mark.parametrize("T,post,pre,gate_rows", [("bf16", "layer", "rms", 7), ("f16", "rms", "layer", 2500), ("f32", "rms", "rms", 0), ("f32", "layer", "layer", 1)])
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("M,D", WALKED)
+def test_norms_of_more_rows_than_workgroups(M, D, kind, T, post, pre, gate_rows):
+    """r, codes, scales and n^ of each row are what it gets by itself, bit for bit, with a gate whose row changes on the way; with r in the
+    stream's place too.  Gammas and betas begin at any multiple of four bytes."""
+    T, kind = TYPES[T], KINDS[kind]
+    y, x = rows_of_many_sizes(M, D, T, 2), rows_of_many_sizes(M, D, T, 3)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    R = gate_rows or M
+    gate = (1 + 0.3 * torch.randn(-(-M // R), D, device=DEV, generator=g)).to(T) if gate_rows else None
+    per_row = gate.repeat_interleave(R, 0)[:M] if gate_rows else None
+    vectors = [torch.randn(D + 1, device=DEV, generator=g)[i % 2:D + i % 2] for i in range(4)]
+    post_args = (NORMS[post], vectors[0], vectors[1] if post == "layer" else None)
+    pre_args = (NORMS[pre], vectors[2], vectors[3] if pre == "layer" else None, 1e-5)
+    r, q = bnn.norm_residual_q(y, x, gate, 0.5, *post_args, *pre_args, R, kind, hat=True)
+    real_r, n = bnn.norm_residual(y, x, gate, 0.5, *post_args, *pre_args, R)
+    assert torch.equal(r, real_r)
+    for a in range(0, M, PART):
+        b = min(a + PART, M)
+        own_r, own = bnn.norm_residual_q(y[a:b], x[a:b], per_row[a:b] if gate_rows else None, 0.5, *post_args, *pre_args, 1, kind, hat=True)
+        assert torch.equal(own_r, r[a:b]), a
+        same_rows(part_of(q, a, b), own, a)
+    place = x.clone()
+    got = bnn.norm_residual_q(y, place, gate, 0.5, *post_args, *pre_args, R, out=place, out_q=bnn.quantized_rows(M, D, kind, DEV, T))
+    assert torch.equal(place, r)
+    same_rows(got[1], q, "in place")
+    # Codes are those of n but for its rounding: half a step, and half a unit of n and of n^ (two norms are equal to 2^-20 of the row).
+    c, s = decoded(q)
+    value = (c * s[:, :, None]).reshape(M, -1)[:, :D]
+    step = (s if kind == bnn.ROWS_I8 else 2 * s)[:, :, None].expand(c.shape).reshape(M, -1)[:, :D]
+    n = n.double()
+    assert ((value - n).abs() <= 0.5 * step + ROUND[T] * n.abs() + 2.0 ** -20 * n.abs().amax(1, keepdim=True) + TINY[T]).all()
+
+
+@gpu
+@pytest.mark.parametrize("T", list(TYPES))
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("post,pre", [("layer", "layer"), ("none", "layer"), ("layer", "none")])
+def test_norms_of_long_rows_with_betas(post, pre, kind, T):
+    """Past 8192 elements, against the definition."""
+    norm_against_its_definition(3, 9001, post, pre, True, kind, T)
