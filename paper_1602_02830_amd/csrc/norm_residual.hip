@@ -106,8 +106,9 @@ __global__ __launch_bounds__(64 * L::WAVES) void norm_residual_kernel(const type
     y.load(a.y, m, a.ld_y, D);
     if (a.x) x.load(a.x, m, a.ld_x, D);
     if (a.gate) gate.load(a.gate, gate_row, a.ld_gate, D);
-    // 4000 x 16000 bfloat16 with betas 188 us as rows, 226 otherwise.
-    constexpr bool AS_ROW = BETAS && L::WAVES == 16;
+    // 4000 x 16000 bfloat16 with betas 188 us as rows, 226 otherwise; without betas 300 x 16384 float32 42 and 49, one row of 16000 float32
+    // 14.0 and 16.1, of bfloat16 6.7 and 7.0.
+    constexpr bool AS_ROW = L::WAVES == 16 && (BETAS || ROWS == kReals);
     load_vector<L, AS_ROW>(a.post_gamma, D, 1.0f, post_g);
     load_vector<L, AS_ROW>(a.pre_gamma, D, 1.0f, pre_g);
     if constexpr (BETAS) {
@@ -264,9 +265,11 @@ __global__ __launch_bounds__(64 * L::WAVES) __attribute__((amdgpu_waves_per_eu((
     if (first < last) {
         load(first);
         Values<L> v;
-        load_vector<L>(a.post_gamma, D, 1.0f, v);
+        // 1000 x 16000 bfloat16 147 us as rows, 156 otherwise; with betas 100 x 9001 85 and 78.
+        constexpr bool AS_ROW = L::WAVES == 16 && !BETAS;
+        load_vector<L, AS_ROW>(a.post_gamma, D, 1.0f, v);
         kept.put(kPostGamma, v);
-        load_vector<L>(a.pre_gamma, D, 1.0f, v);
+        load_vector<L, AS_ROW>(a.pre_gamma, D, 1.0f, v);
         kept.put(kPreGamma, v);
         if constexpr (BETAS && Kept<L>::kThree) {
             load_vector<L>(a.post_beta, D, 0.0f, v);
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(64 * L::WAVES) __attribute__((amdgpu_waves_per_eu((
             if constexpr (BETAS) {
                 Values<L> beta;
                 if constexpr (Kept<L>::kThree) kept.get(kPostBeta, beta);
-                else load_vector<L>(a.post_beta, D, 0.0f, beta);
+                else load_vector<L, is_f32<E>>(a.post_beta, D, 0.0f, beta);      // 4000 x 9001 float32 1239 us as rows, 1279 otherwise
                 each<L>([&](int i, int e) { sum_gate[i][e] = fmaf(d[i][e], beta[i][e], sum_gate[i][e]); });
             }
             if (a.strips.per_gate == 0 && (m + 1 == last || m + 1 == gate_end)) {
