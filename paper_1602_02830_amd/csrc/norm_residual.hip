@@ -84,7 +84,7 @@ constexpr int kReals = -1;                   // in the place of a bnn_rows: n as
 // Wavefronts of a compute unit that walk over rows and give codes: as many as are there together, so that no workgroup begins when others
 // end.  16384 x 4096 bfloat16, root-mean-square norms, with codes of 8 bits and n^, on the same matrices again and again: 100 us,
 // 6.0 TB/s (on others each time 123, 4.9 TB/s), with 16 wavefronts 116, with 8 116; of 4 bits 93, without n^
-// 89 and 76.  Rows of one group a lane take fewer registers: 100000 x 300 with 16 85, with 12 93.  A third sum over the
+// 89 and 76 (on others each time 103 and 89).  Rows of one group a lane take fewer registers: 100000 x 300 with 16 85, with 12 93.  A third sum over the
 // workgroup for the scale is what 8 bits cost more; in registers for 16 wavefronts (128 of them) the kernels spill 60 bytes (143 for then 125 us).
 //
 // r, codes and n^ are stored past the cache: 100 us are 125 otherwise, for 1000 rows 9.0 are 11.2.  Not in float32 with n^, whose lanes have two

@@ -37,7 +37,8 @@ __global__ __launch_bounds__(64 * L::WAVES) void quantise_i8_kernel(const Quanti
     }
 }
 
-// Rows of any length, read twice, the second time from the cache.
+// Rows of any length, read twice, the second time from the cache where that holds what is on its way: 4096 x 20000 bfloat16 93 us, 2.6 TB/s, with
+// x^ 105; 1000 x 65536 71.
 template <typename E>
 __global__ __launch_bounds__(1024) void quantise_i8_long_kernel(const QuantiseArgs a) {
     __shared__ uint32_t largest_s[2 * 16];
@@ -83,6 +84,7 @@ __global__ __launch_bounds__(256) void quantise_mx4_kernel(const QuantiseArgs a)
     });
 }
 
+// 16384 x 4096 to bfloat16 42 us from 8 bits (4.9 TB/s), 40 from 4; to float32 78 and 79.
 template <typename E, int ROWS>
 __global__ __launch_bounds__(256) void dequantise_kernel(const QuantiseArgs a) {
     each_group(a.by_row, 4 * ((a.K + 31) >> 5), a.M, [&](int64_t m, int64_t c) {
