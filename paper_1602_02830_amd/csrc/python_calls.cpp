@@ -755,8 +755,9 @@ PyObject* product_backward(PyObject* const* a) {
     const at::ScalarType type = p.x.t->scalar_type();
     if (need_dx) out[0] = empty_like(*p.x.t, {M, K}, type);
     if (need_dw) out[1] = empty_like(*p.x.t, {N, K}, type);
-    if (p.scale) out[2] = empty_like(*p.x.t, {N}, at::kFloat);
-    if (p.bias) out[3] = empty_like(*p.x.t, {N}, at::kFloat);
+    // By what is given: a vector of nothing has no address.
+    if (a[3] != Py_None) out[2] = empty_like(*p.x.t, {N}, at::kFloat);
+    if (a[4] != Py_None) out[3] = empty_like(*p.x.t, {N}, at::kFloat);
     int status;
     if (!run(*p.x.t, status, [&](void* s) {
             return (GATED ? entry.gated_bits_backward : entry.linear_bits_backward)(
@@ -794,9 +795,9 @@ PyObject* norm_residual_backward(PyObject* const* a) {
     if (need_dx) out[0] = empty_like(*y.t, {M, D}, type);
     out[1] = empty_like(*y.t, {M, D}, type);
     if (gate.t) out[2] = empty_like(*y.t, {gate.rows, D}, type);
-    const float* const vectors[4] = {post_gamma, post_beta, pre_gamma, pre_beta};
+    PyObject* const vectors[4] = {a[7], a[8], a[10], a[11]};
     for (int i = 0; i < 4; ++i)
-        if (vectors[i]) out[3 + i] = empty_like(*y.t, {D}, at::kFloat);
+        if (vectors[i] != Py_None) out[3 + i] = empty_like(*y.t, {D}, at::kFloat);
     int status;
     if (!run(*y.t, status, [&](void* s) {
             return entry.norm_residual_backward(

@@ -14,6 +14,7 @@ import pytest
 import torch
 
 import paper_1602_02830_amd as bnn
+from paper_1602_02830_amd import binding
 from test_launch_limits import A, B, C, CHILD, LIB, OUT, RUNTIME, launches_of  # noqa: F401
 from test_quantised_activations import INF, KINDS, MX4, NAN, check_codes, placed, result
 from test_quantised_activations import test_norm as norm_against_its_definition
@@ -370,3 +371,39 @@ def test_norms_of_more_rows_than_workgroups(M, D, kind, T, post, pre, gate_rows)
 def test_norms_of_long_rows_with_betas(post, pre, kind, T):
     """Past 8192 elements, against the definition."""
     norm_against_its_definition(3, 9001, post, pre, True, kind, T)
+
+
+# ---- nothing ----------------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("kind", [*KINDS, "real"])
+@pytest.mark.parametrize("M,N,K", [(0, 64, 96), (5, 0, 96), (5, 64, 0)])
+def test_gradients_of_nothing(M, N, K, kind, native, monkeypatch):
+    """No rows, no channels, no elements: gradients of the inputs' sizes, of zeros where nothing comes in; of real rows too."""
+    if not native:
+        monkeypatch.setattr(binding, "_calls", None)
+    x = torch.randn(M, K, device=DEV, requires_grad=True)
+    w = torch.zeros(N, (K + 31) // 32, dtype=torch.int32, device=DEV)
+    s, b = (torch.ones(N, device=DEV, requires_grad=True) for _ in range(2))
+    if kind == "real":
+        results = [bnn.linear_bits(x, w, s, b), bnn.gated_bits(x, w, s, b, ACTS["none"])]
+    else:
+        q = bnn.quantize_rows(x, KINDS[kind])
+        results = [bnn.linear_q_bits(q, w, s, b), bnn.gated_q_bits(q, w, s, b, ACTS["none"]),
+                   bnn.gated_q_bits(q, w, s, b, ACTS["none"], out_kind=bnn.ROWS_MX4).hat]
+    for y in results:
+        dx, ds, db = torch.autograd.grad(y, (x, s, b), torch.ones_like(y), retain_graph=True)
+        assert dx.shape == x.shape and ds.shape == s.shape and db.shape == b.shape
+        assert (dx == 0).all() and (K > 0 or (ds == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_norm_gradients_of_rows_of_nothing(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(binding, "_calls", None)
+    y, gamma, beta = (torch.randn(*s, device=DEV, requires_grad=True) for s in ((5, 0), (0,), (0,)))
+    for n in (bnn.norm_residual(y, pre=bnn.NORM_LAYER, pre_gamma=gamma, pre_beta=beta)[1],
+              bnn.norm_residual_q(y, pre=bnn.NORM_LAYER, pre_gamma=gamma, pre_beta=beta)[1].hat):
+        assert [g.shape for g in torch.autograd.grad(n, (y, gamma, beta), torch.ones_like(n))] == [(5, 0), (0,), (0,)]
