@@ -373,6 +373,49 @@ def test_norms_of_long_rows_with_betas(post, pre, kind, T):
     norm_against_its_definition(3, 9001, post, pre, True, kind, T)
 
 
+# ---- matrices past 2^31 elements ------------------------------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_matrices_of_more_than_2_31_elements(kind):
+    """Rows, results, codes and x^ on both sides of the 2^31st element, and the last ones, are what they are in a small call.  Sums are exact."""
+    M, K, N, kind = (1 << 19) + 700, 4128, 4160, KINDS[kind]
+    assert M * K > 1 << 31 < M * N
+    g = torch.Generator(device=DEV).manual_seed(8)
+    few = torch.randint(-6, 7, (1000, K), device=DEV, generator=g).bfloat16()
+    few[:, ::32] = 6 if kind == bnn.ROWS_MX4 else 127             # steps of 1
+    few[few.abs() == 5] = 4                                       # not a code of 4 bits
+    x = few[torch.arange(M, device=DEV) % 1000]
+    w, gate = bnn.pack_sign(torch.randn(N, K, device=DEV, generator=g)), bnn.pack_sign(torch.randn(2 * N, K, device=DEV, generator=g))
+    q = bnn.quantize_rows(x, kind, hat=True)
+    assert torch.equal(q.hat, x) and torch.equal(bnn.dequantize_rows(q, torch.bfloat16), x)
+    r, n = bnn.norm_residual_q(x, x, None, 0.5, pre=bnn.NORM_RMS, kind=kind, hat=True)
+    y = bnn.linear_q_bits(q, w, dtype=torch.float32)
+    h = bnn.gated_q_bits(q, gate, act=ACTS["none"], dtype=torch.bfloat16)
+    hq = bnn.gated_q_bits(q, gate, act=ACTS["none"], dtype=torch.bfloat16, out_kind=bnn.ROWS_MX4, hat=True)
+    assert torch.equal(bnn.dequantize_rows(hq, torch.bfloat16), hq.hat)
+    for a in (0, (1 << 31) // N - 100, (1 << 31) // K - 100, M - 200):
+        b = a + 200
+        own = bnn.quantize_rows(x[a:b], kind, hat=True)
+        same_rows(part_of(q, a, b), own, a)
+        own_r, own_n = bnn.norm_residual_q(x[a:b], x[a:b], None, 0.5, pre=bnn.NORM_RMS, kind=kind, hat=True)
+        assert torch.equal(r[a:b], own_r), a
+        same_rows(part_of(n, a, b), own_n, a)
+        assert torch.equal(y[a:b], bnn.linear_q_bits(own, w, dtype=torch.float32)), a
+        assert torch.equal(h[a:b], bnn.gated_q_bits(own, gate, act=ACTS["none"], dtype=torch.bfloat16)), a
+        same_rows(part_of(hq, a, b), bnn.gated_q_bits(own, gate, act=ACTS["none"], dtype=torch.bfloat16, out_kind=bnn.ROWS_MX4, hat=True), a)
+
+
+@gpu
+def test_more_groups_than_one_launch_of_4_bit_rows_holds():
+    """2^31 groups of eight elements and more: rows of one element, quantised and made reals of again."""
+    M = (1 << 29) + 1000
+    x = torch.randint(-4, 5, (M, 1), device=DEV, dtype=torch.int8, generator=torch.Generator(device=DEV).manual_seed(9)).bfloat16()
+    q = bnn.quantize_rows(x, bnn.ROWS_MX4, hat=True)              # every number up to 4 is a code times a power of two
+    assert torch.equal(q.hat, x)
+    assert torch.equal(bnn.dequantize_rows(q, torch.bfloat16), x)
+
+
 # ---- nothing ----------------------------------------------------------------------------------------------------
 
 @gpu
