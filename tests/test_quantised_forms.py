@@ -222,11 +222,9 @@ def test_gated_of_each_form(kind, form, M, N, K):
         assert (codes[M] == 0xA5).all() and (codes[:, 16 * blocks:] == 0xA5).all() and (scales[M] == 0xA5).all() and (scales[:, blocks:] == 0xA5).all()
 
 
-@gpu
-@pytest.mark.parametrize("kind,form,M,N,K", ALL)
-def test_exact_sums_of_each_form(kind, form, M, N, K):
+def exact_sums(M, N, K, kind):
     """Rows whose sums float32 holds exactly in any order: every element and every sign counts, to the last bit.  8 bits: whole numbers
-    up to 127 with scales that are powers of two; 4 bits: codes with four scales, multiples of 1/2 below 48 K < 2^18."""
+    up to 127 with scales that are powers of two; 4 bits: codes with four scales, multiples of 1/2 below 48 K < 2^19."""
     p = Product(M, N, K, kind)
     g = torch.Generator(device=DEV).manual_seed(2)
     if kind == "i8":
@@ -242,8 +240,34 @@ def test_exact_sums_of_each_form(kind, form, M, N, K):
     assert torch.equal((c * steps[:, :, None]).reshape(M, -1)[:, :K], x)
     sums = x @ p.w.t()
     assert torch.equal(bnn.linear_q_bits(q, p.wd, dtype=torch.float32).double(), sums)
-    h = sums[:, :N // 2] * sums[:, N // 2:]
-    assert torch.equal(bnn.gated_q_bits(q, p.wd, act=ACTS["none"], dtype=torch.float32), h.float())
+    if N % 2 == 0:
+        h = sums[:, :N // 2] * sums[:, N // 2:]
+        assert torch.equal(bnn.gated_q_bits(q, p.wd, act=ACTS["none"], dtype=torch.float32), h.float())
+
+
+@gpu
+@pytest.mark.parametrize("kind,form,M,N,K", ALL)
+def test_exact_sums_of_each_form(kind, form, M, N, K):
+    exact_sums(M, N, K, kind)
+
+
+#: Tiles of 16 rows: runs of 512 elements by one wavefront to eight and more, that end inside a block of 32 and a piece of four.
+SMALL = [(1, 64, 32), (3, 18, 40), (16, 48, 512), (2, 34, 513), (5, 100, 1030), (17, 96, 4096), (8, 40, 8200), (33, 130, 700), (1, 8192, 4096), (9, 20, 5000),
+         (16, 200, 1057), (40, 64, 1569), (66, 33, 545), (80, 1800, 97), (100, 1002, 333), (1, 2, 1)]
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_few_rows_take_small_tiles(kernels_of, kind):
+    names = kernels_of(*(library_call(kind, gated, M, N, K, 0) for M, N, K in SMALL for gated in (False, True) if not gated or N % 2 == 0))
+    assert all("q_small_kernel" in name for name in names)
+    assert len(set(names)) == 4              # one block of channels and two, linear and gated
+
+
+@gpu
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("M,N,K", SMALL)
+def test_exact_sums_of_small_tiles(M, N, K, kind):
+    exact_sums(M, N, K, kind)
 
 
 @gpu
